@@ -354,6 +354,98 @@ size_t abq_gemm_grouped_workspace_bytes(int p, int q, int M, int count, const ab
 int abq_gemm_grouped(int p, int q, int M, int count, const abq_problem* host_problems,
                      int a_layout, int w_layout, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The attention half of a decoder block, for many requests at once: what lies between the q / k / v projections and the
+ * output projection (rotation, paged cache, attention), and the requests' own low-rank adapters beside the projections.
+ * All tensors are binary16, as the projections write them; queries, keys and values may be column ranges of one fused
+ * projection's output (row strides in elements, a multiple of 8).
+ * ------------------------------------------------------------------------------------------ */
+
+/* Keys and values of one layer, in pages handed out to sequences by the caller.  Vector (page, head, offset) lies at
+ * ((page * heads + head) * page_size + offset) * head_dim elements.
+ *   kv_bits    16: binary16 values.  8: codes 0..255 (one byte each) with a scale and a zero-point per vector, the
+ *              quantizer of abq_quant_pack_act with q = 8 on the binary16 vector; value = scale * (code - zero).
+ *   page_size  tokens per page: a power of two, 16..4096;  head_dim a multiple of 16, 16..256;  num_pages, heads >= 1
+ *   k, v       [num_pages][heads][page_size][head_dim] binary16 or uint8
+ *   k_scale, v_scale [num_pages][heads][page_size] float;  k_zero, v_zero the same of uint8 (a zero-point of 8-bit codes
+ *              fits a byte, and a decoding step reads one per vector).  NULL when kv_bits is 16. */
+typedef struct abq_kv_cache {
+    int kv_bits, num_pages, page_size, heads, head_dim;
+    void *k, *v;
+    float* k_scale;
+    uint8_t* k_zero;
+    float* v_scale;
+    uint8_t* v_zero;
+} abq_kv_cache;
+
+/* The rows of one step: `rows` new tokens of `seqs` sequences, sequence s owning rows row_start[s] .. row_start[s+1] - 1.
+ * Row i of a sequence with n rows stands at position lens[s] - n + i.
+ *   row_start [seqs+1] int32, ascending from 0;  lens [seqs] int32: tokens of each sequence, the new ones among them
+ *   pages     [seqs][max_pages] int32: token t of sequence s lies in page pages[s][t / page_size], at offset t % page_size
+ *   max_new   no sequence has more rows in this step;  max_len: no sequence has more tokens.  They size the launches
+ *             (abq_attn_paged): close bounds are faster ones.  1 <= max_new <= rows, 1 <= max_len.
+ * The arrays are device memory and never checked on the host.  Whatever they hold, nothing outside the tensors is read or
+ * written: rows behind row_start[seqs] are left as they were; a page number outside 0..num_pages-1 (-1, say) is a page
+ * that is not there - nothing is appended to it and attention does not see its tokens; tokens beyond max_pages pages and
+ * positions below 0 likewise.  abq_attn_paged leaves rows from max_new on as they were and sees no token from max_len on. */
+typedef struct abq_batch {
+    int rows, seqs, max_pages, max_new, max_len;
+    const int32_t *row_start, *lens, *pages;
+} abq_batch;
+
+/* Puts the rows' keys and values into the cache, at their positions, the keys rotated to them on the way, and rotates the
+ * rows' queries (optional):
+ *   (x[j], x[j + r/2]) -> (x[j] cos a - x[j + r/2] sin a, x[j + r/2] cos a + x[j] sin a),  a = position * inv_freq[j],  j < r/2
+ * with r = rotary_dim (0: no rotation, inv_freq not read; elements from r on are kept); `interleaved`: the pairs are
+ * (x[2j], x[2j+1]).  The angle is formed and reduced in binary64 (positions are exact however far), sine and cosine are
+ * within 2^-23, products and sum in binary32, one rounding to binary16.  A cache of codes quantizes the rotated binary16
+ * vector.
+ *   heads_q    query heads (with q), a multiple of cache->heads;  rotary_dim a multiple of 16, 0..head_dim
+ *   q [rows][heads_q * head_dim] (NULL to skip), k, v [rows][heads * head_dim] with row strides ldq, ldk, ldv in elements
+ *   inv_freq   [rotary_dim / 2] float
+ *   q_out      [rows][heads_q * head_dim], contiguous; it may be q itself where that is contiguous too
+ * Two rows of a call never name the same place unless two sequences share a page that both write (or a page stands twice in
+ * a sequence); which of the rows' elements such a place then holds is unspecified.  NaN/Inf inputs: undefined for codes. */
+int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, int rotary_dim, int interleaved,
+                  const float* inv_freq, const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv,
+                  uint16_t* q_out, void* stream);
+
+/* Reads vectors back out of the cache (exporting a prefix, checks): for each slot = page * page_size + offset the keys and
+ * values of all heads as binary16, codes as half_rne(scale * (code - zero)).  A slot outside the cache reads as zeros.
+ *   slots [count] int32 (device);  k_out, v_out [count][heads * head_dim];  page numbers up to INT32_MAX / page_size */
+int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint16_t* k_out, uint16_t* v_out, void* stream);
+
+/* Attention of the rows over what the cache holds of their sequences (the new tokens' keys and values among it: append
+ * first).  Query head h reads key head h / (heads_q / heads):
+ *   y[row,h,:] = half_rne( sum_t w_t v_t / sum_t w_t ),  w_t = exp(scale * q . k_t),  over the tokens t the row sees:
+ *   all of its sequence up to its own position (causal), or all of its sequence (causal = 0).  A row that sees none is zero.
+ * Scores, running maximum, sums and the weighted sum are binary32; the weights are rounded to binary16 for the product with
+ * the values.  What lies in pages beyond a sequence's length, or in tokens that a row does not see, does not reach its output
+ * (NaN and infinities included).
+ *   q [rows][heads_q * head_dim], row stride ldq;  y [rows][heads_q * head_dim], contiguous, not overlapping q
+ *   workspace  at least abq_attn_paged_workspace_bytes(cache, batch, heads_q) bytes (may be 0): the parts of long sequences
+ *              that several workgroups share.  Contents on entry are irrelevant; calls that may overlap need one each.
+ * The order of the binary32 sums depends on max_new, max_len, rows and seqs, not on other sequences' contents. */
+size_t abq_attn_paged_workspace_bytes(const abq_kv_cache* cache, const abq_batch* batch, int heads_q);
+int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, const uint16_t* q, int ldq, float scale,
+                   int causal, uint16_t* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters beside a shared projection, one of many for each row:
+ *   out[m,:] = half_rne( y[m,:] + scale[i] * B_i (A_i x[m,:]) ),  i = ids[m];   out[m,:] = y[m,:] where ids[m] is outside 0..adapters-1
+ * x is the projection's input before quantization (y_fp16_out of the producers above), y its output.  A_i x is summed in
+ * binary32 and enters the second product with 21 bits or more of its row's largest element.
+ *   rank       1..256 (pad smaller adapters of a pool with zeros);  M, N >= 1, 1 <= K <= ABQ_MAX_K
+ *   x [M][K] row stride ldx;  ids [M] int32 (device);  a [adapters][rank][K], b [adapters][N][rank] binary16;
+ *   scale [adapters] float;  y [M][N] row stride ldy;  out [M][N] row stride ldout: y itself (same stride), or no overlap
+ *   (strides in elements, any value >= K or N)
+ * A row's result does not depend on the other rows' adapters or inputs.
+ *   workspace  at least abq_lora_add_workspace_bytes(M, N, K, rank) bytes; contents on entry are irrelevant, calls that may
+ *              overlap need one each. */
+size_t abq_lora_add_workspace_bytes(int M, int N, int K, int rank);
+int abq_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x, int ldx, const int32_t* ids,
+                 const uint16_t* a, const uint16_t* b, const float* scale, const uint16_t* y, int ldy, uint16_t* out, int ldout,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

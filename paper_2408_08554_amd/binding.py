@@ -57,6 +57,13 @@ _SIGNATURES = {
                                                                           _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "abq_gemm_act_codes_requant": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p] * 4 + [_c.c_int, _c.c_int] + [_c.c_void_p] * 5 + [_c.c_size_t, _c.c_void_p]),
     "abq_check_packed": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "abq_kv_append": (_c.c_int, [_c.c_void_p] * 2 + [_c.c_int] * 3 + [_c.c_void_p] + [_c.c_void_p, _c.c_int] * 3 + [_c.c_void_p] * 2),
+    "abq_kv_read": (_c.c_int, [_c.c_void_p, _c.c_int] + [_c.c_void_p] * 4),
+    "abq_attn_paged_workspace_bytes": (_c.c_size_t, [_c.c_void_p, _c.c_void_p, _c.c_int]),
+    "abq_attn_paged": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_void_p, _c.c_int, _c.c_float, _c.c_int, _c.c_void_p, _c.c_void_p,
+                                  _c.c_size_t, _c.c_void_p]),
+    "abq_lora_add_workspace_bytes": (_c.c_size_t, [_c.c_int] * 4),
+    "abq_lora_add": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p, _c.c_int] + [_c.c_void_p] * 4 + [_c.c_void_p, _c.c_int] * 2 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "abq_gemm_act_codes_static": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p] * 4 + [_c.c_int, _c.c_void_p, _c.c_void_p, _c.c_void_p]),
 }
 
@@ -214,6 +221,26 @@ def abq_gemm_grouped_workspace_bytes(p, q, M, problems, a_layout, w_layout):
     return load().abq_gemm_grouped_workspace_bytes(p, q, M, len(arr), _c.addressof(arr), a_layout, w_layout)
 
 
+class AbqKvCache(_c.Structure):
+    """struct abq_kv_cache of include/abq.h; the calls of this module take the cache as a tuple of tensors instead."""
+    _fields_ = [(n, _c.c_int) for n in ("kv_bits", "num_pages", "page_size", "heads", "head_dim")] + \
+               [(n, _c.c_void_p) for n in ("k", "v", "k_scale", "k_zero", "v_scale", "v_zero")]
+
+
+class AbqBatch(_c.Structure):
+    """struct abq_batch of include/abq.h; the calls of this module take the batch as a tuple of tensors instead."""
+    _fields_ = [(n, _c.c_int) for n in ("rows", "seqs", "max_pages", "max_new", "max_len")] + [(n, _c.c_void_p) for n in ("row_start", "lens", "pages")]
+
+
+def abq_attn_paged_workspace_bytes(cache, batch, heads_q):
+    """cache, batch: AbqKvCache and AbqBatch."""
+    return load().abq_attn_paged_workspace_bytes(_c.addressof(cache), _c.addressof(batch), heads_q)
+
+
+def abq_lora_add_workspace_bytes(M, N, K, rank):
+    return load().abq_lora_add_workspace_bytes(M, N, K, rank)
+
+
 class AbqPlan(_c.Structure):
     """struct abq_plan of include/abq.h (0 = keep the library's rule for that knob)."""
     _fields_ = [(n, _c.c_int) for n in ("skinny_waves", "skinny_kgroups", "tiled_mt", "tiled_ntw", "tiled_wd", "tiled_band", "direct_r")]
@@ -247,7 +274,7 @@ def abq_plan_clear():
 # The online calls, from abq_native; their docstrings say what they take and return.
 _NATIVE = ("abq_quant_pack_act", "abq_pack_act_codes", "abq_f4_pack_codes", "abq_rmsnorm_quant_act", "abq_add_rmsnorm_quant_act",
            "abq_silu_mul_quant_act", "abq_gemm", "abq_gemm_act_codes", "abq_gemm_act_codes_requant", "abq_gemm_act_codes_static",
-           "abq_gemm_grouped", "abq_f4_gemm")
+           "abq_gemm_grouped", "abq_f4_gemm", "abq_kv_append", "abq_kv_read", "abq_attn_paged", "abq_lora_add")
 
 
 def _bind():

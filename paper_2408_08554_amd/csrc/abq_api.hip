@@ -3,6 +3,7 @@
 // can be exercised on a machine without a GPU.
 #include "abq_internal.h"
 #include "../../include/abq.h"
+#include "abq_kv.h"
 
 #include <limits.h>
 #include <stdlib.h>
@@ -854,6 +855,114 @@ int abq_gemm_grouped(int p, int q, int M, int count, const abq_problem* host_pro
         if (e != ABQ_OK) return e;
     }
     return ABQ_OK;
+}
+
+// ---- the attention half: paged cache, attention, adapters ----------------------------------------
+// Row strides: a whole number of 16-byte vectors, at least the row.
+static int check_stride(int64_t ld, int64_t width)
+{
+    if (ld < width) return ABQ_ERR_SHAPE;
+    return ld % 8 != 0 ? ABQ_ERR_ALIGN : ABQ_OK;
+}
+
+static int check_cache(const abq_kv_cache* c)
+{
+    if (!c || !c->k || !c->v) return ABQ_ERR_NULL;
+    if (c->kv_bits != 16 && c->kv_bits != 8) return ABQ_ERR_BITS;
+    if (c->kv_bits == 8 && (!c->k_scale || !c->k_zero || !c->v_scale || !c->v_zero)) return ABQ_ERR_NULL;
+    if (c->num_pages < 1 || c->heads < 1 || c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0 ||
+        c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 != 0 || (int64_t)c->heads * c->head_dim > (1 << 20))
+        return ABQ_ERR_SHAPE;
+    if (misaligned(c->k) || misaligned(c->v) || (c->kv_bits == 8 && (misaligned(c->k_scale) || misaligned(c->k_zero) || misaligned(c->v_scale) || misaligned(c->v_zero))))
+        return ABQ_ERR_ALIGN;
+    return ABQ_OK;
+}
+
+static int check_batch(const abq_batch* b)
+{
+    if (!b || !b->row_start || !b->lens || !b->pages) return ABQ_ERR_NULL;
+    if (b->rows < 1 || b->seqs < 1 || b->seqs > 65535 || b->max_pages < 1 || b->max_new < 1 || b->max_new > b->rows || b->max_len < 1) return ABQ_ERR_SHAPE;
+    if (misaligned(b->row_start) || misaligned(b->lens) || misaligned(b->pages)) return ABQ_ERR_ALIGN;
+    return ABQ_OK;
+}
+
+// Query heads: a multiple of the cache's, and rows that stay below 2^20 elements.
+static int check_heads_q(const abq_kv_cache* c, int heads_q)
+{
+    return heads_q < 1 || heads_q % c->heads != 0 || (int64_t)heads_q * c->head_dim > (1 << 20) ? ABQ_ERR_SHAPE : ABQ_OK;
+}
+
+int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, int rotary_dim, int interleaved, const float* inv_freq,
+                  const uint16_t* q, int ldq, const uint16_t* k, int ldk, const uint16_t* v, int ldv, uint16_t* q_out, void* stream)
+{
+    if (!k || !v || (q && !q_out)) return ABQ_ERR_NULL;
+    if (int e = check_cache(cache)) return e;
+    if (int e = check_batch(batch)) return e;
+    if (rotary_dim < 0 || rotary_dim > cache->head_dim || rotary_dim % 16 != 0) return ABQ_ERR_SHAPE;
+    if (rotary_dim && !inv_freq) return ABQ_ERR_NULL;
+    if (q) {
+        if (int e = check_heads_q(cache, heads_q)) return e;
+        if (int e = check_stride(ldq, (int64_t)heads_q * cache->head_dim)) return e;
+    }
+    if (int e = check_stride(ldk, (int64_t)cache->heads * cache->head_dim)) return e;
+    if (int e = check_stride(ldv, (int64_t)cache->heads * cache->head_dim)) return e;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_out) || (rotary_dim && misaligned(inv_freq))) return ABQ_ERR_ALIGN;
+    return hip_status(launch_kv_append(*cache, *batch, heads_q, rotary_dim, interleaved != 0, inv_freq, q, ldq, k, ldk, v, ldv, q_out, (hipStream_t)stream));
+}
+
+int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint16_t* k_out, uint16_t* v_out, void* stream)
+{
+    if (!slots || !k_out || !v_out) return ABQ_ERR_NULL;
+    if (int e = check_cache(cache)) return e;
+    if (count < 1) return ABQ_ERR_SHAPE;
+    if (misaligned(slots) || misaligned(k_out) || misaligned(v_out)) return ABQ_ERR_ALIGN;
+    return hip_status(launch_kv_read(*cache, count, slots, k_out, v_out, (hipStream_t)stream));
+}
+
+size_t abq_attn_paged_workspace_bytes(const abq_kv_cache* cache, const abq_batch* batch, int heads_q)
+{
+    if (check_cache(cache) || check_batch(batch) || check_heads_q(cache, heads_q)) return 0;
+    return attn_workspace_bytes(*cache, *batch, heads_q);
+}
+
+int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, const uint16_t* q, int ldq, float scale, int causal,
+                   uint16_t* y, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !y) return ABQ_ERR_NULL;
+    if (int e = check_cache(cache)) return e;
+    if (int e = check_batch(batch)) return e;
+    if (int e = check_heads_q(cache, heads_q)) return e;
+    if (int e = check_stride(ldq, (int64_t)heads_q * cache->head_dim)) return e;
+    if (misaligned(q) || misaligned(y) || misaligned(workspace)) return ABQ_ERR_ALIGN;
+    const size_t need = attn_workspace_bytes(*cache, *batch, heads_q);
+    if (need && !workspace) return ABQ_ERR_NULL;
+    if (workspace_bytes < need) return ABQ_ERR_SIZE;
+    return hip_status(launch_attn_paged(*cache, *batch, heads_q, q, ldq, scale, causal != 0, y, workspace, (hipStream_t)stream));
+}
+
+static int check_lora_shape(int M, int N, int K, int rank)
+{
+    return M < 1 || N < 1 || K < 1 || K > ABQ_MAX_K || rank < 1 || rank > 256 ? ABQ_ERR_SHAPE : ABQ_OK;
+}
+
+size_t abq_lora_add_workspace_bytes(int M, int N, int K, int rank)
+{
+    return check_lora_shape(M, N, K, rank) ? 0 : lora_workspace_bytes(M, N, K, rank);
+}
+
+int abq_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x, int ldx, const int32_t* ids, const uint16_t* a,
+                 const uint16_t* b, const float* scale, const uint16_t* y, int ldy, uint16_t* out, int ldout,
+                 void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!x || !ids || !a || !b || !scale || !y || !out) return ABQ_ERR_NULL;
+    if (int e = check_lora_shape(M, N, K, rank)) return e;
+    if (adapters < 1 || ldx < K || ldy < N || ldout < N || (out == y && ldout != ldy)) return ABQ_ERR_SHAPE;
+    if (misaligned(x) || misaligned(ids) || misaligned(a) || misaligned(b) || misaligned(scale) || misaligned(y) || misaligned(out) || misaligned(workspace))
+        return ABQ_ERR_ALIGN;
+    const size_t need = lora_workspace_bytes(M, N, K, rank);
+    if (need && !workspace) return ABQ_ERR_NULL;
+    if (workspace_bytes < need) return ABQ_ERR_SIZE;
+    return hip_status(launch_lora_add(M, N, K, rank, adapters, x, ldx, ids, a, b, scale, y, ldy, out, ldout, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

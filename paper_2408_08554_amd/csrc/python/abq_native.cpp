@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Exceptions.h>
@@ -590,6 +591,250 @@ PyObject* gemm_grouped(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObj
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the attention half: paged cache, attention, adapters ----------------------------------------
+// The operands of one call: device tensors of one device, which is the device that the call runs on.
+struct Operands {
+    c10::optional<at::Device> on;
+
+    bool refuse(const at::Tensor& t, const char* what, const char* want)
+    {
+        PyErr_SetString(PyExc_AssertionError, (std::string(what) + ": expected a device tensor (" + want + "), got " + c10::toString(t.scalar_type()) + " on " + t.device().str() +
+                                               (t.is_contiguous() ? "" : " (not contiguous)")).c_str());
+        return false;
+    }
+    bool same_device(const at::Tensor& t, const char* what)
+    {
+        if (!on) on = t.device();
+        if (*on == t.device()) return true;
+        PyErr_Format(PyExc_ValueError, "%s is on another device than the operands before it", what);
+        return false;
+    }
+    // a contiguous tensor of this type and shape
+    bool whole(PyObject* o, const char* what, at::ScalarType type, at::IntArrayRef shape, void** out)
+    {
+        const at::Tensor* t = tensor(o);
+        if (!t) return false;
+        if (!t->is_cuda() || !t->is_contiguous() || t->scalar_type() != type) return refuse(*t, what, "contiguous, " + std::string(c10::toString(type)));
+        if (t->sizes() != shape) {
+            PyErr_Format(PyExc_ValueError, "%s has another shape than the other operands ask for", what);
+            return false;
+        }
+        *out = t->data_ptr();
+        return same_device(*t, what);
+    }
+    bool refuse(const at::Tensor& t, const char* what, const std::string& want) { return refuse(t, what, want.c_str()); }
+    // rows of halves, each of them contiguous
+    bool rows(PyObject* o, const char* what, int* R, int* C, int* ld, void** out)
+    {
+        const at::Tensor* t = tensor(o);
+        if (!t || !rows_cols(t, R, C)) return false;
+        if (!t->is_cuda() || t->scalar_type() != at::kHalf || (*C > 1 && t->stride(1) != 1)) return refuse(*t, what, "Half, contiguous rows");
+        *out = t->data_ptr();
+        return fits_int(*R > 1 ? t->stride(0) : *C, ld) && same_device(*t, what);
+    }
+    bool rows_of(PyObject* o, const char* what, int R, int C, int* ld, void** out)
+    {
+        int r, c;
+        if (!rows(o, what, &r, &c, ld, out)) return false;
+        if (r == R && c == C) return true;
+        PyErr_Format(PyExc_ValueError, "%s has another shape than the other operands ask for", what);
+        return false;
+    }
+    bool sequence(PyObject* o, const char* what, Py_ssize_t a, Py_ssize_t b, Py_ssize_t* n)
+    {
+        if (PyTuple_Check(o) && ((*n = PyTuple_GET_SIZE(o)) == a || *n == b)) return true;
+        PyErr_Format(PyExc_TypeError, "%s: expected a tuple of %zd%s tensors", what, a, a == b ? "" : " or 6");
+        return false;
+    }
+    // (k, v) of binary16 or (k, v, k_scale, k_zero, v_scale, v_zero)
+    bool cache(PyObject* o, abq_kv_cache* c)
+    {
+        Py_ssize_t n;
+        if (!sequence(o, "cache", 2, 6, &n)) return false;
+        const at::Tensor* k = tensor(PyTuple_GET_ITEM(o, 0));
+        if (!k) return false;
+        if (k->dim() != 4) {
+            PyErr_SetString(PyExc_ValueError, "cache: keys and values are [num_pages, heads, page_size, head_dim]");
+            return false;
+        }
+        *c = abq_kv_cache{};
+        c->kv_bits = n == 2 ? 16 : 8;
+        if (!fits_int(k->size(0), &c->num_pages) || !fits_int(k->size(1), &c->heads) || !fits_int(k->size(2), &c->page_size) || !fits_int(k->size(3), &c->head_dim)) return false;
+        const at::ScalarType type = n == 2 ? at::kHalf : at::kByte;
+        if (!whole(PyTuple_GET_ITEM(o, 0), "keys", type, k->sizes(), &c->k) || !whole(PyTuple_GET_ITEM(o, 1), "values", type, k->sizes(), &c->v)) return false;
+        if (n == 2) return true;
+        const at::IntArrayRef per_vector = k->sizes().slice(0, 3);
+        return whole(PyTuple_GET_ITEM(o, 2), "k_scale", at::kFloat, per_vector, (void**)&c->k_scale) && whole(PyTuple_GET_ITEM(o, 3), "k_zero", at::kByte, per_vector, (void**)&c->k_zero) &&
+               whole(PyTuple_GET_ITEM(o, 4), "v_scale", at::kFloat, per_vector, (void**)&c->v_scale) && whole(PyTuple_GET_ITEM(o, 5), "v_zero", at::kByte, per_vector, (void**)&c->v_zero);
+    }
+    // (row_start, lens, pages); max_new, max_len: 0 for the widest bounds
+    bool batch(PyObject* o, const abq_kv_cache& c, int rows, int max_new, int max_len, abq_batch* b)
+    {
+        Py_ssize_t n;
+        if (!sequence(o, "batch", 3, 3, &n)) return false;
+        const at::Tensor* pages = tensor(PyTuple_GET_ITEM(o, 2));
+        if (!pages) return false;
+        *b = abq_batch{};
+        b->rows = rows;
+        if (!rows_cols(pages, &b->seqs, &b->max_pages)) return false;
+        b->max_new = max_new ? max_new : rows;
+        b->max_len = max_len ? max_len : (int)std::min<int64_t>((int64_t)b->max_pages * c.page_size, INT32_MAX);
+        return whole(PyTuple_GET_ITEM(o, 0), "row_start", at::kInt, {(int64_t)b->seqs + 1}, (void**)&b->row_start) && whole(PyTuple_GET_ITEM(o, 1), "lens", at::kInt, {b->seqs}, (void**)&b->lens) &&
+               whole(PyTuple_GET_ITEM(o, 2), "pages", at::kInt, pages->sizes(), (void**)&b->pages);
+    }
+    // an output that the caller may have given (then contiguous, of this shape), and a workspace
+    bool output(PyObject* given, const char* what, int R, int C, Buffer* out)
+    {
+        out->wanted = is_none(given);
+        return out->wanted || whole(given, what, at::kHalf, {R, C}, &out->ptr);
+    }
+    bool workspace(PyObject* given, size_t need, Workspace* ws)
+    {
+        if (is_none(given)) return ws->arg(nullptr, need);
+        const at::Tensor* t = tensor(given);
+        ws->bytes = t ? (size_t)t->numel() : 0;
+        return t && whole(given, "workspace", at::kByte, t->sizes(), &ws->ptr);
+    }
+};
+
+// The library call on the operands' device and that device's current stream.
+template <class F>
+bool call_on(const char* where, at::Device device, F&& f)
+{
+    return call(where, [&] {
+        const c10::DeviceGuard guard(device);
+        return f();
+    });
+}
+bool truth(PyObject* o, int otherwise, int* out)
+{
+    *out = o ? PyObject_IsTrue(o) : otherwise;
+    return *out >= 0;
+}
+
+Signature<8> sig_kv_append{"abq_kv_append", 4, {"cache", "batch", "k", "v", "q", "inv_freq", "interleaved", "q_out"}};
+PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[8];
+    Operands t;
+    abq_kv_cache c;
+    abq_batch b;
+    int rows, width, ldk, ldv, ldq = 0, q_width = 0, rotary_dim = 0, interleaved;
+    void *kp, *vp, *qp = nullptr, *fp = nullptr;
+    if (!sig_kv_append.parse(args, nargs, kw, a) || !truth(a[6], 0, &interleaved) || !t.cache(a[0], &c) || !t.rows(a[2], "k", &rows, &width, &ldk, &kp)) return nullptr;
+    if ((int64_t)c.heads * c.head_dim != width) return PyErr_SetString(PyExc_ValueError, "k: rows of the cache's heads * head_dim elements"), nullptr;
+    if (!t.rows_of(a[3], "v", rows, width, &ldv, &vp) || !t.batch(a[1], c, rows, 0, 0, &b)) return nullptr;
+    Buffer q_out;
+    if (!is_none(a[4])) {
+        int r;
+        if (!t.rows(a[4], "q", &r, &q_width, &ldq, &qp)) return nullptr;
+        if (r != rows || c.head_dim < 1 || q_width % c.head_dim != 0) return PyErr_SetString(PyExc_ValueError, "q: as many rows as k, of whole heads"), nullptr;
+        if (!t.output(a[7], "q_out", rows, q_width, &q_out)) return nullptr;
+    } else if (!is_none(a[7])) {
+        return PyErr_SetString(PyExc_ValueError, "q_out without q"), nullptr;
+    }
+    if (!is_none(a[5])) {
+        const at::Tensor* f = tensor(a[5]);
+        if (!f || !t.whole(a[5], "inv_freq", at::kFloat, f->sizes(), &fp) || !fits_int(2 * f->numel(), &rotary_dim)) return nullptr;
+    }
+    if (!call_on("abq_kv_append", *t.on, [&] {
+            uint16_t* qo = qp ? q_out.half(rows, q_width, *t.on) : nullptr;
+            return abq_kv_append(&c, &b, qp ? q_width / c.head_dim : 0, rotary_dim, interleaved, (const float*)fp, (const uint16_t*)qp, ldq, (const uint16_t*)kp, ldk, (const uint16_t*)vp, ldv,
+                                 qo, stream());
+        }))
+        return nullptr;
+    return result(a[7], q_out);
+    END_HANDLE_TH_ERRORS
+}
+
+Signature<2> sig_kv_read{"abq_kv_read", 2, {"cache", "slots"}};
+PyObject* kv_read(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[2];
+    Operands t;
+    abq_kv_cache c;
+    int count;
+    void* sp;
+    if (!sig_kv_read.parse(args, nargs, kw, a) || !t.cache(a[0], &c)) return nullptr;
+    const at::Tensor* slots = tensor(a[1]);
+    if (!slots) return nullptr;
+    if (slots->dim() != 1) return PyErr_SetString(PyExc_ValueError, "slots: a tensor of one dimension"), nullptr;
+    if (!fits_int(slots->size(0), &count) || !t.whole(a[1], "slots", at::kInt, slots->sizes(), &sp)) return nullptr;
+    Buffer k, v;
+    k.wanted = v.wanted = true;
+    if (!call_on("abq_kv_read", *t.on, [&] {
+            const int width = c.heads * c.head_dim;
+            uint16_t *kp = k.half(count, width, *t.on), *vp = v.half(count, width, *t.on);
+            return abq_kv_read(&c, count, (const int32_t*)sp, kp, vp, stream());
+        }))
+        return nullptr;
+    return pack({result(k), result(v)});
+    END_HANDLE_TH_ERRORS
+}
+
+Signature<9> sig_attn{"abq_attn_paged", 4, {"cache", "batch", "q", "scale", "causal", "max_new", "max_len", "y", "workspace"}};
+PyObject* attn_paged(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[9];
+    Operands t;
+    abq_kv_cache c;
+    abq_batch b;
+    int rows, width, ldq, causal, max_new = 0, max_len = 0;
+    void* qp;
+    if (!sig_attn.parse(args, nargs, kw, a) || !truth(a[4], 1, &causal) || (a[5] && !to_int(a[5], &max_new)) || (a[6] && !to_int(a[6], &max_len))) return nullptr;
+    const double scale = PyFloat_AsDouble(a[3]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    if (!t.cache(a[0], &c) || !t.rows(a[2], "q", &rows, &width, &ldq, &qp) || !t.batch(a[1], c, rows, max_new, max_len, &b)) return nullptr;
+    if (c.head_dim < 1 || width % c.head_dim != 0) return PyErr_SetString(PyExc_ValueError, "q: rows of whole heads"), nullptr;
+    Buffer y;
+    Workspace ws;
+    const int heads_q = width / c.head_dim;
+    if (!t.output(a[7], "y", rows, width, &y) || !t.workspace(a[8], abq_attn_paged_workspace_bytes(&c, &b, heads_q), &ws)) return nullptr;
+    if (!call_on("abq_attn_paged", *t.on, [&] {
+            uint16_t* yp = y.half(rows, width, *t.on);
+            void* wsp = ws.make(*t.on);
+            return abq_attn_paged(&c, &b, heads_q, (const uint16_t*)qp, ldq, (float)scale, causal, yp, wsp, ws.bytes, stream());
+        }))
+        return nullptr;
+    return result(a[7], y);
+    END_HANDLE_TH_ERRORS
+}
+
+Signature<8> sig_lora{"abq_lora_add", 6, {"x", "ids", "a", "b", "scale", "y", "out", "workspace"}};
+PyObject* lora_add(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[8];
+    Operands t;
+    int M, K, N, ldx, ldy, ldout, rank, adapters, rows;
+    void *xp, *ip, *ap, *bp, *sp, *yp;
+    if (!sig_lora.parse(args, nargs, kw, a) || !t.rows(a[0], "x", &M, &K, &ldx, &xp) || !t.rows(a[5], "y", &rows, &N, &ldy, &yp)) return nullptr;
+    if (rows != M) return PyErr_SetString(PyExc_ValueError, "y: as many rows as x"), nullptr;
+    const at::Tensor* A = tensor(a[2]);
+    if (!A) return nullptr;
+    if (A->dim() != 3) return PyErr_SetString(PyExc_ValueError, "a: a tensor of three dimensions"), nullptr;
+    if (!fits_int(A->size(0), &adapters) || !fits_int(A->size(1), &rank) || !t.whole(a[1], "ids", at::kInt, {M}, &ip) || !t.whole(a[2], "a", at::kHalf, {adapters, rank, K}, &ap) ||
+        !t.whole(a[3], "b", at::kHalf, {adapters, N, rank}, &bp) || !t.whole(a[4], "scale", at::kFloat, {adapters}, &sp))
+        return nullptr;
+    Buffer out;
+    Workspace ws;
+    out.wanted = is_none(a[6]);
+    ldout = N;
+    if ((!out.wanted && !t.rows_of(a[6], "out", M, N, &ldout, &out.ptr)) || !t.workspace(a[7], abq_lora_add_workspace_bytes(M, N, K, rank), &ws)) return nullptr;
+    if (!call_on("abq_lora_add", *t.on, [&] {
+            uint16_t* op = out.half(M, N, *t.on);
+            void* wsp = ws.make(*t.on);
+            return abq_lora_add(M, N, K, rank, adapters, (const uint16_t*)xp, ldx, (const int32_t*)ip, (const uint16_t*)ap, (const uint16_t*)bp, (const float*)sp, (const uint16_t*)yp, ldy, op,
+                                ldout, wsp, ws.bytes, stream());
+        }))
+        return nullptr;
+    return result(a[6], out);
+    END_HANDLE_TH_ERRORS
+}
+
 // binding.py hands over its exception class, make_problems and ctypes.Array once
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -630,6 +875,19 @@ PyMethodDef methods[] = {
                "abq_f4_gemm(p, q, M, N, K, packed_act, packed_w, y=None, acc=None, want_acc=False)\n--\n\n-> (y float16 [M,N], acc int32 [M,N] or None)."),
     ABQ_METHOD("abq_gemm_grouped", gemm_grouped,
                "abq_gemm_grouped(p, q, M, problems, a_layout, w_layout, workspace=None)\n--\n\nOne call for a list of independent problems that share p, q, M (see make_problems); outputs are written to\nthe y / acc tensors of each problem."),
+    ABQ_METHOD("abq_kv_append", kv_append,
+               "abq_kv_append(cache, batch, k, v, q=None, inv_freq=None, interleaved=False, q_out=None)\n--\n\nk, v float16 [rows, heads * head_dim] into the paged cache, k (and q) rotated to the rows' positions\n"
+               "by inv_freq float32 [rotary_dim / 2] -> the rotated q float16 [rows, heads_q * head_dim], or None.\n"
+               "cache: (k, v) float16 [num_pages, heads, page_size, head_dim], or uint8 ones with k_scale float32, k_zero uint8,\nv_scale, v_zero [num_pages, heads, page_size] behind them.\n"
+               "batch: (row_start int32 [seqs + 1], lens int32 [seqs], pages int32 [seqs, max_pages]).  Rows may be columns of a wider tensor."),
+    ABQ_METHOD("abq_kv_read", kv_read,
+               "abq_kv_read(cache, slots)\n--\n\nslots int32 [count], page * page_size + offset -> (k, v float16 [count, heads * head_dim]) as the cache holds them."),
+    ABQ_METHOD("abq_attn_paged", attn_paged,
+               "abq_attn_paged(cache, batch, q, scale, causal=True, max_new=0, max_len=0, y=None, workspace=None)\n--\n\n-> y float16 [rows, heads_q * head_dim]: attention of the rows over what the cache holds of their sequences.\n"
+               "max_new, max_len: bounds of any sequence's rows and tokens (0: the widest)."),
+    ABQ_METHOD("abq_lora_add", lora_add,
+               "abq_lora_add(x, ids, a, b, scale, y, out=None, workspace=None)\n--\n\nx float16 [M,K], ids int32 [M], a float16 [adapters, rank, K], b float16 [adapters, N, rank], scale float32 [adapters],\n"
+               "y float16 [M,N] -> out = y + scale[id] * B[id] (A[id] x) float16 [M,N] (rows with an id outside 0..adapters-1: y)."),
     {"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, "init(error, make_problems, array)"},
     {nullptr, nullptr, 0, nullptr}};
 
@@ -640,7 +898,8 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "abq_native", "The online entry
 PyMODINIT_FUNC PyInit_abq_native()
 {
     if (!(sig_quant_pack.intern() && sig_pack_codes.intern() && sig_f4_pack.intern() && sig_rmsnorm.intern() && sig_add_rmsnorm.intern() && sig_silu.intern() &&
-          sig_gemm.intern() && sig_act_codes.intern() && sig_requant.intern() && sig_static.intern() && sig_f4_gemm.intern() && sig_grouped.intern()))
+          sig_gemm.intern() && sig_act_codes.intern() && sig_requant.intern() && sig_static.intern() && sig_f4_gemm.intern() && sig_grouped.intern() && sig_kv_append.intern() && sig_kv_read.intern() &&
+          sig_attn.intern() && sig_lora.intern()))
         return nullptr;
     return PyModule_Create(&module_def);
 }
