@@ -364,8 +364,9 @@ int abq_gemm_grouped(int p, int q, int M, int count, const abq_problem* host_pro
 /* Keys and values of one layer, in pages handed out to sequences by the caller.  Vector (page, head, offset) lies at
  * ((page * heads + head) * page_size + offset) * head_dim elements.
  *   kv_bits    16: binary16 values.  8: codes 0..255 (one byte each) with a scale and a zero-point per vector, the
- *              quantizer of abq_quant_pack_act with q = 8 on the binary16 vector; value = scale * (code - zero).
- *   page_size  tokens per page: a power of two, 16..4096;  head_dim a multiple of 16, 16..256;  num_pages, heads >= 1
+ *              quantizer of abq_quant_pack_act with q = 8 on the binary16 vector; value = scale * (code - zero), scale > 0.
+ *   page_size  tokens per page: a power of two, 16..4096;  head_dim a multiple of 16, 16..256;  num_pages, heads >= 1,
+ *              heads * head_dim < 2^20
  *   k, v       [num_pages][heads][page_size][head_dim] binary16 or uint8
  *   k_scale, v_scale [num_pages][heads][page_size] float;  k_zero, v_zero the same of uint8 (a zero-point of 8-bit codes
  *              fits a byte, and a decoding step reads one per vector).  NULL when kv_bits is 16. */
@@ -400,7 +401,7 @@ typedef struct abq_batch {
  * (x[2j], x[2j+1]).  The angle is formed and reduced in binary64 (positions are exact however far), sine and cosine are
  * within 2^-23, products and sum in binary32, one rounding to binary16.  A cache of codes quantizes the rotated binary16
  * vector.
- *   heads_q    query heads (with q), a multiple of cache->heads;  rotary_dim a multiple of 16, 0..head_dim
+ *   heads_q    query heads (with q), a multiple of cache->heads, rows * heads_q <= 2^30;  rotary_dim a multiple of 16, 0..head_dim
  *   q [rows][heads_q * head_dim] (NULL to skip), k, v [rows][heads * head_dim] with row strides ldq, ldk, ldv in elements
  *   inv_freq   [rotary_dim / 2] float
  *   q_out      [rows][heads_q * head_dim], contiguous; it may be q itself where that is contiguous too

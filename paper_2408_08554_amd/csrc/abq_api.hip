@@ -871,7 +871,7 @@ static int check_cache(const abq_kv_cache* c)
     if (c->kv_bits != 16 && c->kv_bits != 8) return ABQ_ERR_BITS;
     if (c->kv_bits == 8 && (!c->k_scale || !c->k_zero || !c->v_scale || !c->v_zero)) return ABQ_ERR_NULL;
     if (c->num_pages < 1 || c->heads < 1 || c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0 ||
-        c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 != 0 || (int64_t)c->heads * c->head_dim > (1 << 20))
+        c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 != 0 || (int64_t)c->heads * c->head_dim >= (1 << 20))
         return ABQ_ERR_SHAPE;
     if (misaligned(c->k) || misaligned(c->v) || (c->kv_bits == 8 && (misaligned(c->k_scale) || misaligned(c->k_zero) || misaligned(c->v_scale) || misaligned(c->v_zero))))
         return ABQ_ERR_ALIGN;
@@ -886,10 +886,10 @@ static int check_batch(const abq_batch* b)
     return ABQ_OK;
 }
 
-// Query heads: a multiple of the cache's, and rows that stay below 2^20 elements.
-static int check_heads_q(const abq_kv_cache* c, int heads_q)
+// Query heads: a multiple of the cache's, rows that stay below 2^20 elements, and at most 2^30 of all rows.
+static int check_heads_q(const abq_kv_cache* c, const abq_batch* b, int heads_q)
 {
-    return heads_q < 1 || heads_q % c->heads != 0 || (int64_t)heads_q * c->head_dim > (1 << 20) ? ABQ_ERR_SHAPE : ABQ_OK;
+    return heads_q < 1 || heads_q % c->heads != 0 || (int64_t)heads_q * c->head_dim >= (1 << 20) || (int64_t)b->rows * heads_q > (1 << 30) ? ABQ_ERR_SHAPE : ABQ_OK;
 }
 
 int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, int rotary_dim, int interleaved, const float* inv_freq,
@@ -901,7 +901,7 @@ int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q
     if (rotary_dim < 0 || rotary_dim > cache->head_dim || rotary_dim % 16 != 0) return ABQ_ERR_SHAPE;
     if (rotary_dim && !inv_freq) return ABQ_ERR_NULL;
     if (q) {
-        if (int e = check_heads_q(cache, heads_q)) return e;
+        if (int e = check_heads_q(cache, batch, heads_q)) return e;
         if (int e = check_stride(ldq, (int64_t)heads_q * cache->head_dim)) return e;
     }
     if (int e = check_stride(ldk, (int64_t)cache->heads * cache->head_dim)) return e;
@@ -921,7 +921,7 @@ int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint
 
 size_t abq_attn_paged_workspace_bytes(const abq_kv_cache* cache, const abq_batch* batch, int heads_q)
 {
-    if (check_cache(cache) || check_batch(batch) || check_heads_q(cache, heads_q)) return 0;
+    if (check_cache(cache) || check_batch(batch) || check_heads_q(cache, batch, heads_q)) return 0;
     return attn_workspace_bytes(*cache, *batch, heads_q);
 }
 
@@ -931,7 +931,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
     if (!q || !y) return ABQ_ERR_NULL;
     if (int e = check_cache(cache)) return e;
     if (int e = check_batch(batch)) return e;
-    if (int e = check_heads_q(cache, heads_q)) return e;
+    if (int e = check_heads_q(cache, batch, heads_q)) return e;
     if (int e = check_stride(ldq, (int64_t)heads_q * cache->head_dim)) return e;
     if (misaligned(q) || misaligned(y) || misaligned(workspace)) return ABQ_ERR_ALIGN;
     const size_t need = attn_workspace_bytes(*cache, *batch, heads_q);

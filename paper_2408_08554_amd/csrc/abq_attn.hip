@@ -1,73 +1,119 @@
-// Attention of a step's rows over the paged cache: one wave per row and query head, 64 tokens at a time, running maximum and
-// sum in binary32.
-#include "abq_kv.h"
+// Attention of a step's rows over the paged cache: which kernel takes a sequence, how its tokens are shared out, and the joining
+// of the parts.
+#include "abq_attn_kernels.h"
+
+#include <algorithm>
 
 namespace abq {
 
-__device__ __forceinline__ float cache_value(const abq_kv_cache& c, bool is_v, int64_t vec, int d)
-{
-    if (c.kv_bits == 16) return __half2float(__ushort_as_half(((const uint16_t*)(is_v ? c.v : c.k))[vec * c.head_dim + d]));
-    const int code = ((const uint8_t*)(is_v ? c.v : c.k))[vec * c.head_dim + d], zero = (is_v ? c.v_zero : c.k_zero)[vec];
-    return (is_v ? c.v_scale : c.k_scale)[vec] * (float)(code - zero);
-}
+template <>
+void launch_attn_few<64>(const AttnArgs&, int, const dim3&, hipStream_t);
+template <>
+void launch_attn_few<128>(const AttnArgs&, int, const dim3&, hipStream_t);
+template <>
+void launch_attn_few<256>(const AttnArgs&, int, const dim3&, hipStream_t);
+template <>
+void launch_attn_many<64>(const AttnArgs&, const dim3&, hipStream_t);
+template <>
+void launch_attn_many<128>(const AttnArgs&, const dim3&, hipStream_t);
+template <>
+void launch_attn_many<256>(const AttnArgs&, const dim3&, hipStream_t);
 
-__global__ __launch_bounds__(64) void attn_rows_kernel(abq_kv_cache c, abq_batch b, int heads_q, const uint16_t* q, int ldq, float scale, bool causal,
-                                                       uint16_t* y, int page_shift)
+// One wave per row and head of a sequence that was shared out: its parts as one.
+__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a)
 {
-    __shared__ float sq[256], sp[64];
-    __shared__ int64_t sv[64];
-    const int row = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x, D = c.head_dim, head = hq / (heads_q / c.heads);
+    const int row = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x, D = a.c.head_dim;
     int seq = 0;
-    while (seq < b.seqs && b.row_start[seq + 1] <= row) ++seq;
-    if (seq >= b.seqs || row - b.row_start[seq] >= b.max_new) return;
-    const int len = min(max(b.lens[seq], 0), b.max_len);
-    const int64_t pos = (int64_t)b.lens[seq] - ((int64_t)b.row_start[seq + 1] - row);
-    const int seen = causal ? (int)min((int64_t)len, max(pos + 1, (int64_t)0)) : len;
-    for (int d = lane; d < D; d += 64) sq[d] = __half2float(__ushort_as_half(q[(size_t)row * ldq + (size_t)hq * D + d]));
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o[4] = {0, 0, 0, 0};
-    for (int t0 = 0; t0 < seen; t0 += 64) {
-        const int t = t0 + lane, page = t < seen ? page_of(b, c, page_shift, seq, t) : -1;
-        const int64_t vec = page < 0 ? -1 : vector_of(c, page, head, t & (c.page_size - 1));
-        float s = -INFINITY;
-        if (vec >= 0) {
-            s = 0.0f;
-            for (int d = 0; d < D; ++d) s = fmaf(sq[d], cache_value(c, false, vec, d), s);
-            s *= scale;
-        }
-        float top = s;
-        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        const float next = fmaxf(m, top), base = next == -INFINITY ? 0.0f : next;
-        const float fade = expf(m - base), p = vec >= 0 ? expf(s - base) : 0.0f;
-        sp[lane] = p;
-        sv[lane] = vec;
-        float sum = p;
-        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        l = l * fade + sum;
-        m = next;
-        __syncthreads();
-        for (int i = 0; i < 4; ++i) {
-            const int d = lane + 64 * i;
-            if (d >= D) break;
-            float acc = o[i] * fade;
-            for (int j = 0; j < 64; ++j)
-                if (sv[j] >= 0) acc = fmaf(sp[j], cache_value(c, true, sv[j], d), acc);
-            o[i] = acc;
-        }
-        __syncthreads();
+    for (int s0 = 0; s0 < a.b.seqs; s0 += 64) {
+        const int s = s0 + lane;
+        seq += __popcll(__ballot(s < a.b.seqs && a.b.row_start[s + 1] <= row));
     }
-    for (int i = 0; i < 4; ++i) {
-        const int d = lane + 64 * i;
-        if (d < D) y[((size_t)row * heads_q + hq) * D + d] = __half_as_ushort(__float2half_rn(l == 0.0f ? 0.0f : o[i] / l));
+    if (seq >= a.b.seqs) return;
+    const Sequence sq(a, seq);
+    const int i = row - sq.first;
+    if (i < 0 || i >= sq.tokens) return;
+    const int nrows = sq.tokens * a.group;
+    const bool few = nrows <= a.few;
+    const int last = few ? nrows : min(nrows, ((i * a.group + hq % a.group) / kManyRows + 1) * kManyRows);
+    const int top = sq.seen((last - 1) / a.group, a.causal);
+    const int per = few ? part_tokens(top, a.few_parts, kFewTokens, kFewLeast) : part_tokens(top, a.many_parts, kManyTokens, kManyLeast);
+    const int nparts = (top + per - 1) / per;
+    if (nparts <= 1) return;   // (written by its workgroup)
+    const int64_t yrow = (int64_t)row * a.heads_q + hq;
+    const float2* ml = a.part_ml + yrow * a.parts;
+    const float* o = a.part_o + yrow * a.parts * D;
+    float m = kFloor, l = 0.0f;
+    for (int p = 0; p < nparts; ++p) m = fmaxf(m, ml[p].x);
+    f4 v = {0, 0, 0, 0};
+    for (int p = 0; p < nparts; ++p) {
+        const float f = __builtin_amdgcn_exp2f(ml[p].x - m);
+        l = fmaf(f, ml[p].y, l);
+        if (4 * lane < D) v += f * *reinterpret_cast<const f4*>(o + (int64_t)p * D + 4 * lane);
     }
+    if (4 * lane >= D) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (l == 0.0f) v = f4{0, 0, 0, 0};
+    *reinterpret_cast<uint2*>(a.y + yrow * D + 4 * lane) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
 }
 
-size_t attn_workspace_bytes(const abq_kv_cache&, const abq_batch&, int) { return 0; }
+// Which kernels a step needs, and into how many parts sequences are cut at most; from the sizes that the host knows alone, so that a
+// captured launch serves whatever lengths the arrays hold later.
+struct AttnPlan {
+    int nr, few, few_parts, many_parts, parts;
+    int64_t many_tiles;
+};
+static AttnPlan attn_plan(const abq_kv_cache& c, const abq_batch& b, int heads_q)
+{
+    AttnPlan p{};
+    const int group = heads_q / c.heads;
+    const int64_t most = (int64_t)b.max_new * group, all = (int64_t)b.rows * group;
+    p.nr = most <= 16 || (group <= 16 && most > 32) ? 1 : 2;
+    p.few = group <= 32 && (b.seqs > 1 || most <= 32) ? 16 * p.nr : 0;
+    const int tokens = (int)std::min<int64_t>(b.max_len, (int64_t)b.max_pages * c.page_size);
+    p.few_parts = p.many_parts = 1;
+    if (p.few) {
+        const int64_t wgs = (int64_t)b.seqs * c.heads;
+        p.few_parts = (int)std::min<int64_t>({(1024 + wgs - 1) / wgs, (tokens + kFewLeast - 1) / kFewLeast, 64});
+    }
+    if (most > p.few) {
+        p.many_tiles = all / kManyRows + std::min<int64_t>(b.seqs, all / (p.few + 1));
+        const int64_t wgs = p.many_tiles * c.heads;
+        p.many_parts = (int)std::min<int64_t>({(512 + wgs - 1) / wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
+    }
+    p.parts = std::max(p.few_parts, p.many_parts);
+    return p;
+}
+
+size_t attn_workspace_bytes(const abq_kv_cache& c, const abq_batch& b, int heads_q)
+{
+    const AttnPlan p = attn_plan(c, b, heads_q);
+    return p.parts == 1 ? 0 : (size_t)b.rows * heads_q * p.parts * (c.head_dim * sizeof(float) + sizeof(float2));
+}
 
 hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int heads_q, const uint16_t* q, int ldq, float scale, bool causal,
-                             uint16_t* y, void*, hipStream_t s)
+                             uint16_t* y, void* workspace, hipStream_t s)
 {
-    attn_rows_kernel<<<dim3(b.rows, heads_q), 64, 0, s>>>(c, b, heads_q, q, ldq, scale, causal, y, __builtin_ctz(c.page_size));
+    const AttnPlan p = attn_plan(c, b, heads_q);
+    AttnArgs a{c, b, heads_q, heads_q / c.heads, __builtin_ctz(c.page_size), q, ldq, (float)((double)scale * 1.44269504088896340736), causal, y, nullptr, nullptr,
+               p.parts, p.few, p.few_parts, p.many_parts};
+    if (p.parts > 1) {
+        a.part_o = (float*)workspace;
+        a.part_ml = (float2*)(a.part_o + (size_t)b.rows * heads_q * p.parts * c.head_dim);
+    }
+    if (p.many_tiles * c.heads > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (p.many_tiles) {
+        const dim3 grid((unsigned)(p.many_tiles * c.heads), p.many_parts);
+        if (c.head_dim <= 64) launch_attn_many<64>(a, grid, s);
+        else if (c.head_dim <= 128) launch_attn_many<128>(a, grid, s);
+        else launch_attn_many<256>(a, grid, s);
+    }
+    if (p.few) {
+        const dim3 grid(c.heads, b.seqs, p.few_parts);
+        if (c.head_dim <= 64) launch_attn_few<64>(a, p.nr, grid, s);
+        else if (c.head_dim <= 128) launch_attn_few<128>(a, p.nr, grid, s);
+        else launch_attn_few<256>(a, p.nr, grid, s);
+    }
+    if (p.parts > 1) attn_join_kernel<<<dim3(b.rows, heads_q), 64, 0, s>>>(a);
     return hipGetLastError();
 }
 

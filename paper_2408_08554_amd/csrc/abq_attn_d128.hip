@@ -1,0 +1,4 @@
+// Attention over the paged cache, heads of 65 to 128.
+#include "abq_attn_kernels.h"
+
+ABQ_ATTN_INSTANTIATE(128)
