@@ -78,7 +78,7 @@ static AttnPlan attn_plan(const abq_kv_cache& c, const abq_batch& b, int heads_q
     if (most > p.few) {
         p.many_tiles = all / kManyRows + std::min<int64_t>(b.seqs, all / (p.few + 1));
         const int64_t wgs = p.many_tiles * c.heads;
-        p.many_parts = (int)std::min<int64_t>({(512 + wgs - 1) / wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
+        p.many_parts = (int)std::min<int64_t>({(256 + wgs - 1) / wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
     }
     p.parts = std::max(p.few_parts, p.many_parts);
     return p;

@@ -13,6 +13,8 @@
 #pragma once
 #include "abq_kv.h"
 
+#include <type_traits>
+
 namespace abq {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
@@ -47,6 +49,7 @@ struct AttnArgs {
 // A sequence's rows and tokens within all bounds.
 struct Sequence {
     int first, tokens, before, length;   // first row; new tokens that are handled; position of the first; tokens held
+    __device__ __forceinline__ Sequence() : first(0), tokens(0), before(0), length(0) {}
     __device__ __forceinline__ Sequence(const AttnArgs& a, int seq)
     {
         const int r0 = a.b.row_start[seq], r1 = a.b.row_start[seq + 1], len = a.b.lens[seq];
@@ -132,7 +135,7 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
 {
     __syncthreads();
     const int D = a.c.head_dim;
-    for (int i = threadIdx.x; i < (R1 - R0) * D; i += 256) {
+    for (int i = threadIdx.x; i < (R1 - R0) * D; i += blockDim.x) {
         const int R = R0 + i / D, d = i % D, end = min(last + 1, sq.seen(R / a.group, a.causal));
         float x = 0.0f;
         for (int t = first; t < end; ++t) {
@@ -406,15 +409,13 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
 // ---- many rows -----------------------------------------------------------------------------------
 // The sequence and tile of a workgroup: tiles of the sequences with more than `few` rows, in order; within a sequence the last
 // tile (the longest under the causal mask) first.  false: there is none.
-__device__ __forceinline__ bool many_tile(const AttnArgs& a, int index, int* seq, int* tile)
+__device__ __forceinline__ bool many_tile(const AttnArgs& a, int index, int* seq, int* tile, Sequence* sq)
 {
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < a.b.seqs; s0 += 64) {
-        int nt = 0;
-        if (s0 + lane < a.b.seqs) {
-            const int nrows = Sequence(a, s0 + lane).tokens * a.group;
-            nt = nrows > a.few ? (nrows + kManyRows - 1) / kManyRows : 0;
-        }
+        Sequence mine;
+        if (s0 + lane < a.b.seqs) mine = Sequence(a, s0 + lane);
+        const int nrows = mine.tokens * a.group, nt = nrows > a.few ? (nrows + kManyRows - 1) / kManyRows : 0;
         int sum = nt;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -423,56 +424,101 @@ __device__ __forceinline__ bool many_tile(const AttnArgs& a, int index, int* seq
         }
         const uint64_t past = __ballot(sum > index);
         if (past) {
-            const int at = __ffsll((unsigned long long)past) - 1;
+            const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past));
             *seq = s0 + at;
-            *tile = __shfl(sum, at, 64) - 1 - index;
+            *tile = __builtin_amdgcn_readlane(sum, at) - 1 - index;
+            sq->first = __builtin_amdgcn_readlane(mine.first, at);
+            sq->tokens = __builtin_amdgcn_readlane(mine.tokens, at);
+            sq->before = __builtin_amdgcn_readlane(mine.before, at);
+            sq->length = __builtin_amdgcn_readlane(mine.length, at);
             return true;
         }
-        index -= __shfl(sum, 63, 64);
+        index -= __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }
 
-// One workgroup per key head, 128 rows (token * group + query head) and part of the tokens: four waves of 32 rows, which share 64
-// tokens of K and V at a time in LDS, two buffers, one barrier a step; the next step's loads are in flight meanwhile.
-template <int DP, bool CODES>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attn_many_kernel(AttnArgs a)
+// The waves' LDS work done and seen by the workgroup.  (Loads from memory stay in flight: a workgroup fence would wait for them.)
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// N loads of sixteen bytes a lane from base + offset[i] + 1024 i to LDS, a wave's N KB in a row from LDS address `to` on (the immediate
+// offset counts on both sides); complete when the wave's vmcnt says so.
+template <int N>
+__device__ __forceinline__ void lds_load(const uint8_t* base, const uint32_t* offset, uint32_t to)
+{
+    static_assert(N == 2 || N == 4);
+    if constexpr (N == 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+                     : : "s"(to), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+                     : : "s"(to), "v"(offset[0]), "v"(offset[1]), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const uint16_t* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint16_t*)p; }
+
+// One workgroup per key head, 128 rows (token * group + query head) and part of the tokens.  GROUPS groups of four waves, a
+// wave for 32 of the rows in each; the groups take the steps of 64 tokens in turn and are joined at the end.  A step of a group has two
+// halves with a barrier behind each: the matrix instructions (scores of this step, and the weights of the last one times
+// its values), and everything else (softmax, the next K and this V to LDS, loads).  The second group runs half a step behind the
+// first, so that of the two waves of a SIMD one has matrix and the other vector work.  Each group has one buffer for K and one
+// for V: K is read in the first half and written in the second, V written in the second and read in the next first.
+template <int DP, bool CODES, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArgs a)
 {
     constexpr int DT = DP / 32;                       // tiles of 32 columns of the result
     constexpr int QS = DP / 16;                       // steps of the first product
     constexpr int LPT = CODES ? DP / 16 : DP / 8;     // lanes that hold a token
-    constexpr int TPP = 256 / LPT;                    // tokens per load of the workgroup
-    constexpr int LV = kManyTokens / TPP;             // 16-byte loads of a thread per step, of K and of V
-    constexpr int KS = DP + 8, VS = DP + 32;          // halves of a row in LDS: 4 banks on for the reads of K, 16 for the transposing ones of V
-    constexpr int NB = DP > 128 ? 1 : 2;              // buffers
-    __shared__ __align__(16) uint16_t lk[NB][kManyTokens * KS], lv[NB][kManyTokens * VS];
-    __shared__ __align__(16) float s_ks[CODES ? NB : 1][kManyTokens], s_lg[CODES ? NB : 1][kManyTokens], s_inv[CODES ? NB : 1][kManyTokens];
+    constexpr int TPL = 64 / LPT;                     // tokens per load of a wave
+    constexpr int LV = 16 / TPL;                      // 16-byte loads of a lane per step, of K and of V: wave w loads the step's w-th sixteen tokens
+    constexpr int BYTES = CODES ? 1 : 2;
+    constexpr bool DIRECT = !CODES;                   // binary16 goes from memory to LDS directly, codes through registers
+    // Halves of a row in LDS.  Codes: 4 banks on from row to row for the reads of K, 16 for the transposing ones of V.  The direct loads
+    // write rows as they are; there the 16-byte pieces of row r change places, piece c lying in place c ^ turn(r).
+    constexpr int KS = DIRECT ? DP : DP + 8, VS = DIRECT ? DP : DP + 32;
+    constexpr int KL = kManyTokens * KS, VL = kManyTokens * VS;   // halves of a buffer
+    constexpr int GL = 2 * (KL + VL);                 // of a group
+    static_assert(GROUPS == 1 || GROUPS * GL * 2 >= kManyRows * DP * 4, "the groups are joined in the memory of K and V");
+    __shared__ __align__(16) uint16_t lds[GROUPS * GL];
+    __shared__ __align__(16) float s_par[CODES ? GROUPS : 1][2][3][CODES ? kManyTokens : 4];   // codes, of two steps: scales of K, logarithms and reciprocals of those of V
+    __shared__ float2 s_ml[GROUPS == 1 ? 1 : kManyRows];
     __shared__ OddTokens s_odd;
 
-    const int head = blockIdx.x % a.c.heads, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int head = blockIdx.x % a.c.heads, tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const int n32 = lane & 31, hh = lane >> 5, D = a.c.head_dim;
     int seq, tile;
-    if (!many_tile(a, blockIdx.x / a.c.heads, &seq, &tile)) return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    tile = __builtin_amdgcn_readfirstlane(tile);
-    const Sequence sq(a, seq);
+    Sequence sq;
+    if (!many_tile(a, blockIdx.x / a.c.heads, &seq, &tile, &sq)) return;
     const int nrows = sq.tokens * a.group, R0 = tile * kManyRows;
     const int top = sq.seen((min(nrows, R0 + kManyRows) - 1) / a.group, a.causal);
     const int per = part_tokens(top, a.many_parts, kManyTokens, kManyLeast), nparts = max(1, (top + per - 1) / per), part = blockIdx.y;
     if (part >= nparts) return;
-    const int from = part * per, to = min(top, from + per), steps = (to - from + kManyTokens - 1) / kManyTokens;
+    const int from = part * per, to = min(top, from + per), all_steps = (to - from + kManyTokens - 1) / kManyTokens;
+    const int steps = (all_steps - grp + GROUPS - 1) / GROUPS, rounds = (all_steps + GROUPS - 1) / GROUPS;   // this group's; the most of any group
 
-    // this lane's row, and what the wave's rows see at least and at most
+    // this lane's row, and what the wave's rows and the tile's see at least and at most
     const int W0 = R0 + 32 * wave, R = W0 + n32, tok = R / a.group, hq = head * a.group + R % a.group;
-    const int vis = R < nrows ? sq.seen(tok, a.causal) : 0;
+    const int vis = R < nrows ? sq.seen(tok, a.causal) : 0, tile_least = sq.seen(R0 / a.group, a.causal);
     const int wave_least = W0 < nrows ? sq.seen(W0 / a.group, a.causal) : 0, wave_top = W0 < nrows ? sq.seen((min(nrows, W0 + 32) - 1) / a.group, a.causal) : 0;
+    // A negative scale is the queries' sign; the scale itself is kept above 0, so that a masked score stays minus infinity under it.
+    const float scale2 = fmaxf(fabsf(a.scale2), 1e-37f);
     h8 qv[QS];
     {
+        const uint32_t sign = a.scale2 < 0.0f ? 0x80008000u : 0u;
         const uint16_t* row = a.q + (size_t)(sq.first + (R < nrows ? tok : 0)) * a.ldq + (size_t)hq * D;
 #pragma unroll
         for (int s = 0; s < QS; ++s) {
             u4 v = {0, 0, 0, 0};
-            if (R < nrows && 16 * s + 8 * hh < D) v = *reinterpret_cast<const u4*>(row + 16 * s + 8 * hh);
+            if (R < nrows && 16 * s + 8 * hh < D) v = *reinterpret_cast<const u4*>(row + 16 * s + 8 * hh) ^ sign;
             qv[s] = __builtin_bit_cast(h8, v);
         }
     }
@@ -481,184 +527,350 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attn_many_kernel(AttnAr
     for (int d = 0; d < DT; ++d) o[d] = f16{};
     float m = kFloor, l = 0.0f;
 
-    u4 kr[LV], vr[LV];
+    uint16_t *const lk = lds + grp * GL, *const lv = lk + 2 * KL;   // two buffers each, a step's in number step % 2
+    auto t_of = [&](int j) { return from + (j * GROUPS + grp) * kManyTokens; };   // first token of the group's step j
+
+    // Where the group's steps lie: lane 4 i + q holds the q-th sixteen tokens of step at + i, as the number of sixteens in front of them
+    // (0 where there is no page, and a bit of `gone`).  Sixteen steps to a window; the next one, fourteen steps on, is fetched ahead,
+    // so that step j's window always holds steps j + 1 and j + 2.
+    const int per_head = a.c.page_size >> 4, per_page = per_head * a.c.heads;
+    struct Window { uint32_t sixteens; uint64_t gone; };
+    auto fetch = [&](int j) {
+        const int t = t_of(j + (lane >> 2)) + 16 * (lane & 3), page = t < to ? page_of(a.b, a.c, a.page_shift, seq, t) : -1;
+        return page < 0 ? -1 : page * per_page + head * per_head + ((t & (a.c.page_size - 1)) >> 4);
+    };
+    auto window = [&](int fetched) { return Window{(uint32_t)max(fetched, 0), __ballot(fetched < 0)}; };
+    int at = 0, ahead = -1;
+    Window win{};
+    // Reads of K: eight rows, one piece of each, sixteen rows with one turn each (two rows of up to 64 columns fill the banks: one turn for
+    // both).  Transposing reads of V: of four rows four neighbouring pieces each, which have to lie in four different quarters of the banks.
+    auto turn_k = [](int r) { return !DIRECT ? 0 : DP == 64 ? (r >> 1) & 7 : r & 15; };
+    auto turn_v = [](int r) { return !DIRECT ? 0 : DP == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2 | ((r >> 2) & 3); };
+    // this lane's places from the first byte of its wave's sixteen tokens (direct loads: less what lds_load adds, on kBias)
+    constexpr uint32_t kBias = DIRECT ? 3072 : 0;
+    uint32_t place_k[LV], place_v[LV];
+#pragma unroll
+    for (int u = 0; u < LV; ++u) {
+        const int r = u * TPL + lane / LPT;
+        int dk = ((lane % LPT) ^ turn_k(r)) * (CODES ? 16 : 8), dv = ((lane % LPT) ^ turn_v(r)) * (CODES ? 16 : 8);
+        if (dk >= D) dk = 0;   // (the queries are zero there, and the columns of V are not stored)
+        if (dv >= D) dv = 0;
+        const uint32_t less = DIRECT ? kBias - 1024u * (u & 3) : 0u;
+        place_k[u] = (uint32_t)(r * D + dk) * BYTES + less;
+        place_v[u] = (uint32_t)(r * D + dv) * BYTES + less;
+    }
+    const uint32_t stride = 16u * D * BYTES;
+    uint32_t next = 0;   // the wave's sixteen tokens of the step whose K is loaded, and the byte they begin with
+    uint64_t next_byte = 0;
+    auto locate = [&](int j) {
+        next = __builtin_amdgcn_readlane(win.sixteens, 4 * (j - at) + wave);
+        next_byte = (uint64_t)next * stride - kBias;
+    };
+    const uint32_t lk_to = __builtin_amdgcn_readfirstlane(lds_address(lk + 16 * wave * KS)), lv_to = __builtin_amdgcn_readfirstlane(lds_address(lv + 16 * wave * VS));
+    auto load_zero = [&](const uint8_t* base, int u) { return (uint32_t)(base + (uint64_t)next * 16)[(uint32_t)(u * TPL + lane / LPT)]; };
+    u4 kr[CODES ? LV : 1], vr[CODES ? LV : 1];
     uint32_t kz[LV], vz[LV];
-    float t_ks = 0.0f, t_vs = 1.0f;   // codes: scales of token tid of the step (threads 0..63)
-    int pages_at = 0, table = -1;     // the pages of the next 16 steps, four to a step
-    auto fetch_pages = [&](int i) {
-        pages_at = i;
-        const int t = from + i * kManyTokens + 16 * lane;
-        table = t < to ? page_of(a.b, a.c, a.page_shift, seq, t) : -1;
+    float t_ks = 0.0f, t_vs = 1.0f;   // codes: scales of the step's token `lane` (the group's first wave)
+    auto load_k = [&](int u) {   // codes, of the step that `next` tells of
+        kr[u] = *reinterpret_cast<const u4*>((const uint8_t*)a.c.k + next_byte + place_k[u]);
+        kz[u] = load_zero(a.c.k_zero, u);
     };
-    auto page_at = [&](int i, int sixteenth) { return __builtin_amdgcn_readlane(table, 4 * (i - pages_at) + sixteenth); };
-    unsigned gone_next = 0;           // sixteens of the loaded step that have no page
-    auto load = [&](int i) {
-        if (i - pages_at >= 16) fetch_pages(i);
-        const int t0 = from + i * kManyTokens;
-        gone_next = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) gone_next |= (page_at(i, j) < 0 ? 1u : 0u) << j;
-#pragma unroll
-        for (int u = 0; u < LV; ++u) {
-            int d = (tid % LPT) * (CODES ? 16 : 8);
-            if (d >= D) d = 0;   // (the queries are zero there, and the columns of V are not stored)
-            const int sixteenth = __builtin_amdgcn_readfirstlane((u * TPP + (wave * 64) / LPT) >> 4);   // (a wave's tokens of one load lie in one)
-            const int page = page_at(i, sixteenth);
-            const int64_t at = vector_of(a.c, max(page, 0), head, (t0 + u * TPP + tid / LPT) & (a.c.page_size - 1));   // (no page: the first one's, masked)
-            kr[u] = *reinterpret_cast<const u4*>((const uint8_t*)a.c.k + (at * D + d) * (CODES ? 1 : 2));
-            vr[u] = *reinterpret_cast<const u4*>((const uint8_t*)a.c.v + (at * D + d) * (CODES ? 1 : 2));
-            if constexpr (CODES) {
-                kz[u] = a.c.k_zero[at];
-                vz[u] = a.c.v_zero[at];
-            }
-        }
-        if constexpr (CODES) {
-            if (wave == 0) {
-                int page = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int pj = page_at(i, j);
-                    if ((lane >> 4) == j) page = pj;
-                }
-                t_ks = 0.0f;
-                t_vs = 1.0f;
-                if (t0 + lane < to && page >= 0) {
-                    const int64_t at = vector_of(a.c, page, head, (t0 + lane) & (a.c.page_size - 1));
-                    t_ks = a.c.k_scale[at];
-                    t_vs = a.c.v_scale[at];
-                }
-            }
+    auto load_v = [&](int u) {
+        vr[u] = *reinterpret_cast<const u4*>((const uint8_t*)a.c.v + next_byte + place_v[u]);
+        vz[u] = load_zero(a.c.v_zero, u);
+    };
+    auto load_scales = [&](int j) {
+        if (CODES && wave == 0) {
+            const uint32_t mine = __shfl(win.sixteens, 4 * (j - at) + (lane >> 4), 64);
+            const uint64_t vec = (uint64_t)mine * 16 + (lane & 15);
+            t_ks = a.c.k_scale[vec];
+            t_vs = a.c.v_scale[vec];
         }
     };
-    const int tile_least = sq.seen(R0 / a.group, a.causal);
-    auto store = [&](int i) {   // what load(i) has brought, to its buffer
-        const int buf = NB == 2 ? i & 1 : 0;
-        const bool masked = from + (i + 1) * kManyTokens > tile_least || gone_next != 0;
+    auto gone_at = [&](int j) { return (unsigned)(win.gone >> (4 * (j - at))) & 15u; };   // sixteens of a step that have no page
+    const int row_at = 16 * wave + lane / LPT, col_at = (lane % LPT) * (CODES ? 16 : 8);
+    auto store = [&](uint16_t* dst, const u4& v, uint32_t z) {
+        const h2 bias = code_bias((int)z);
+        uint32_t x[8];
 #pragma unroll
-        for (int u = 0; u < LV; ++u) {
-            const int t = u * TPP + tid / LPT, d = (tid % LPT) * (CODES ? 16 : 8);
-            uint16_t *dk = lk[buf] + t * KS + d, *dv = lv[buf] + t * VS + d;
-            if constexpr (CODES) {
-                const h2 kb = code_bias((int)kz[u]), vb = code_bias((int)vz[u]);
-                uint32_t w[8];
+        for (int e = 0; e < 4; ++e) codes_to_halves(v[e], bias, x + 2 * e);
+        *reinterpret_cast<u4*>(dst) = u4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<u4*>(dst + 8) = u4{x[4], x[5], x[6], x[7]};
+    };
+    auto store_k = [&](int u, int j) { store(lk + (j & 1) * KL + (u * TPL + row_at) * KS + col_at, kr[u], kz[u]); };
+    auto store_v = [&](int u, int j) { store(lv + (j & 1) * VL + (u * TPL + row_at) * VS + col_at, vr[u], vz[u]); };
+    // Direct loads, in the second half, where they hold up no matrix instruction: V of the next step and K of the one behind it, into the
+    // buffers that the first half has read.
+    auto send_v = [&](int j) {
+        if constexpr (DIRECT) {
+            constexpr int N = LV < 4 ? LV : 4;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) codes_to_halves(kr[u][j], kb, w + 2 * j);
-                *reinterpret_cast<u4*>(dk) = u4{w[0], w[1], w[2], w[3]};
-                *reinterpret_cast<u4*>(dk + 8) = u4{w[4], w[5], w[6], w[7]};
+            for (int u = 0; u < LV; u += N) lds_load<N>((const uint8_t*)a.c.v + next_byte, place_v + u, lv_to + (j & 1) * VL * 2 + u * 1024);
+        }
+    };
+    auto send_k = [&](int j) {
+        if constexpr (DIRECT) {
+            constexpr int N = LV < 4 ? LV : 4;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) codes_to_halves(vr[u][j], vb, w + 2 * j);
-                *reinterpret_cast<u4*>(dv) = u4{w[0], w[1], w[2], w[3]};
-                *reinterpret_cast<u4*>(dv + 8) = u4{w[4], w[5], w[6], w[7]};
-            } else {
-                u4 v = vr[u];
-                if (masked && drop_not_finite(v)) s_odd.found(from + i * kManyTokens + t, to);
-                *reinterpret_cast<u4*>(dk) = kr[u];
-                *reinterpret_cast<u4*>(dv) = v;
+            for (int u = 0; u < LV; u += N) lds_load<N>((const uint8_t*)a.c.k + next_byte, place_k + u, lk_to + (j & 1) * KL * 2 + u * 1024);
+        }
+    };
+    auto send = [&](int j) {
+        if (DIRECT && j + 1 < steps) {
+            send_v(j + 1);
+            if (j + 2 < steps) {
+                locate(j + 2);
+                send_k(j + 2);
             }
         }
-        if constexpr (CODES) {
-            if (wave == 0) {
-                s_ks[buf][lane] = t_ks * a.scale2;
-                s_lg[buf][lane] = __builtin_amdgcn_logf(t_vs);
-                s_inv[buf][lane] = __builtin_amdgcn_rcpf(t_vs);
+    };
+    // Those of the second half before have arrived (V of this step, K of the next; all but this half's own), V of a masked step without what
+    // is not finite.  (A thread looks after what it has loaded.)
+    auto arrive = [&](int j) {
+        if constexpr (DIRECT) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (j + 2 < steps) __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * LV & 15) | (2 * LV >> 4) << 14);   // vmcnt(2 LV)
+            else __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+            asm volatile("" ::: "memory");
+            if (j < steps && (t_of(j) + kManyTokens > tile_least || gone_at(j) != 0)) {
+#pragma unroll
+                for (int u = 0; u < LV; ++u) {
+                    u4* const p = reinterpret_cast<u4*>(lv + (j & 1) * VL + (u * TPL + row_at) * VS + col_at);
+                    u4 v = *p;
+                    if (drop_not_finite(v)) {
+                        s_odd.found(t_of(j) + u * TPL + row_at, to);
+                        *p = v;
+                    }
+                }
             }
+        }
+    };
+    auto store_scales = [&](int j) {
+        if (CODES && wave == 0) {
+            s_par[grp][j & 1][0][lane] = t_ks * scale2;
+            s_par[grp][j & 1][1][lane] = __builtin_amdgcn_logf(t_vs);
+            s_par[grp][j & 1][2][lane] = __builtin_amdgcn_rcpf(t_vs);
         }
     };
 
-    if (tid == 0) s_odd.clear();
-    if (steps) {
-        fetch_pages(0);
-        load(0);
-    }
-    __syncthreads();
-    unsigned gone = gone_next;
-    if (steps) store(0);
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < steps; ++i) {
-        const int t0 = from + i * kManyTokens, buf = NB == 2 ? i & 1 : 0;
-        if (i + 1 < steps) load(i + 1);
-        if (t0 < wave_top) {
-            const bool masked = t0 + kManyTokens > wave_least || gone != 0;
-            f16 s[2] = {f16{}, f16{}};
+    h8 w[4];   // a step's weights in the order of the second product: of s[c / 2][8 (c % 2) ..] in w[c]
+    // this lane's place in the operands' rows, in bytes; of another piece of the row: the turned place
+    const uint32_t k_at = (n32 * KS + (hh ^ turn_k(n32)) * 8) * 2;
+    const int v_row = 4 * hh + ((lane & 15) >> 2);
+    const uint32_t v_at = (v_row * VS + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ turn_v(v_row)) * 8 + 4 * (lane & 1)) * 2;
+    // First half of step j: the matrix instructions in QS slots of two of each product, their operands read one slot ahead; and between
+    // them, of codes, V of this step and K of the next from registers to LDS and the loads behind those.  The scores of token 32 k + 8
+    // (e / 4) + 4 hh + e % 4 come to s[k][e].
+    auto matrix = [&](int j, auto with_scores, auto with_values, f16* s) {
+        constexpr bool S = decltype(with_scores)::value, V = decltype(with_values)::value;
+        const uint8_t *const kp = (const uint8_t*)(lk + (j & 1) * KL), *const vp = (const uint8_t*)(lv + ((j & 1) ^ 1) * VL);
+        const bool v_here = j < steps, k_here = j + 1 < steps, k_next = j + 2 < steps;
+        if (j + 2 - at >= 16) {
+            at += 14;
+            win = window(ahead);
+            ahead = fetch(at + 14);
+        }
+        h8 ko[2][2], vo[2][2];
+        auto read = [&](int st) {
 #pragma unroll
-            for (int st = 0; st < QS; ++st)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    const u4 kv = *reinterpret_cast<const u4*>(lk[buf] + (32 * kt + n32) * KS + 16 * st + 8 * hh);
-                    s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, kv), qv[st], s[kt], 0, 0, 0);
+            for (int k = 0; k < 2; ++k) {
+                if constexpr (S) ko[st & 1][k] = *reinterpret_cast<const h8*>(kp + (DIRECT ? k_at ^ (uint32_t)(32 * st) : k_at + 32 * st) + 32 * k * KS * 2);
+                if constexpr (V) {
+                    const int c = (2 * st + k) / DT, d = (2 * st + k) % DT;
+                    const uint8_t *const p0 = vp + (DIRECT ? v_at ^ (uint32_t)(64 * d) : v_at + 64 * d) + 16 * c * VS * 2;
+                    const uint8_t *const p1 = vp + (DIRECT ? v_at ^ (uint32_t)(64 * d + (DP == 64 ? 0 : 32)) : v_at + 64 * d) + (16 * c + 8) * VS * 2;
+                    vo[st & 1][k] = join(read_transposed((const uint16_t*)p0), read_transposed((const uint16_t*)p1));
                 }
+            }
+        };
+        read(0);
+#pragma unroll
+        for (int st = 0; st < QS; ++st) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (st + 1 < QS) read(st + 1);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (CODES) {
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const f4 c = *reinterpret_cast<const f4*>(&s_ks[buf][32 * kt + 8 * e + 4 * hh]), lg = *reinterpret_cast<const f4*>(&s_lg[buf][32 * kt + 8 * e + 4 * hh]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kt][4 * e + r] = fmaf(s[kt][4 * e + r], c[r], lg[r]);
+                for (int i = st * 2 * LV / QS; i < (st + 1) * 2 * LV / QS; ++i) {   // V first: it is loaded first
+                    if (i < LV) {
+                        if (v_here) store_v(i, j);
+                        if (k_here) load_v(i);
+                    } else {
+                        if (i == LV && k_next) locate(j + 2);
+                        if (k_here) store_k(i - LV, j + 1);
+                        if (k_next) load_k(i - LV);
                     }
-            } else {
-                s[0] *= a.scale2;
-                s[1] *= a.scale2;
-            }
-            if (masked) {
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int t = 32 * kt + 8 * (e >> 2) + 4 * hh + (e & 3);
-                        if (t0 + t >= vis || (gone >> (2 * kt + (e >> 3)) & 1u)) s[kt][e] = -INFINITY;
-                    }
-            }
-            float lm = s[0][0];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) lm = fmaxf(lm, s[kt][e]);
-            if (any(lm > m + 8.0f)) {
-                lm = fmaxf(fmaxf(lm, __shfl_xor(lm, 32, 64)), m);
-                const float fade = __builtin_amdgcn_exp2f(m - lm);
-                m = lm;
-                l *= fade;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= fade;
+                }
             }
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int k = 0; k < 2; ++k) {
+                if constexpr (S) s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[st & 1][k], qv[st], st ? s[k] : f16{}, 0, 0, 0);
+                if constexpr (V) o[(2 * st + k) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vo[st & 1][k], w[(2 * st + k) / DT], o[(2 * st + k) % DT], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (k_here) store_scales(j + 1);
+        if (k_next) load_scales(j + 2);
+    };
+    auto softmax = [&](int j, f16* s) {
+        const int t0 = t_of(j);
+        const unsigned gone = gone_at(j);
+        const bool masked = t0 + kManyTokens > wave_least || gone != 0;
+        const float* par = &s_par[CODES ? grp : 0][j & 1][0][0];
+        if constexpr (CODES) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    f4 inv = {1, 1, 1, 1};
-                    if constexpr (CODES) inv = *reinterpret_cast<const f4*>(&s_inv[buf][32 * kt + 8 * e + 4 * hh]);
+                    const f4 c = *reinterpret_cast<const f4*>(par + 32 * k + 8 * e + 4 * hh), lg = *reinterpret_cast<const f4*>(par + kManyTokens + 32 * k + 8 * e + 4 * hh);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float w = __builtin_amdgcn_exp2f(s[kt][4 * e + r] - m);
-                        s[kt][4 * e + r] = w;
-                        if constexpr (CODES) l += w != 0.0f || !masked ? w * inv[r] : 0.0f;   // (a masked token's scale may be anything)
-                        else l += w;
-                    }
+                    for (int r = 0; r < 4; ++r) s[k][4 * e + r] = fmaf(s[k][4 * e + r], c[r], lg[r]);
                 }
-            const uint16_t* const src = lv[buf] + (4 * hh + ((lane & 15) >> 2)) * VS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                u4 pw;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = pack2(s[c >> 1][8 * (c & 1) + 2 * e], s[c >> 1][8 * (c & 1) + 2 * e + 1]);
-                const h8 p = __builtin_bit_cast(h8, pw);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const h8 v = join(read_transposed(src + 16 * c * VS + 32 * d), read_transposed(src + (16 * c + 8) * VS + 32 * d));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p, o[d], 0, 0, 0);
-                }
-            }
         }
-        if constexpr (NB == 1) __syncthreads();
-        if (i + 1 < steps) store(i + 1);
-        gone = gone_next;
-        __syncthreads();
+        if (masked) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int t = 32 * k + 8 * (e >> 2) + 4 * hh + (e & 3);
+                    if (t0 + t >= vis || (gone >> (2 * k + (e >> 3)) & 1u)) s[k][e] = -INFINITY;
+                }
+        }
+        float lm = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) lm = fmaxf(fmaxf(lm, s[0][e]), s[1][e]);
+        if constexpr (!CODES) lm *= scale2;
+        if (any(lm > m + 8.0f)) {
+            lm = fmaxf(fmaxf(lm, __shfl_xor(lm, 32, 64)), m);
+            const float fade = __builtin_amdgcn_exp2f(m - lm);
+            m = lm;
+            l *= fade;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= fade;
+        }
+        float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            u4 pw;
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                float x[4];
+                f4 inv = {0, 0, 0, 0};
+                if constexpr (CODES) inv = *reinterpret_cast<const f4*>(par + 2 * kManyTokens + 16 * c + 4 * e + 4 * hh);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float v = s[c >> 1][8 * (c & 1) + 2 * e + r];
+                    x[r] = __builtin_amdgcn_exp2f(CODES ? v - m : fmaf(v, scale2, -m));
+                    const float part = !CODES ? x[r] : x[r] != 0.0f || !masked ? x[r] * inv[r] : 0.0f;   // (a masked token's scale may be anything)
+                    (r & 1 ? sum1 : sum0) += part;
+                }
+                pw[e] = pack2(x[0], x[1]);
+                pw[e + 1] = pack2(x[2], x[3]);
+            }
+            w[c] = __builtin_bit_cast(h8, pw);
+        }
+        l += sum0 + sum1;
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]), "+v"(l));   // (all of it in this half of the step)
+    };
+
+    if (threadIdx.x == 0) s_odd.clear();
+    if (steps) {   // K of step 0 to LDS, V of step 0 and K of step 1 on their way
+        win = window(fetch(0));
+        ahead = fetch(14);
+        locate(0);
+        load_scales(0);
+        if constexpr (CODES) {
+#pragma unroll
+            for (int u = 0; u < LV; ++u) load_k(u);
+#pragma unroll
+            for (int u = 0; u < LV; ++u) load_v(u);
+#pragma unroll
+            for (int u = 0; u < LV; ++u) store_k(u, 0);
+            store_scales(0);
+            if (steps > 1) {
+                locate(1);
+                load_scales(1);
+#pragma unroll
+                for (int u = 0; u < LV; ++u) load_k(u);
+            }
+        } else {
+            send_k(0);
+            send(-1);
+        }
     }
+    if constexpr (DIRECT) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    lds_barrier();
+    if (GROUPS == 2 && grp == 1) lds_barrier();   // half a step behind
+    // the steps that this wave's rows see anything of; it takes part in the others' staging and barriers
+    const int mine = min(steps, max(0, (wave_top - from - grp * kManyTokens + GROUPS * kManyTokens - 1) / (GROUPS * kManyTokens)));
+    const std::true_type yes;
+    const std::false_type no;
+    int j = 0;
+    if (mine > 0) {
+        {
+            f16 s[2];
+            matrix(0, yes, no, s);
+            lds_barrier();
+            send(0);
+            softmax(0, s);
+            arrive(0);
+            lds_barrier();
+        }
+#pragma unroll 1
+        for (j = 1; j < mine; ++j) {
+            f16 s[2];
+            __builtin_amdgcn_s_setprio(2);   // (ahead of the other group's wave, which has more to choose from)
+            matrix(j, yes, yes, s);
+            __builtin_amdgcn_s_setprio(0);
+            lds_barrier();
+            send(j);
+            softmax(j, s);
+            arrive(j);
+            lds_barrier();
+        }
+        matrix(j, no, yes, nullptr);
+        lds_barrier();
+        send(j);
+        arrive(j++);
+        lds_barrier();
+    }
+#pragma unroll 1
+    for (; j <= rounds; ++j) {
+        matrix(j, no, no, nullptr);
+        lds_barrier();
+        send(j);
+        arrive(j);
+        lds_barrier();
+    }
+    if (GROUPS == 2 && grp == 0) lds_barrier();   // (as many as the other group's)
 
     l += __shfl_xor(l, 32, 64);
-    if (R < nrows) {
+    if constexpr (GROUPS == 2) {   // the second group's sums into the first's, lane by lane
+        f4* const so = reinterpret_cast<f4*>(lds) + (wave * DT * 4) * 64 + lane;
+        if (grp == 1) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) so[(d * 4 + e) * 64] = f4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+            if (hh == 0) s_ml[32 * wave + n32] = float2{m, l};
+        }
+        lds_barrier();
+        if (grp == 0) {
+            const float2 other = s_ml[32 * wave + n32];
+            const float both = fmaxf(m, other.x), f0 = __builtin_amdgcn_exp2f(m - both), f1 = __builtin_amdgcn_exp2f(other.x - both);
+            m = both;
+            l = l * f0 + other.y * f1;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f4 v = so[(d * 4 + e) * 64];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[d][4 * e + r] = fmaf(o[d][4 * e + r], f0, v[r] * f1);
+                }
+        }
+    }
+    if (grp == 0 && R < nrows) {
         const int64_t yrow = (int64_t)(sq.first + tok) * a.heads_q + hq;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
@@ -704,8 +916,9 @@ void launch_attn_many(const AttnArgs& a, const dim3& grid, hipStream_t s);
     template <>                                                                                                      \
     void launch_attn_many<DP>(const AttnArgs& a, const dim3& grid, hipStream_t s)                                    \
     {                                                                                                                \
-        if (a.c.kv_bits == 8) attn_many_kernel<DP, true><<<grid, 256, 0, s>>>(a);                                    \
-        else attn_many_kernel<DP, false><<<grid, 256, 0, s>>>(a);                                                    \
+        constexpr int G = DP > 128 ? 1 : 2; /* (two groups of the widest heads run out of registers) */                 \
+        if (a.c.kv_bits == 8) attn_many_kernel<DP, true, G><<<grid, 256 * G, 0, s>>>(a);                             \
+        else attn_many_kernel<DP, false, G><<<grid, 256 * G, 0, s>>>(a);                                             \
     }                                                                                                                \
     }
 
