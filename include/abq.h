@@ -435,7 +435,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
  *   out[m,:] = half_rne( y[m,:] + scale[i] * B_i (A_i x[m,:]) ),  i = ids[m];   out[m,:] = y[m,:] where ids[m] is outside 0..adapters-1
  * x is the projection's input before quantization (y_fp16_out of the producers above), y its output.  A_i x is summed in
  * binary32 and enters the second product with 21 bits or more of its row's largest element.
- *   rank       1..256 (pad smaller adapters of a pool with zeros);  M, N >= 1, 1 <= K <= ABQ_MAX_K
+ *   rank       1..256 (pad smaller adapters of a pool with zeros);  1 <= M <= 2^19, N >= 1, 1 <= K <= ABQ_MAX_K
  *   x [M][K] row stride ldx;  ids [M] int32 (device);  a [adapters][rank][K], b [adapters][N][rank] binary16;
  *   scale [adapters] float;  y [M][N] row stride ldy;  out [M][N] row stride ldout: y itself (same stride), or no overlap
  *   (strides in elements, any value >= K or N)

@@ -942,7 +942,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
 
 static int check_lora_shape(int M, int N, int K, int rank)
 {
-    return M < 1 || N < 1 || K < 1 || K > ABQ_MAX_K || rank < 1 || rank > 256 ? ABQ_ERR_SHAPE : ABQ_OK;
+    return M < 1 || M > (1 << 19) || N < 1 || K < 1 || K > ABQ_MAX_K || rank < 1 || rank > 256 ? ABQ_ERR_SHAPE : ABQ_OK;
 }
 
 size_t abq_lora_add_workspace_bytes(int M, int N, int K, int rank)

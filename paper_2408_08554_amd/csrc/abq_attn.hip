@@ -19,10 +19,16 @@ void launch_attn_many<128>(const AttnArgs&, const dim3&, hipStream_t);
 template <>
 void launch_attn_many<256>(const AttnArgs&, const dim3&, hipStream_t);
 
-// One wave per row and head of a sequence that was shared out: its parts as one.
-__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a)
+// The parts of a row and head that was shared out as one.  What bounds it is latency (sequence, maxima and sums, parts: three
+// dependent loads), so WAVES waves of a workgroup take the parts in turn, four at a time (few parts: a wave for each of four heads); a
+// wave holds up to 64 parts' maxima and sums in its lanes.
+template <int WAVES>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
-    const int row = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x, D = a.c.head_dim;
+    __shared__ __align__(16) f4 s_o[WAVES][64];
+    const int lane = threadIdx.x & 63, nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = WAVES == 4 ? nth : 0, D = a.c.head_dim;
+    const int row = blockIdx.x, hq = WAVES == 4 ? blockIdx.y : 4 * blockIdx.y + nth;
+    if (hq >= a.heads_q) return;
     int seq = 0;
     for (int s0 = 0; s0 < a.b.seqs; s0 += 64) {
         const int s = s0 + lane;
@@ -40,17 +46,36 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a)
     const int nparts = (top + per - 1) / per;
     if (nparts <= 1) return;   // (written by its workgroup)
     const int64_t yrow = (int64_t)row * a.heads_q + hq;
-    const float2* ml = a.part_ml + yrow * a.parts;
-    const float* o = a.part_o + yrow * a.parts * D;
-    float m = kFloor, l = 0.0f;
-    for (int p = 0; p < nparts; ++p) m = fmaxf(m, ml[p].x);
+    const float* const o = a.part_o + yrow * a.parts * D + 4 * lane;
+    const float2 ml = lane < nparts ? a.part_ml[yrow * a.parts + lane] : float2{kFloor, 0.0f};
+    const bool mine = 4 * lane < D;
+    // this wave's parts: its first four are on their way before their weights are known
+    f4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = mine && wave + WAVES * u < nparts ? *reinterpret_cast<const f4*>(o + (int64_t)(wave + WAVES * u) * D) : f4{0, 0, 0, 0};
+    float m = ml.x;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+    float l = f * ml.y;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
     f4 v = {0, 0, 0, 0};
-    for (int p = 0; p < nparts; ++p) {
-        const float f = __builtin_amdgcn_exp2f(ml[p].x - m);
-        l = fmaf(f, ml[p].y, l);
-        if (4 * lane < D) v += f * *reinterpret_cast<const f4*>(o + (int64_t)p * D + 4 * lane);
+    for (int p0 = wave; p0 < nparts; p0 += 4 * WAVES) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p0 + WAVES * u < nparts) v += __shfl(f, p0 + WAVES * u, 64) * x[u];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (mine && p0 + WAVES * (4 + u) < nparts) x[u] = *reinterpret_cast<const f4*>(o + (int64_t)(p0 + WAVES * (4 + u)) * D);
     }
-    if (4 * lane >= D) return;
+    if constexpr (WAVES == 4) {
+        s_o[wave][lane] = v;
+        __syncthreads();
+        if (wave != 0) return;
+        v = s_o[0][lane] + s_o[1][lane] + (s_o[2][lane] + s_o[3][lane]);
+    }
+    if (!mine) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (l == 0.0f) v = f4{0, 0, 0, 0};
     *reinterpret_cast<uint2*>(a.y + yrow * D + 4 * lane) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
@@ -113,7 +138,10 @@ hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int head
         else if (c.head_dim <= 128) launch_attn_few<128>(a, p.nr, grid, s);
         else launch_attn_few<256>(a, p.nr, grid, s);
     }
-    if (p.parts > 1) attn_join_kernel<<<dim3(b.rows, heads_q), 64, 0, s>>>(a);
+    if (p.parts > 1) {
+        if (p.parts > 8) attn_join_kernel<4><<<dim3(b.rows, heads_q), 256, 0, s>>>(a);
+        else attn_join_kernel<1><<<dim3(b.rows, (heads_q + 3) / 4), 256, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 
