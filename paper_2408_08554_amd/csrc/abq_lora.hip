@@ -32,230 +32,382 @@ __device__ __forceinline__ lu4 load_eight(const uint16_t* row, int k, int n)
     return v;
 }
 
-// The distinct adapters of sixteen rows, one after the other (lane l: row l % 16).
+// The same where all eight are there.  (No branch: a load that only some lanes take makes every later one wait for it.)
+__device__ __forceinline__ lu4 load_whole(const uint16_t* p)
+{
+    const u32x4_half v = *reinterpret_cast<const u32x4_half*>(p);
+    return lu4{v.x, v.y, v.z, v.w};
+}
+
+// The distinct adapters of up to 64 rows (lane l: row l), one after the other.
 struct Adapters {
     int id;          // of the lane's row, -1 for none
-    uint32_t left;   // rows whose adapter has not had its turn
-    __device__ __forceinline__ Adapters(const int32_t* ids, int m, int M, int adapters)
+    uint64_t left;   // rows whose adapter has not had its turn
+    __device__ __forceinline__ Adapters(const int32_t* ids, int m, int M, int adapters, bool mine)
     {
-        const int v = m < M ? ids[m] : -1;
+        const int v = mine && m < M ? ids[m] : -1;
         id = (unsigned)v < (unsigned)adapters ? v : -1;
-        left = (uint32_t)__ballot(id >= 0) & 0xFFFFu;
+        left = __ballot(id >= 0);
     }
-    __device__ __forceinline__ int next()   // -1: all had theirs
+    __device__ __forceinline__ int next(uint64_t* rows)   // its rows; -1: all had theirs
     {
         if (!left) return -1;
-        const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
-        left &= ~(uint32_t)__ballot(id == a);
+        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        *rows = __ballot(id == a);
+        left &= ~*rows;
         return a;
     }
 };
 
-// u[part][m][r] = sum over a part of K of A_i[r][k] x[m][k].  A workgroup: sixteen rows, a part of K (its four waves a quarter each),
-// the adapters number blockIdx.y, blockIdx.y + gridDim.y, ... of the tile.  RT tiles of sixteen ranks share a load of x.
-template <int RT>
+// u[part][m][r] = sum over a part of K of A_i[r][k] x[m][k].  A workgroup: MT tiles of sixteen rows, a part of K (its four waves a
+// quarter each), the adapters number blockIdx.y, blockIdx.y + gridDim.y, ... of its rows.  RT tiles of sixteen ranks share a load of x,
+// the tiles of rows one of A (a tile without rows of the adapter goes through it all the same: prompts have few adapters to a tile).
+template <int RT, int MT>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(int M, int K, int rank, int adapters, int slice, const uint16_t* __restrict__ x, int ldx, const int32_t* __restrict__ ids,
                                                           const uint16_t* __restrict__ a, float* __restrict__ u)
 {
-    __shared__ lf4 part[4][RT][64];
+    __shared__ lf4 part[4][RT * MT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    const int m = blockIdx.z * 16 + n16, quarter = slice >> 2;
-    Adapters turn(ids, m, M, adapters);
-    const uint16_t* const xr = x + (size_t)min(m, M - 1) * ldx;
+    const int m0 = blockIdx.z * 16 * MT, quarter = slice >> 2;
+    Adapters turn(ids, m0 + lane, M, adapters, lane < 16 * MT);
+    const uint16_t* xr[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) xr[j] = x + (size_t)min(m0 + 16 * j + n16, M - 1) * ldx;
     const int k0 = blockIdx.x * slice + wave * quarter, k1 = min(K, k0 + quarter);   // (quarters are whole steps of 32)
     int nth = 0;
-    for (int i = turn.next(); i >= 0; i = turn.next(), ++nth) {
+    uint64_t rows = 0;
+    for (int i = turn.next(&rows); i >= 0; i = turn.next(&rows), ++nth) {
         if (nth % (int)gridDim.y != (int)blockIdx.y) continue;
         const uint16_t* row[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) row[t] = a + ((size_t)i * rank + min(16 * t + n16, rank - 1)) * K;
-        lf4 acc[RT];
+        lf4 acc[RT][MT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = lf4{0, 0, 0, 0};
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[t][j] = lf4{0, 0, 0, 0};
+        auto step = [&](const lu4* av, const lu4* xv) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, av[t]), __builtin_bit_cast(lh8, xv[j]), acc[t][j], 0, 0, 0);
+        };
         int k = k0;
-        constexpr int AHEAD = RT <= 2 ? 4 : RT <= 4 ? 2 : 1;   // steps whose loads are in flight together
+        constexpr int AHEAD = RT + MT <= 3 ? 4 : RT + MT <= 9 ? 2 : 1;   // steps whose loads are in flight together
         for (; k + 32 * AHEAD <= k1; k += 32 * AHEAD) {
-            lu4 xv[AHEAD], av[AHEAD][RT];
+            lu4 xv[AHEAD][MT], av[AHEAD][RT];
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) {
-                const u32x4_half v = *reinterpret_cast<const u32x4_half*>(xr + k + 32 * s + 8 * g);
-                xv[s] = lu4{v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const u32x4_half w = *reinterpret_cast<const u32x4_half*>(row[t] + k + 32 * s + 8 * g);
-                    av[s][t] = lu4{w.x, w.y, w.z, w.w};
-                }
+                for (int j = 0; j < MT; ++j) xv[s][j] = load_whole(xr[j] + k + 32 * s + 8 * g);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) av[s][t] = load_whole(row[t] + k + 32 * s + 8 * g);
             }
 #pragma unroll
-            for (int s = 0; s < AHEAD; ++s)
-#pragma unroll
-                for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, av[s][t]), __builtin_bit_cast(lh8, xv[s]), acc[t], 0, 0, 0);
+            for (int s = 0; s < AHEAD; ++s) step(av[s], xv[s]);
         }
         for (; k < k1; k += 32) {
-            const lu4 xv = load_eight(xr, k + 8 * g, K);
+            lu4 xv[MT], av[RT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, load_eight(row[t], k + 8 * g, K)), __builtin_bit_cast(lh8, xv), acc[t], 0, 0, 0);
+            for (int j = 0; j < MT; ++j) xv[j] = load_eight(xr[j], k + 8 * g, K);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) av[t] = load_eight(row[t], k + 8 * g, K);
+            step(av, xv);
         }
         __syncthreads();   // (the adapter before is stored)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) part[wave][t][lane] = acc[t];
-        __syncthreads();
-        // a lane's four values: ranks 16 t + 4 g .. of row n16
-        if (turn.id == i) {
-            float* const dst = u + ((size_t)blockIdx.x * M + m) * rank;
-            for (int t = wave; t < RT; t += 4) {
-                const lf4 v = part[0][t][lane] + part[1][t][lane] + (part[2][t][lane] + part[3][t][lane]);
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (16 * t + 4 * g + e < rank) dst[16 * t + 4 * g + e] = v[e];
-            }
+            for (int j = 0; j < MT; ++j) part[wave][t * MT + j][lane] = acc[t][j];
+        __syncthreads();
+        // a lane's four values: ranks 16 t + 4 g .. of row 16 j + n16
+        for (int q = wave; q < RT * MT; q += 4) {
+            const int t = q / MT, j = q % MT;
+            if (!(rows >> (16 * j + n16) & 1)) continue;
+            const lf4 v = part[0][q][lane] + part[1][q][lane] + (part[2][q][lane] + part[3][q][lane]);
+            float* const dst = u + ((size_t)blockIdx.x * M + m0 + 16 * j + n16) * rank + 16 * t + 4 * g;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * t + 4 * g + e < rank) dst[e] = v[e];
         }
     }
 }
 
-// The rows of the output.  A workgroup: sixteen rows, `blocks` blocks of 256 columns (its waves 64 each).  u enters the product as two
-// halves, hi + lo, of u over the power of two above its row's largest element: 22 bits of it, for one matrix instruction per sixteen ranks
-// (16 k of hi, 16 of lo).  The rows of B are dealt to the operand's rows so that a lane ends with sixteen neighbouring columns of one row.
-__global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank, int adapters, int parts, int blocks, const int32_t* __restrict__ ids, const uint16_t* __restrict__ b,
-                                                          const float* __restrict__ scale, const float* __restrict__ u, const uint16_t* y, int ldy, uint16_t* out, int ldout)
+// u enters the second product as two halves, hi + lo, of u over the power of two above its row's largest element: 22 bits of it, for one
+// matrix instruction per sixteen ranks (16 k of hi, 16 of lo).
+__device__ __forceinline__ void split_u(float v, int e, uint16_t* hi, uint16_t* lo)
 {
-    constexpr int US = 256 + 8;   // halves of a row of u in LDS
-    __shared__ __align__(16) uint16_t hi[16 * US], lo[16 * US];
-    __shared__ float factor[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
-    const int m0 = blockIdx.y * 16, m = m0 + n16, RT = (rank + 15) >> 4;
-    const Adapters rows(ids, m, M, adapters);
+    const float w = ldexpf(v, -e);
+    const __half h = __float2half_rn(w);
+    *hi = __half_as_ushort(h);
+    *lo = __half_as_ushort(__float2half_rn(w - __half2float(h)));
+}
+__device__ __forceinline__ int exponent_above(float top) { return top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0; }
 
-    {   // sixteen threads a row: its parts added, the largest element, the two halves
-        const int r = tid >> 4, c = tid & 15, row = min(m0 + r, M - 1), id = ids[row];
-        const bool there = m0 + r < M && (unsigned)id < (unsigned)adapters;
-        float v[16], top = 0.0f;
-        const float* src = u + (size_t)row * rank;
+// Many rows: the parts of u added up and split once, a wave a row, where every workgroup of the second kernel would do it over.
+// halves [M][2][padded]: hi, lo, zeros behind the rank; factor [M]: the adapter's scale times the row's power of two.
+__global__ __launch_bounds__(256) void lora_split_kernel(int M, int rank, int padded, int adapters, int parts, const int32_t* __restrict__ ids, const float* __restrict__ scale,
+                                                         const float* __restrict__ u, uint16_t* __restrict__ halves, float* __restrict__ factor)
+{
+    const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (m >= M) return;
+    const int id = ids[m];
+    const bool there = (unsigned)id < (unsigned)adapters;
+    float v[4], top = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            v[t] = 0.0f;
-            if (t < RT && there && 16 * t + c < rank) {
-                for (int p = 0; p < parts; ++p) v[t] += src[(size_t)p * M * rank + 16 * t + c];
+    for (int q = 0; q < 4; ++q) {
+        v[q] = 0.0f;
+        if (64 * q >= rank) continue;
+        const int r = min(64 * q + lane, rank - 1);
+        float w[16];
+#pragma unroll
+        for (int p = 0; p < 16; ++p) w[p] = u[((size_t)min(p, parts - 1) * M + m) * rank + r];
+#pragma unroll
+        for (int p = 0; p < 16; ++p) v[q] += p < parts ? w[p] : 0.0f;
+        if (!there || 64 * q + lane >= rank) v[q] = 0.0f;
+        top = fmaxf(top, fabsf(v[q]));
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const int e = exponent_above(top);
+    if (lane == 0) factor[m] = there ? ldexpf(scale[id], e) : 0.0f;
+    uint16_t* const dst = halves + (size_t)m * 2 * padded;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (64 * q + lane < padded) split_u(v[q], e, dst + 64 * q + lane, dst + padded + 64 * q + lane);
+}
+
+// The rows of the output.  A workgroup: MT tiles of sixteen rows; its waves take blocks of 64 columns, `blocks` each (SPREAD: one block
+// for all four, and every fourth adapter each).  The rows of B are dealt to the operand's rows so that a lane ends with sixteen
+// neighbouring columns of one row.  EIGHTS: the rank is a multiple of eight.  SPLIT: u comes split, else in parts.
+template <int RT, int MT, bool SPREAD, bool EIGHTS, bool SPLIT>
+__global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank, int adapters, int parts, int blocks, const int32_t* __restrict__ ids, const uint16_t* __restrict__ b,
+                                                          const float* __restrict__ scale, const float* __restrict__ u, const uint16_t* __restrict__ halves, const float* __restrict__ factors,
+                                                          const uint16_t* y, int ldy, uint16_t* out, int ldout)
+{
+    constexpr int RP = 16 * RT, US = 2 * RP + 8;   // halves of a row of u, hi and lo, in LDS
+    __shared__ __align__(16) uint16_t us[16 * MT * US];
+    __shared__ float factor[16 * MT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
+    const int m0 = blockIdx.y * 16 * MT;
+    Adapters all(ids, m0 + lane, M, adapters, lane < 16 * MT);
+    const int n0 = SPREAD ? blockIdx.x * 64 : (blockIdx.x * 4 * blocks + wave) * 64;   // the wave's first block
+
+    // y of the first block, on its way early
+    lu4 yv[MT][2];
+    auto load_y = [&](int at) {
+        const int n = at + 16 * g;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            const uint16_t* const yr = y + (size_t)min(m0 + 16 * j + n16, M - 1) * ldy;
+            if (at + 64 <= N) {
+                yv[j][0] = load_whole(yr + n);
+                yv[j][1] = load_whole(yr + n + 8);
+            } else {
+                yv[j][0] = load_eight(yr, n, N);
+                yv[j][1] = load_eight(yr, n + 8, N);
+            }
+        }
+    };
+    if (n0 < N) load_y(n0);
+
+    if constexpr (SPLIT) {
+        constexpr int EACH = 2 * RP / 8, ALL = 16 * MT * EACH;   // vectors of eight halves
+#pragma unroll
+        for (int i = 0; i < (ALL + 255) / 256; ++i) {
+            const int v = i * 256 + tid, r = v / EACH, c = v % EACH;
+            if (ALL % 256 == 0 || v < ALL) *reinterpret_cast<lu4*>(us + r * US + 8 * c) = *reinterpret_cast<const lu4*>(halves + (size_t)min(m0 + r, M - 1) * 2 * RP + 8 * c);
+        }
+        if (tid < 16 * MT) factor[tid] = factors[min(m0 + tid, M - 1)];
+    } else {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {   // sixteen threads a row: its parts added, the largest element, the two halves
+            const int r = 16 * j + (tid >> 4), c = tid & 15, row = min(m0 + r, M - 1);
+            constexpr int PB = RT <= 4 ? 16 / RT : 4;   // parts whose loads are in flight together
+            float v[RT], top = 0.0f;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) v[t] = 0.0f;
+            for (int p0 = 0; p0 < parts; p0 += PB) {
+                float w[PB][RT];
+#pragma unroll
+                for (int p = 0; p < PB; ++p)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) w[p][t] = u[((size_t)min(p0 + p, parts - 1) * M + row) * rank + min(16 * t + c, rank - 1)];
+#pragma unroll
+                for (int p = 0; p < PB; ++p)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) v[t] += p0 + p < parts ? w[p][t] : 0.0f;
+            }
+            const int mine = __shfl(all.id, r, 64);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                if (mine < 0 || 16 * t + c >= rank) v[t] = 0.0f;
                 top = fmaxf(top, fabsf(v[t]));
             }
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+            const int e = exponent_above(top);
+            if (c == 0) factor[r] = mine >= 0 ? ldexpf(scale[mine], e) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) split_u(v[t], e, us + r * US + 16 * t + c, us + r * US + RP + 16 * t + c);
         }
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        int e = 0;
-        if (top > 0.0f && top < INFINITY) (void)frexpf(top, &e);
-        if (c == 0) factor[r] = there ? ldexpf(scale[id], e) : 0.0f;
-#pragma unroll
-        for (int t = 0; t < 16; ++t)
-            if (t < RT) {
-                const float w = ldexpf(v[t], -e);
-                const __half h = __float2half_rn(w);
-                hi[r * US + 16 * t + c] = __half_as_ushort(h);
-                lo[r * US + 16 * t + c] = __half_as_ushort(__float2half_rn(w - __half2float(h)));
-            }
     }
     __syncthreads();
-    const float f = factor[n16];
-    const uint16_t* const us = (g < 2 ? hi : lo) + n16 * US + 8 * (g & 1);
+    const uint16_t* const mine = us + n16 * US + (g < 2 ? 0 : RP) + 8 * (g & 1);
 
     for (int blk = 0; blk < blocks; ++blk) {
-        const int n0 = (blockIdx.x * blocks + blk) * 256 + wave * 64;
-        if (n0 >= N) return;
-        // y of this lane's columns
-        const int n = n0 + 16 * g;
-        const uint16_t* const yr = y + (size_t)min(m, M - 1) * ldy;
-        lu4 yv[2] = {lu4{0, 0, 0, 0}, lu4{0, 0, 0, 0}};
-        if (m < M) {
-            yv[0] = load_eight(yr, n, N);
-            yv[1] = load_eight(yr, n + 8, N);
-        }
-        lf4 res[4];
+        const int at = n0 + blk * 256, n = at + 16 * g;
+        if (at >= N) return;
+        if (blk) load_y(at);
+        auto store = [&](int j) {
+            uint16_t* const dst = out + (size_t)(m0 + 16 * j + n16) * ldout;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) res[t] = lf4{0, 0, 0, 0};
-        // operand row n16 of tile t: column n0 + 16 (n16 / 4) + 4 t + n16 % 4
+            for (int h = 0; h < 2; ++h)
+                if (n + 8 * h < N) store_row_part8(dst + n + 8 * h, n + 8 * h, N, yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]);
+        };
+        // operand row n16 of tile t: column at + 16 (n16 / 4) + 4 t + n16 % 4
         int nb[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) nb[t] = min(n0 + 16 * (n16 >> 2) + 4 * t + (n16 & 3), N - 1);
+        for (int t = 0; t < 4; ++t) nb[t] = min(at + 16 * (n16 >> 2) + 4 * t + (n16 & 3), N - 1);
         auto load = [&](int i, int rt, lu4* v) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] = load_eight(b + ((size_t)i * N + nb[t]) * rank, 16 * rt + 8 * (g & 1), rank);
+            for (int t = 0; t < 4; ++t) {
+                const uint16_t* const row = b + ((size_t)i * N + nb[t]) * rank;
+                const int r = 16 * rt + 8 * (g & 1);
+                if constexpr (EIGHTS) {
+                    v[t] = load_whole(row + min(r, rank - 8));
+                    if (r >= rank) v[t] = lu4{0, 0, 0, 0};
+                } else {
+                    v[t] = load_eight(row, r, rank);
+                }
+            }
         };
-        Adapters turn = rows;
-        int i = turn.next();
+        Adapters turn = all;
+        uint64_t rows = 0, then_rows = 0;
+        int nth = 0;
+        auto next = [&](uint64_t* r) {
+            for (;;) {
+                const int i = turn.next(r);
+                if (!SPREAD || i < 0 || (nth++ & 3) == wave) return i;
+            }
+        };
+        int i = next(&rows);
         lu4 bv[4];
         if (i >= 0) load(i, 0, bv);
         while (i >= 0) {
-            const int then = turn.next();
-            lf4 acc[4];
+            const int then = next(&then_rows);
+            lf4 acc[MT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = lf4{0, 0, 0, 0};
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[j][t] = lf4{0, 0, 0, 0};
+#pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 lu4 nv[4];   // the next sixteen ranks, or the next adapter's first
-                const bool more = rt + 1 < RT;
-                if (more || then >= 0) load(more ? i : then, more ? rt + 1 : 0, nv);
-                const lh8 uv = *reinterpret_cast<const lh8*>(us + 16 * rt);
+                if (rt + 1 < RT) load(i, rt + 1, nv);
+                else load(then >= 0 ? then : i, 0, nv);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, bv[t]), uv, acc[t], 0, 0, 0);
+                for (int j = 0; j < MT; ++j) {
+                    if (MT > 1 && !(rows >> (16 * j) & 0xFFFFu)) continue;
+                    const lh8 uv = *reinterpret_cast<const lh8*>(mine + 16 * j * US + 16 * rt);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, bv[t]), uv, acc[j][t], 0, 0, 0);
+                }
 #pragma unroll
                 for (int t = 0; t < 4; ++t) bv[t] = nv[t];
             }
-            if (rows.id == i) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) res[t] = acc[t];
-            }
-            i = then;
-        }
-        if (m < M) {
-            if (rows.id >= 0) {   // (a row without an adapter keeps its bits)
+            for (int j = 0; j < MT; ++j) {
+                if (!(rows >> (16 * j + n16) & 1)) continue;   // (a row takes its own adapter's result alone)
+                const float f = factor[16 * j + n16];
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    const uint32_t w = yv[e >> 3][(e & 7) >> 1];
-                    const float v0 = fmaf(f, res[e >> 2][e & 3], __half2float(__ushort_as_half((unsigned short)w)));
-                    const float v1 = fmaf(f, res[e >> 2][(e & 3) + 1], __half2float(__ushort_as_half((unsigned short)(w >> 16))));
-                    yv[e >> 3][(e & 7) >> 1] = (uint32_t)__half_as_ushort(__float2half_rn(v0)) | (uint32_t)__half_as_ushort(__float2half_rn(v1)) << 16;
+                    const uint32_t w = yv[j][e >> 3][(e & 7) >> 1];
+                    const float v0 = fmaf(f, acc[j][e >> 2][e & 3], __half2float(__ushort_as_half((unsigned short)w)));
+                    const float v1 = fmaf(f, acc[j][e >> 2][(e & 3) + 1], __half2float(__ushort_as_half((unsigned short)(w >> 16))));
+                    yv[j][e >> 3][(e & 7) >> 1] = (uint32_t)__half_as_ushort(__float2half_rn(v0)) | (uint32_t)__half_as_ushort(__float2half_rn(v1)) << 16;
                 }
+                store(j);
             }
-            uint16_t* const dst = out + (size_t)m * ldout;
+            rows = then_rows;
+            i = then;
+        }
+        if (!SPREAD || wave == 0) {   // a row without an adapter keeps its bits
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (n + 8 * h < N) store_row_part8(dst + n + 8 * h, n + 8 * h, N, yv[h][0], yv[h][1], yv[h][2], yv[h][3]);
+            for (int j = 0; j < MT; ++j) {
+                const int id = __shfl(all.id, 16 * j + n16, 64);
+                if (id < 0 && m0 + 16 * j + n16 < M) store(j);
+            }
         }
     }
 }
+
+// Tiles of rows that share a workgroup: many rows (prompts, whose tiles have one or few adapters) as many as the accumulators allow.
+static int lora_tiles(int M, int rank) { return M < 256 || rank > 128 ? 1 : rank > 64 ? 2 : 4; }
 
 // Parts of K, each a whole number of steps for four waves: few tiles of rows leave the chip idle and want many short parts, but the
 // second kernel adds them up once per workgroup.
 struct LoraPlan { int slice, parts; };
-static LoraPlan lora_plan(int M, int K)
+static LoraPlan lora_plan(int M, int K, int rank)
 {
-    const int tiles = (M + 15) / 16, wgs = tiles * std::min(M, 8);   // (a tile of a few requests has as many adapters)
-    const int want = std::max(1, std::min({256 / std::max(wgs, 1), (K + 255) / 256, 16}));
+    const int each = 16 * lora_tiles(M, rank), tiles = (M + each - 1) / each, wgs = M < 256 ? tiles * std::min(M, 8) : tiles;   // (a tile of a few requests has as many adapters)
+    const int want = std::max(1, std::min({(M < 256 ? 256 : 512) / std::max(wgs, 1), (K + 255) / 256, 16}));
     LoraPlan p;
     p.slice = ((K + want - 1) / want + 127) / 128 * 128;
     p.parts = (K + p.slice - 1) / p.slice;
     return p;
 }
 
-size_t lora_workspace_bytes(int M, int, int K, int rank) { return (size_t)lora_plan(M, K).parts * M * rank * sizeof(float); }
+// The workspace: the parts of u, and for many rows u split.
+static bool lora_split(int M) { return M >= 256; }
+static int lora_padded(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : rank <= 128 ? 128 : 256; }
+size_t lora_workspace_bytes(int M, int, int K, int rank)
+{
+    const size_t parts = align_up((size_t)lora_plan(M, K, rank).parts * M * rank * sizeof(float), 16);
+    return lora_split(M) ? parts + (size_t)M * (4 * lora_padded(rank) + sizeof(float)) : parts;
+}
+
+template <int RT, int MT>
+static void launch_lora(int M, int N, int K, int rank, int adapters, const uint16_t* x, int ldx, const int32_t* ids, const uint16_t* a, const uint16_t* b,
+                        const float* scale, const uint16_t* y, int ldy, uint16_t* out, int ldout, float* u, hipStream_t s)
+{
+    const LoraPlan p = lora_plan(M, K, rank);
+    const int tiles = (M + 16 * MT - 1) / (16 * MT);
+    // distinct adapters of a tile side by side where the tiles alone are few
+    lora_shrink_kernel<RT, MT><<<dim3(p.parts, tiles <= 16 ? std::min({M, adapters, 16}) : 1, tiles), 256, 0, s>>>(M, K, rank, adapters, p.slice, x, ldx, ids, a, u);
+    uint16_t* const halves = (uint16_t*)((uint8_t*)u + align_up((size_t)p.parts * M * rank * sizeof(float), 16));
+    float* const factors = (float*)(halves + (size_t)M * 2 * 16 * RT);
+    const int64_t columns = ((int64_t)N + 63) / 64;
+    auto expand = [&](auto kernel, unsigned wgs, int blocks) {
+        kernel<<<dim3(wgs, tiles), 256, 0, s>>>(M, N, rank, adapters, p.parts, blocks, ids, b, scale, u, halves, factors, y, ldy, out, ldout);
+    };
+    if (lora_split(M)) {
+        lora_split_kernel<<<(M + 3) / 4, 256, 0, s>>>(M, rank, 16 * RT, adapters, p.parts, ids, scale, u, halves, factors);
+        const int blocks = columns * tiles >= 8192 ? 4 : 1;
+        expand(rank % 8 ? lora_expand_kernel<RT, MT, false, false, true> : lora_expand_kernel<RT, MT, false, true, true>, (unsigned)((columns + 4 * blocks - 1) / (4 * blocks)), blocks);
+    } else if constexpr (MT == 1) {
+        if (M > 1 && adapters > 1) expand(rank % 8 ? lora_expand_kernel<RT, 1, true, false, false> : lora_expand_kernel<RT, 1, true, true, false>, (unsigned)columns, 1);
+        else expand(rank % 8 ? lora_expand_kernel<RT, 1, false, false, false> : lora_expand_kernel<RT, 1, false, true, false>, (unsigned)((columns + 3) / 4), 1);
+    }
+}
 
 hipError_t launch_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x, int ldx, const int32_t* ids, const uint16_t* a,
                            const uint16_t* b, const float* scale, const uint16_t* y, int ldy, uint16_t* out, int ldout, void* workspace,
                            hipStream_t s)
 {
-    const LoraPlan p = lora_plan(M, K);
-    const int tiles = (M + 15) / 16;
-    float* const u = (float*)workspace;
-    // distinct adapters of a tile side by side where the tiles alone are few
-    const dim3 grid(p.parts, tiles <= 16 ? std::min({M, adapters, 16}) : 1, tiles);
-#define ABQ_LORA_SHRINK(RT) lora_shrink_kernel<RT><<<grid, 256, 0, s>>>(M, K, rank, adapters, p.slice, x, ldx, ids, a, u)
-    if (rank <= 16) ABQ_LORA_SHRINK(1);
-    else if (rank <= 32) ABQ_LORA_SHRINK(2);
-    else if (rank <= 64) ABQ_LORA_SHRINK(4);
-    else if (rank <= 128) ABQ_LORA_SHRINK(8);
-    else ABQ_LORA_SHRINK(16);
-#undef ABQ_LORA_SHRINK
-    const int64_t columns = ((int64_t)N + 255) / 256;
-    const int blocks = columns * tiles >= 2048 ? 4 : 1;
-    lora_expand_kernel<<<dim3((unsigned)((columns + blocks - 1) / blocks), tiles), 256, 0, s>>>(M, N, rank, adapters, p.parts, blocks, ids, b, scale, u, y, ldy, out, ldout);
+    const int mt = lora_tiles(M, rank);
+    auto go = [&](auto rt, auto tiles) {
+        launch_lora<decltype(rt)::value, decltype(tiles)::value>(M, N, K, rank, adapters, x, ldx, ids, a, b, scale, y, ldy, out, ldout, (float*)workspace, s);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    if (rank <= 16) mt == 1 ? go(one, one) : go(one, four);
+    else if (rank <= 32) mt == 1 ? go(two, one) : go(two, four);
+    else if (rank <= 64) mt == 1 ? go(four, one) : go(four, four);
+    else if (rank <= 128) mt == 1 ? go(integral_constant<int, 8>{}, one) : go(integral_constant<int, 8>{}, two);
+    else go(integral_constant<int, 16>{}, one);
     return hipGetLastError();
 }
 
