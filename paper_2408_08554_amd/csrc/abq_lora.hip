@@ -179,9 +179,10 @@ __global__ __launch_bounds__(256) void lora_split_kernel(int M, int rank, int pa
 
 // The rows of the output.  A workgroup: MT tiles of sixteen rows; its waves take blocks of 64 columns, `blocks` each (SPREAD: one block
 // for all four, and every fourth adapter each).  The rows of B are dealt to the operand's rows so that a lane ends with sixteen
-// neighbouring columns of one row.  EIGHTS: the rank is a multiple of eight.  SPLIT: u comes split, else in parts.
-template <int RT, int MT, bool SPREAD, bool EIGHTS, bool SPLIT>
-__global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank, int adapters, int parts, int blocks, const int32_t* __restrict__ ids, const uint16_t* __restrict__ b,
+// neighbouring columns of one row.  FAST: a rank of whole eights, columns of whole blocks; the branches that the others need for their
+// ends cost a third of the time.  SPLIT: u comes split, else in parts.
+template <int RT, int MT, bool SPREAD, bool FAST, bool SPLIT>
+__global__ __launch_bounds__(256, MT == 4 && FAST ? 2 : 1) void lora_expand_kernel(int M, int N, int rank, int adapters, int parts, int blocks, const int32_t* __restrict__ ids, const uint16_t* __restrict__ b,
                                                           const float* __restrict__ scale, const float* __restrict__ u, const uint16_t* __restrict__ halves, const float* __restrict__ factors,
                                                           const uint16_t* y, int ldy, uint16_t* out, int ldout)
 {
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
             const uint16_t* const yr = y + (size_t)min(m0 + 16 * j + n16, M - 1) * ldy;
-            if (at + 64 <= N) {
+            if (FAST || at + 64 <= N) {
                 yv[j][0] = load_whole(yr + n);
                 yv[j][1] = load_whole(yr + n + 8);
             } else {
@@ -209,17 +210,24 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
             }
         }
     };
-    if (n0 < N) load_y(n0);
-
     if constexpr (SPLIT) {
-        constexpr int EACH = 2 * RP / 8, ALL = 16 * MT * EACH;   // vectors of eight halves
+        constexpr int EACH = 2 * RP / 8, ALL = 16 * MT * EACH, VT = (ALL + 255) / 256;   // vectors of eight halves
+        lu4 v[VT];
 #pragma unroll
-        for (int i = 0; i < (ALL + 255) / 256; ++i) {
-            const int v = i * 256 + tid, r = v / EACH, c = v % EACH;
-            if (ALL % 256 == 0 || v < ALL) *reinterpret_cast<lu4*>(us + r * US + 8 * c) = *reinterpret_cast<const lu4*>(halves + (size_t)min(m0 + r, M - 1) * 2 * RP + 8 * c);
+        for (int i = 0; i < VT; ++i) {
+            const int at = min(i * 256 + tid, ALL - 1);
+            v[i] = *reinterpret_cast<const lu4*>(halves + (size_t)min(m0 + at / EACH, M - 1) * 2 * RP + 8 * (at % EACH));
         }
-        if (tid < 16 * MT) factor[tid] = factors[min(m0 + tid, M - 1)];
+        const float f = factors[min(m0 + tid % (16 * MT), M - 1)];
+        if (n0 < N) load_y(n0);   // (behind what is waited for)
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+            const int at = i * 256 + tid;
+            if (ALL % 256 == 0 || at < ALL) *reinterpret_cast<lu4*>(us + at / EACH * US + 8 * (at % EACH)) = v[i];
+        }
+        if (tid < 16 * MT) factor[tid] = f;
     } else {
+        if (n0 < N) load_y(n0);
 #pragma unroll
         for (int j = 0; j < MT; ++j) {   // sixteen threads a row: its parts added, the largest element, the two halves
             const int r = 16 * j + (tid >> 4), c = tid & 15, row = min(m0 + r, M - 1);
@@ -262,8 +270,10 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
         auto store = [&](int j) {
             uint16_t* const dst = out + (size_t)(m0 + 16 * j + n16) * ldout;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (n + 8 * h < N) store_row_part8(dst + n + 8 * h, n + 8 * h, N, yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]);
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (FAST) *reinterpret_cast<u32x4_half*>(dst + n + 8 * h) = u32x4_half{yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]};
+                else if (n + 8 * h < N) store_row_part8(dst + n + 8 * h, n + 8 * h, N, yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]);
+            }
         };
         // operand row n16 of tile t: column at + 16 (n16 / 4) + 4 t + n16 % 4
         int nb[4];
@@ -274,7 +284,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
             for (int t = 0; t < 4; ++t) {
                 const uint16_t* const row = b + ((size_t)i * N + nb[t]) * rank;
                 const int r = 16 * rt + 8 * (g & 1);
-                if constexpr (EIGHTS) {
+                if constexpr (FAST) {
                     v[t] = load_whole(row + min(r, rank - 8));
                     if (r >= rank) v[t] = lu4{0, 0, 0, 0};
                 } else {
@@ -291,11 +301,21 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
                 if (!SPREAD || i < 0 || (nth++ & 3) == wave) return i;
             }
         };
+        // An adapter's operands on their way together as far as registers go: up to two tiles of ranks, the next adapter's too.
+        constexpr int LOADED = RT <= 4 ? RT : 2;
+        constexpr bool NEXT = RT <= 2;
         int i = next(&rows);
-        lu4 bv[4];
-        if (i >= 0) load(i, 0, bv);
+        lu4 bv[LOADED][4];
+        auto load_first = [&](int of, lu4 (*v)[4]) {
+#pragma unroll
+            for (int rt = 0; rt < LOADED; ++rt) load(of, rt, v[rt]);
+        };
+        if (i >= 0 && NEXT) load_first(i, bv);
         while (i >= 0) {
             const int then = next(&then_rows);
+            lu4 nv[NEXT ? LOADED : 1][4];
+            if constexpr (NEXT) load_first(then >= 0 ? then : i, nv);
+            else load_first(i, bv);
             lf4 acc[MT][4];
 #pragma unroll
             for (int j = 0; j < MT; ++j)
@@ -303,18 +323,22 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(int M, int N, int rank
                 for (int t = 0; t < 4; ++t) acc[j][t] = lf4{0, 0, 0, 0};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                lu4 nv[4];   // the next sixteen ranks, or the next adapter's first
-                if (rt + 1 < RT) load(i, rt + 1, nv);
-                else load(then >= 0 ? then : i, 0, nv);
+                lu4 now[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) now[t] = bv[rt % LOADED][t];
+                if (rt + LOADED < RT) load(i, rt + LOADED, bv[rt % LOADED]);
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
-                    if (MT > 1 && !(rows >> (16 * j) & 0xFFFFu)) continue;
                     const lh8 uv = *reinterpret_cast<const lh8*>(mine + 16 * j * US + 16 * rt);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, bv[t]), uv, acc[j][t], 0, 0, 0);
+                    for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(lh8, now[t]), uv, acc[j][t], 0, 0, 0);
                 }
+            }
+            if constexpr (NEXT) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) bv[t] = nv[t];
+                for (int rt = 0; rt < LOADED; ++rt)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) bv[rt][t] = nv[rt][t];
             }
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
@@ -378,16 +402,17 @@ static void launch_lora(int M, int N, int K, int rank, int adapters, const uint1
     uint16_t* const halves = (uint16_t*)((uint8_t*)u + align_up((size_t)p.parts * M * rank * sizeof(float), 16));
     float* const factors = (float*)(halves + (size_t)M * 2 * 16 * RT);
     const int64_t columns = ((int64_t)N + 63) / 64;
+    const bool fast = rank % 8 == 0 && N % 64 == 0;
     auto expand = [&](auto kernel, unsigned wgs, int blocks) {
         kernel<<<dim3(wgs, tiles), 256, 0, s>>>(M, N, rank, adapters, p.parts, blocks, ids, b, scale, u, halves, factors, y, ldy, out, ldout);
     };
     if (lora_split(M)) {
         lora_split_kernel<<<(M + 3) / 4, 256, 0, s>>>(M, rank, 16 * RT, adapters, p.parts, ids, scale, u, halves, factors);
         const int blocks = columns * tiles >= 8192 ? 4 : 1;
-        expand(rank % 8 ? lora_expand_kernel<RT, MT, false, false, true> : lora_expand_kernel<RT, MT, false, true, true>, (unsigned)((columns + 4 * blocks - 1) / (4 * blocks)), blocks);
+        expand(!fast ? lora_expand_kernel<RT, MT, false, false, true> : lora_expand_kernel<RT, MT, false, true, true>, (unsigned)((columns + 4 * blocks - 1) / (4 * blocks)), blocks);
     } else if constexpr (MT == 1) {
-        if (M > 1 && adapters > 1) expand(rank % 8 ? lora_expand_kernel<RT, 1, true, false, false> : lora_expand_kernel<RT, 1, true, true, false>, (unsigned)columns, 1);
-        else expand(rank % 8 ? lora_expand_kernel<RT, 1, false, false, false> : lora_expand_kernel<RT, 1, false, true, false>, (unsigned)((columns + 3) / 4), 1);
+        if (M > 1 && adapters > 1) expand(!fast ? lora_expand_kernel<RT, 1, true, false, false> : lora_expand_kernel<RT, 1, true, true, false>, (unsigned)columns, 1);
+        else expand(!fast ? lora_expand_kernel<RT, 1, false, false, false> : lora_expand_kernel<RT, 1, false, true, false>, (unsigned)((columns + 3) / 4), 1);
     }
 }
 

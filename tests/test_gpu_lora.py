@@ -43,6 +43,20 @@ def test_sizes_that_divide_nothing(abq, N, K):
     check(abq, make(40, N, K, 20, 3, seed=K))
 
 
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 100, 128, 136, 256])
+@pytest.mark.parametrize("M,adapters", [(1, 3), (20, 9), (270, 3), (333, 40)])
+def test_whole_blocks_of_columns(abq, rank, M, adapters):
+    """Columns in whole blocks of 64, for few and many rows, with the adapters in any order; and runs of rows."""
+    check(abq, make(M, 192, 160, rank, adapters, seed=rank + M))
+    if M > 100:
+        check(abq, make(M, 320, 1056, rank, adapters, seed=rank, ids=torch.arange(M) * adapters // M - 1))
+
+
+def test_many_rows_and_columns(abq):
+    check(abq, make(1100, 2048, 300, 16, 5, seed=1, ids=torch.arange(1100) * 5 // 1100))
+    check(abq, make(700, 4100, 64, 8, 3, seed=2))
+
+
 def test_every_row_its_own_adapter_and_all_rows_one(abq):
     check(abq, make(50, 96, 256, 16, 50, ids=torch.randperm(50)))
     check(abq, make(50, 96, 256, 16, 50, ids=torch.full((50,), 49)))
