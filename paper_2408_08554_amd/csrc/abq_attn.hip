@@ -7,17 +7,21 @@
 namespace abq {
 
 template <>
-void launch_attn_few<64>(const AttnArgs&, int, const dim3&, hipStream_t);
+void launch_attn_few<64>(const AttnArgs&, int, hipStream_t);
 template <>
-void launch_attn_few<128>(const AttnArgs&, int, const dim3&, hipStream_t);
+void launch_attn_many<64>(const AttnArgs&, hipStream_t);
 template <>
-void launch_attn_few<256>(const AttnArgs&, int, const dim3&, hipStream_t);
+void launch_attn_few<128>(const AttnArgs&, int, hipStream_t);
 template <>
-void launch_attn_many<64>(const AttnArgs&, const dim3&, hipStream_t);
+void launch_attn_many<128>(const AttnArgs&, hipStream_t);
 template <>
-void launch_attn_many<128>(const AttnArgs&, const dim3&, hipStream_t);
+void launch_attn_few<256>(const AttnArgs&, int, hipStream_t);
 template <>
-void launch_attn_many<256>(const AttnArgs&, const dim3&, hipStream_t);
+void launch_attn_many<256>(const AttnArgs&, hipStream_t);
+template <>
+void launch_attn_both<64>(const AttnArgs&, hipStream_t);
+template <>
+void launch_attn_both<128>(const AttnArgs&, hipStream_t);
 
 // The parts of a row and head that was shared out as one.  What bounds it is latency (sequence, maxima and sums, parts: three
 // dependent loads), so WAVES waves of a workgroup take the parts in turn, four at a time (few parts: a wave for each of four heads); a
@@ -46,8 +50,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     const int nparts = (top + per - 1) / per;
     if (nparts <= 1) return;   // (written by its workgroup)
     const int64_t yrow = (int64_t)row * a.heads_q + hq;
-    const float* const o = a.part_o + yrow * a.parts * D + 4 * lane;
-    const float2 ml = lane < nparts ? a.part_ml[yrow * a.parts + lane] : float2{kFloor, 0.0f};
+    const int64_t place = few ? a.few_part(seq, hq / a.group, i * a.group + hq % a.group) : a.many_part(yrow);
+    const float* const o = (few ? a.few_o : a.many_o) + place * D + 4 * lane;
+    const float2 ml = lane < nparts ? (few ? a.few_ml : a.many_ml)[place + lane] : float2{kFloor, 0.0f};
     const bool mine = 4 * lane < D;
     // this wave's parts: its first four are on their way before their weights are known
     f4 x[4];
@@ -84,64 +89,85 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 // Which kernels a step needs, and into how many parts sequences are cut at most; from the sizes that the host knows alone, so that a
 // captured launch serves whatever lengths the arrays hold later.
 struct AttnPlan {
-    int nr, few, few_parts, many_parts, parts;
-    int64_t many_tiles;
+    int nr, few, few_parts, few_rows, many_parts;
+    int64_t many_wgs;
+    bool both;   // one launch for the two parts
+    size_t few_places, many_places;   // of results of parts
 };
 static AttnPlan attn_plan(const abq_kv_cache& c, const abq_batch& b, int heads_q)
 {
     AttnPlan p{};
     const int group = heads_q / c.heads;
     const int64_t most = (int64_t)b.max_new * group, all = (int64_t)b.rows * group;
+    // Up to 32 rows of a sequence belong to the part for few rows; beside longer ones up to sixteen, so that one launch can take both.
+    // (24 rows each, 16 sequences of 1000, 4 heads: 16 us there, 22 as many rows; a group of 32, four of 1000: 14 and 20, and 32 of 2000
+    // 20.5 and 21.  33 requests, one of them a prompt of 100 tokens: 26 us in one launch, 46 as 32 rows and two launches.)
     p.nr = most <= 16 || (group <= 16 && most > 32) ? 1 : 2;
     p.few = group <= 32 && (b.seqs > 1 || most <= 32) ? 16 * p.nr : 0;
+    p.few_rows = (int)std::min<int64_t>(p.few, most);
+    p.both = p.few && most > p.few && p.nr == 1 && c.head_dim <= 128;
     const int tokens = (int)std::min<int64_t>(b.max_len, (int64_t)b.max_pages * c.page_size);
     p.few_parts = p.many_parts = 1;
+    // Parts until each compute unit has a workgroup (of codes two, which have half the bytes in flight); beside prompts half of them
+    // have one.  More parts balance better but have to be joined (us at 256, 512, 1024 workgroups; heads of 128: 32 sequences of 2048 on
+    // 8 heads 41, 47, 47, 8 of 1000 on 32 21, 25, 26, 40 of 2048 on 8 62, 62, 59; codes, 4 of 32768 on 8 58, 50, 54; a prompt of 333
+    // with eight decoding requests at 128 and 256: 30, 33).
     if (p.few) {
-        const int64_t wgs = (int64_t)b.seqs * c.heads;
-        p.few_parts = (int)std::min<int64_t>({(1024 + wgs - 1) / wgs, (tokens + kFewLeast - 1) / kFewLeast, 64});
+        const int64_t wgs = (int64_t)b.seqs * c.heads, want = p.both ? 128 : c.kv_bits == 8 ? 512 : 256;
+        p.few_parts = (int)std::min<int64_t>({(want + wgs - 1) / wgs, (tokens + kFewLeast - 1) / kFewLeast, 64});
     }
-    if (most > p.few) {
-        p.many_tiles = all / kManyRows + std::min<int64_t>(b.seqs, all / (p.few + 1));
-        const int64_t wgs = p.many_tiles * c.heads;
-        p.many_parts = (int)std::min<int64_t>({(256 + wgs - 1) / wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
+    if (most > p.few) {   // a workgroup to a compute unit (256 tokens over 4096, 8 heads: 37 us; of two, 47)
+        p.many_wgs = (all / kManyRows + std::min<int64_t>(b.seqs, all / (p.few + 1))) * c.heads;
+        p.many_parts = (int)std::min<int64_t>({(256 + p.many_wgs - 1) / p.many_wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
     }
-    p.parts = std::max(p.few_parts, p.many_parts);
+    p.few_places = p.few_parts > 1 ? (size_t)b.seqs * c.heads * p.few_rows * p.few_parts : 0;
+    p.many_places = p.many_parts > 1 ? (size_t)b.rows * heads_q * p.many_parts : 0;
     return p;
 }
 
 size_t attn_workspace_bytes(const abq_kv_cache& c, const abq_batch& b, int heads_q)
 {
     const AttnPlan p = attn_plan(c, b, heads_q);
-    return p.parts == 1 ? 0 : (size_t)b.rows * heads_q * p.parts * (c.head_dim * sizeof(float) + sizeof(float2));
+    return (p.few_places + p.many_places) * (c.head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int heads_q, const uint16_t* q, int ldq, float scale, bool causal,
                              uint16_t* y, void* workspace, hipStream_t s)
 {
     const AttnPlan p = attn_plan(c, b, heads_q);
-    AttnArgs a{c, b, heads_q, heads_q / c.heads, __builtin_ctz(c.page_size), q, ldq, (float)((double)scale * 1.44269504088896340736), causal, y, nullptr, nullptr,
-               p.parts, p.few, p.few_parts, p.many_parts};
-    if (p.parts > 1) {
-        a.part_o = (float*)workspace;
-        a.part_ml = (float2*)(a.part_o + (size_t)b.rows * heads_q * p.parts * c.head_dim);
+    const int64_t few_wgs = (int64_t)c.heads * b.seqs * p.few_parts;
+    if (p.many_wgs * p.many_parts + few_wgs > INT32_MAX) return hipErrorInvalidConfiguration;
+    AttnArgs a{};
+    a.c = c;
+    a.b = b;
+    a.heads_q = heads_q;
+    a.group = heads_q / c.heads;
+    a.page_shift = __builtin_ctz(c.page_size);
+    a.q = q;
+    a.ldq = ldq;
+    a.scale2 = (float)((double)scale * 1.44269504088896340736);
+    a.causal = causal;
+    a.y = y;
+    a.few = p.few;
+    a.few_parts = p.few_parts;
+    a.many_parts = p.many_parts;
+    a.few_rows = p.few_rows;
+    a.many_wgs = (unsigned)p.many_wgs;
+    a.few_o = (float*)workspace;   // (16-byte vectors first, the pairs behind them)
+    a.many_o = a.few_o + p.few_places * c.head_dim;
+    a.few_ml = (float2*)(a.many_o + p.many_places * c.head_dim);
+    a.many_ml = a.few_ml + p.few_places;
+    if (p.both) {
+        c.head_dim <= 64 ? launch_attn_both<64>(a, s) : launch_attn_both<128>(a, s);
+    } else {
+        if (p.many_wgs) c.head_dim <= 64 ? launch_attn_many<64>(a, s) : c.head_dim <= 128 ? launch_attn_many<128>(a, s) : launch_attn_many<256>(a, s);
+        if (p.few) c.head_dim <= 64 ? launch_attn_few<64>(a, p.nr, s) : c.head_dim <= 128 ? launch_attn_few<128>(a, p.nr, s) : launch_attn_few<256>(a, p.nr, s);
     }
-    if (p.many_tiles * c.heads > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (p.many_tiles) {
-        const dim3 grid((unsigned)(p.many_tiles * c.heads), p.many_parts);
-        if (c.head_dim <= 64) launch_attn_many<64>(a, grid, s);
-        else if (c.head_dim <= 128) launch_attn_many<128>(a, grid, s);
-        else launch_attn_many<256>(a, grid, s);
-    }
-    if (p.few) {
-        const dim3 grid(c.heads, b.seqs, p.few_parts);
-        if (c.head_dim <= 64) launch_attn_few<64>(a, p.nr, grid, s);
-        else if (c.head_dim <= 128) launch_attn_few<128>(a, p.nr, grid, s);
-        else launch_attn_few<256>(a, p.nr, grid, s);
-    }
-    if (p.parts > 1) {
-        if (p.parts > 8) attn_join_kernel<4><<<dim3(b.rows, heads_q), 256, 0, s>>>(a);
-        else attn_join_kernel<1><<<dim3(b.rows, (heads_q + 3) / 4), 256, 0, s>>>(a);
-    }
+    const int parts = std::max(p.few_parts, p.many_parts);
+    // (A prompt's rows fill the chip with a wave for each head; where a few rows have many parts, four waves share one.  One request of
+    // 32000 tokens: 44 us with one, 29 with four; a prompt of 256 over 4096 in up to eight parts: 37 and 49.)
+    if (parts > 8) attn_join_kernel<4><<<dim3(b.rows, heads_q), 256, 0, s>>>(a);
+    else if (parts > 1) attn_join_kernel<1><<<dim3(b.rows, (heads_q + 3) / 4), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -2,3 +2,4 @@
 #include "abq_attn_kernels.h"
 
 ABQ_ATTN_INSTANTIATE(128)
+ABQ_ATTN_INSTANTIATE_BOTH(128)

@@ -39,11 +39,14 @@ struct AttnArgs {
     float scale2;        // scale * log2 e
     bool causal;
     uint16_t* y;
-    float* part_o;       // [rows][heads_q][parts][head_dim], not yet divided by the sum
-    float2* part_ml;     // [rows][heads_q][parts]: (m, sum)
-    int parts;           // places per row and head there
-    int few, few_parts;  // sequences of up to `few` rows (tokens * group) go to the kernel for few rows, in so many parts at most
-    int many_parts;
+    int few, few_parts, many_parts;   // sequences of up to `few` rows (tokens * group) are the business of the part for few rows; parts at most
+    int few_rows;        // and have at most so many rows
+    unsigned many_wgs;   // workgroups of the part for many rows, per part of the tokens
+    float *few_o, *many_o;      // results of parts, not yet divided by the sum: [seqs][heads][few_rows][few_parts][head_dim], [rows][heads_q][many_parts][head_dim]
+    float2 *few_ml, *many_ml;   // their (m, sum)
+    // number of the first part of row R (token * group + query head) of a sequence
+    __device__ __forceinline__ int64_t few_part(int seq, int head, int R) const { return (((int64_t)seq * c.heads + head) * few_rows + R) * few_parts; }
+    __device__ __forceinline__ int64_t many_part(int64_t yrow) const { return yrow * many_parts; }
 };
 
 // A sequence's rows and tokens within all bounds.
@@ -134,7 +137,8 @@ struct OddTokens {
 };
 // ... and what they hold is added to the results of the rows that see them, behind the stores of rows R0 .. R1 - 1.  (Whatever positive
 // weight it has, it makes the sum infinite or NaN; what has gone through the product is so already.)
-__device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence& sq, int seq, int head, int R0, int R1, int first, int last, int part, int nparts)
+template <class F>   // part_of(R, yrow): where the part's result of a row is, null when the row's result is whole
+__device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence& sq, int seq, int head, int R0, int R1, int first, int last, F&& part_of)
 {
     __syncthreads();
     const int D = a.c.head_dim;
@@ -147,8 +151,8 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
         }
         if (x == 0.0f) continue;
         const int64_t yrow = (int64_t)(sq.first + R / a.group) * a.heads_q + head * a.group + R % a.group;
-        if (nparts > 1) {
-            a.part_o[(yrow * a.parts + part) * D + d] += x;
+        if (float* const o = part_of(R, yrow)) {
+            o[d] += x;
         } else {
             uint16_t* const y = a.y + yrow * D + d;
             *y = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(*y)) + x));
@@ -160,12 +164,16 @@ constexpr float kFloor = -1e30f;   // m of a row that has seen nothing: any scor
 
 // ---- few rows ------------------------------------------------------------------------------------
 // One workgroup per sequence, key head and part of the tokens; NR tiles of sixteen rows (token * group + query head).  Its
-// four waves take 32 tokens in turn, each with a maximum, sums and an LDS region of its own (no barrier in the loop), and are
+// WAVES waves take 32 tokens in turn, each with a maximum, sums and an LDS region of its own (no barrier in the loop), and are
 // joined at the end.  K goes from memory straight into the matrix operand's registers, V through LDS for the transposition.
 // What bounds it: memory.  A wave has 16 KB in flight (32 tokens of K and V, 128 halves each) from the moment it has used the
-// last ones, and three or four workgroups share a compute unit.
-template <int DP, bool CODES, int NR>
-__global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
+// last ones, and two to four workgroups share a compute unit.  32 sequences of 2048 tokens, 32 heads on 8 of 128: 148 us, 5.5 TB/s (a
+// large copy: 5.1); as codes, 4 of 32768: 41 us and 5 for the joining, 219 MB at 5.3 TB/s.  One sequence of 513 is latency: 7.6 us
+// (6.5 for a lone workgroup's one step) and 2.8 for the joining.
+template <int DP, int WAVES>
+constexpr int kFewLds = WAVES * kFewTokens * (DP + 16);   // halves
+template <int DP, bool CODES, int NR, int WAVES>
+__device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int head, int seq, int part)
 {
     constexpr int DT = DP / 16;                      // tiles of sixteen columns
     constexpr int QS = DP / 32;                      // steps of the first product
@@ -175,12 +183,11 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
     constexpr int VV = kFewTokens / TPL;             // 16-byte loads of a lane per step's V
     constexpr int VS = DP + 16;                      // halves of a row of V in LDS: eight banks on, sixteen lanes of a transposing read take all
     constexpr int OS = DP + 4;                       // floats of a row when the waves are joined
-    __shared__ __align__(16) uint16_t lds[4 * kFewTokens * VS];
-    __shared__ float2 s_ml[4][16];
+    __shared__ float2 s_ml[WAVES][16];
     __shared__ OddTokens s_odd;
-    static_assert(sizeof(lds) >= 4 * 16 * OS * sizeof(float), "the waves are joined in the memory of V");
+    static_assert(kFewLds<DP, WAVES> == WAVES * kFewTokens * VS && kFewLds<DP, WAVES> * 2 >= WAVES * 16 * OS * 4, "the waves are joined in the memory of V");
 
-    const int head = blockIdx.x, seq = blockIdx.y, part = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4, D = a.c.head_dim;
     const Sequence sq(a, seq);
     const int nrows = sq.tokens * a.group;
@@ -227,13 +234,13 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
     int pages_at = 0, table = -1;   // the pages of the wave's next 32 steps, two to a step: lane 2 i + j holds step i's j-th
     auto fetch_pages = [&](int i) {
         pages_at = i;
-        const int t = from + ((i + (lane >> 1)) * 4 + wave) * kFewTokens + 16 * (lane & 1);
+        const int t = from + ((i + (lane >> 1)) * WAVES + wave) * kFewTokens + 16 * (lane & 1);
         table = t < to ? page_of(a.b, a.c, a.page_shift, seq, t) : -1;
     };
     int pg[2];   // (of the step that is loaded)
     auto load = [&](int i) {
         if (i - pages_at >= 32) fetch_pages(i);
-        const int t0 = from + (i * 4 + wave) * kFewTokens;
+        const int t0 = from + (i * WAVES + wave) * kFewTokens;
         int64_t vec[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -261,14 +268,14 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
         }
     };
 
-    const int steps = to > from + wave * kFewTokens ? (to - from - wave * kFewTokens + 4 * kFewTokens - 1) / (4 * kFewTokens) : 0;
+    const int steps = to > from + wave * kFewTokens ? (to - from - wave * kFewTokens + WAVES * kFewTokens - 1) / (WAVES * kFewTokens) : 0;
     if (steps) {
         fetch_pages(0);
         load(0);
     }
 #pragma unroll 1
     for (int i = 0; i < steps; ++i) {
-        const int t0 = from + (i * 4 + wave) * kFewTokens;
+        const int t0 = from + (i * WAVES + wave) * kFewTokens;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const bool masked = t0 + kFewTokens > least || pg[0] < 0 || pg[1] < 0;
         const bool gone0 = pg[0] < 0, gone1 = pg[1] < 0;
@@ -367,7 +374,7 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
         }
     }
 
-    // the four waves' sums as one, a tile of rows at a time
+    // the waves' sums as one, a tile of rows at a time, 4 WAVES threads to a row
     float* const so = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
@@ -378,34 +385,35 @@ __global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
 #pragma unroll
         for (int d = 0; d < DT; ++d) *reinterpret_cast<f4*>(so + (wave * 16 + n16) * OS + 16 * d + 4 * g) = o[t][d];
         __syncthreads();
-        const int r = tid >> 4, R = 16 * t + r;
+        constexpr int TPR = 4 * WAVES;
+        const int r = tid / TPR, R = 16 * t + r;
         if (R < nrows) {
-            float top_m = kFloor, sum = 0.0f, f[4];
+            float top_m = kFloor, sum = 0.0f, f[WAVES];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top_m = fmaxf(top_m, s_ml[w][r].x);
+            for (int w = 0; w < WAVES; ++w) top_m = fmaxf(top_m, s_ml[w][r].x);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 f[w] = __builtin_amdgcn_exp2f(s_ml[w][r].x - top_m);
                 sum += f[w] * s_ml[w][r].y;
             }
             const int64_t yrow = (int64_t)(sq.first + R / a.group) * a.heads_q + head * a.group + R % a.group;
-            for (int d = 4 * (tid & 15); d < D; d += 64) {
+            for (int d = 4 * (tid % TPR); d < D; d += 4 * TPR) {
                 f4 v = {0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v += f[w] * *reinterpret_cast<const f4*>(so + (w * 16 + r) * OS + d);
+                for (int w = 0; w < WAVES; ++w) v += f[w] * *reinterpret_cast<const f4*>(so + (w * 16 + r) * OS + d);
                 if (nparts > 1) {
-                    *reinterpret_cast<f4*>(a.part_o + (yrow * a.parts + part) * D + d) = v;
+                    *reinterpret_cast<f4*>(a.few_o + (a.few_part(seq, head, R) + part) * D + d) = v;
                 } else {
                     const float inv_sum = sum == 0.0f ? 0.0f : 1.0f / sum;
                     if (sum == 0.0f) v = f4{0, 0, 0, 0};
                     *reinterpret_cast<uint2*>(a.y + yrow * D + d) = uint2{pack2(v[0] * inv_sum, v[1] * inv_sum), pack2(v[2] * inv_sum, v[3] * inv_sum)};
                 }
             }
-            if (nparts > 1 && (tid & 15) == 0) a.part_ml[yrow * a.parts + part] = float2{top_m, sum};
+            if (nparts > 1 && tid % TPR == 0) a.few_ml[a.few_part(seq, head, R) + part] = float2{top_m, sum};
         }
     }
     if constexpr (!CODES) {
-        if (s_odd.any()) add_not_finite(a, sq, seq, head, 0, nrows, s_odd.first, s_odd.last, part, nparts);
+        if (s_odd.any()) add_not_finite(a, sq, seq, head, 0, nrows, s_odd.first, s_odd.last, [&](int R, int64_t) { return nparts > 1 ? a.few_o + (a.few_part(seq, head, R) + part) * D : nullptr; });
     }
 }
 
@@ -471,11 +479,16 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t* p) { return (uin
 // One workgroup per key head, 128 rows (token * group + query head) and part of the tokens.  GROUPS groups of four waves, a
 // wave for 32 of the rows in each; the groups take the steps of 64 tokens in turn and are joined at the end.  A step of a group has two
 // halves with a barrier behind each: the matrix instructions (scores of this step, and the weights of the last one times
-// its values), and everything else (softmax, the next K and this V to LDS, loads).  The second group runs half a step behind the
-// first, so that of the two waves of a SIMD one has matrix and the other vector work.  Each group has one buffer for K and one
-// for V: K is read in the first half and written in the second, V written in the second and read in the next first.
+// its values), and everything else (softmax, loads; of codes also the next step's way through registers to LDS).  The second group runs
+// half a step behind the first, so that of the two waves of a SIMD one has matrix and the other vector work.  Each group has two
+// buffers for K and two for V, of steps in turn; binary16 goes into them straight from memory, the next but one while this is used.
+// What bounds it: of a step's 3400 clocks the matrix half takes 1500 and the rest 1900 (1150 of them softmax),
+// which the other group's matrix half hides all but 400 of.  1024 tokens over 15360, 32 heads on 8 of 128: 275 us (969 TFLOP/s; one group alone 370), as codes 354 (750);
+// a prompt of 2048, 32 heads on 8: 53 us (645, its causal edge and 256 tiles for 256 units included).
 template <int DP, bool CODES, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArgs a)
+constexpr int kManyLds = GROUPS * 2 * kManyTokens * (CODES ? 2 * DP + 40 : 2 * DP);   // halves
+template <int DP, bool CODES, int GROUPS>
+__device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsigned index, int part)
 {
     constexpr int DT = DP / 32;                       // tiles of 32 columns of the result
     constexpr int QS = DP / 16;                       // steps of the first product
@@ -490,20 +503,20 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArg
     constexpr int KL = kManyTokens * KS, VL = kManyTokens * VS;   // halves of a buffer
     constexpr int GL = 2 * (KL + VL);                 // of a group
     static_assert(GROUPS == 1 || GROUPS * GL * 2 >= kManyRows * DP * 4, "the groups are joined in the memory of K and V");
-    __shared__ __align__(16) uint16_t lds[GROUPS * GL];
+    static_assert(kManyLds<DP, CODES, GROUPS> == GROUPS * GL);
     __shared__ __align__(16) float s_par[CODES ? GROUPS : 1][2][3][CODES ? kManyTokens : 4];   // codes, of two steps: scales of K, logarithms and reciprocals of those of V
     __shared__ float2 s_ml[GROUPS == 1 ? 1 : kManyRows];
     __shared__ OddTokens s_odd;
 
-    const int head = blockIdx.x % a.c.heads, tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int head = index % a.c.heads, tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const int n32 = lane & 31, hh = lane >> 5, D = a.c.head_dim;
     int seq, tile;
     Sequence sq;
-    if (!many_tile(a, blockIdx.x / a.c.heads, &seq, &tile, &sq)) return;
+    if (!many_tile(a, index / a.c.heads, &seq, &tile, &sq)) return;
     const int nrows = sq.tokens * a.group, R0 = tile * kManyRows;
     const int top = sq.seen((min(nrows, R0 + kManyRows) - 1) / a.group, a.causal);
-    const int per = part_tokens(top, a.many_parts, kManyTokens, kManyLeast), nparts = max(1, (top + per - 1) / per), part = blockIdx.y;
+    const int per = part_tokens(top, a.many_parts, kManyTokens, kManyLeast), nparts = max(1, (top + per - 1) / per);
     if (part >= nparts) return;
     const int from = part * per, to = min(top, from + per), all_steps = (to - from + kManyTokens - 1) / kManyTokens;
     const int steps = (all_steps - grp + GROUPS - 1) / GROUPS, rounds = (all_steps + GROUPS - 1) / GROUPS;   // this group's; the most of any group
@@ -884,30 +897,60 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArg
                 if (DP != D && at >= D) continue;
                 f4 v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
                 if (nparts > 1) {
-                    *reinterpret_cast<f4*>(a.part_o + (yrow * a.parts + part) * D + at) = v;
+                    *reinterpret_cast<f4*>(a.many_o + (a.many_part(yrow) + part) * D + at) = v;
                 } else {
                     if (l == 0.0f) v = f4{0, 0, 0, 0};
                     *reinterpret_cast<uint2*>(a.y + yrow * D + at) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
                 }
             }
-        if (nparts > 1 && hh == 0) a.part_ml[yrow * a.parts + part] = float2{m, l};
+        if (nparts > 1 && hh == 0) a.many_ml[a.many_part(yrow) + part] = float2{m, l};
     }
     if constexpr (!CODES) {
-        if (s_odd.any()) add_not_finite(a, sq, seq, head, R0, min(nrows, R0 + kManyRows), s_odd.first, s_odd.last, part, nparts);
+        if (s_odd.any()) add_not_finite(a, sq, seq, head, R0, min(nrows, R0 + kManyRows), s_odd.first, s_odd.last, [&](int, int64_t yrow) { return nparts > 1 ? a.many_o + (a.many_part(yrow) + part) * D : nullptr; });
     }
 }
 
-// ---- launches (one file per head size) --------------------------------------------------------------
+// ---- kernels and launches (one file per head size) ---------------------------------------------------
+template <int DP, bool CODES, int NR>
+__global__ __launch_bounds__(256) void attn_few_kernel(AttnArgs a)
+{
+    __shared__ __align__(16) uint16_t lds[kFewLds<DP, 4>];
+    attn_few<DP, CODES, NR, 4>(a, lds, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+template <int DP, bool CODES, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArgs a)
+{
+    __shared__ __align__(16) uint16_t lds[kManyLds<DP, CODES, GROUPS>];
+    attn_many<DP, CODES, GROUPS>(a, lds, blockIdx.x, blockIdx.y);
+}
+// Prompts beside single tokens: the workgroups of both parts in one launch, the longer ones (of many rows) first; one after the
+// other they would each leave the chip half empty (a chunk of 333 tokens and eight decoding requests: 24 + 9 us).
+template <int DP, bool CODES>
+__global__ __launch_bounds__(512, 2) void attn_both_kernel(AttnArgs a)
+{
+    __shared__ __align__(16) uint16_t lds[kManyLds<DP, CODES, 2> > kFewLds<DP, 8> ? kManyLds<DP, CODES, 2> : kFewLds<DP, 8>];
+    const unsigned many = a.many_wgs * a.many_parts;
+    if (blockIdx.x < many) {
+        attn_many<DP, CODES, 2>(a, lds, blockIdx.x % a.many_wgs, blockIdx.x / a.many_wgs);
+    } else {
+        const unsigned i = blockIdx.x - many, pair = i / a.few_parts;
+        attn_few<DP, CODES, 1, 8>(a, lds, pair % a.c.heads, pair / a.c.heads, i % a.few_parts);
+    }
+}
+
 template <int DP>
-void launch_attn_few(const AttnArgs& a, int nr, const dim3& grid, hipStream_t s);
+void launch_attn_few(const AttnArgs& a, int nr, hipStream_t s);
 template <int DP>
-void launch_attn_many(const AttnArgs& a, const dim3& grid, hipStream_t s);
+void launch_attn_many(const AttnArgs& a, hipStream_t s);
+template <int DP>
+void launch_attn_both(const AttnArgs& a, hipStream_t s);   // up to 128 columns, one tile of few rows
 
 #define ABQ_ATTN_INSTANTIATE(DP)                                                                                     \
     namespace abq {                                                                                                  \
     template <>                                                                                                      \
-    void launch_attn_few<DP>(const AttnArgs& a, int nr, const dim3& grid, hipStream_t s)                             \
+    void launch_attn_few<DP>(const AttnArgs& a, int nr, hipStream_t s)                                               \
     {                                                                                                                \
+        const dim3 grid(a.c.heads, a.b.seqs, a.few_parts);                                                           \
         if (a.c.kv_bits == 8) {                                                                                      \
             if (nr == 1) attn_few_kernel<DP, true, 1><<<grid, 256, 0, s>>>(a);                                       \
             else attn_few_kernel<DP, true, 2><<<grid, 256, 0, s>>>(a);                                               \
@@ -917,11 +960,22 @@ void launch_attn_many(const AttnArgs& a, const dim3& grid, hipStream_t s);
         }                                                                                                            \
     }                                                                                                                \
     template <>                                                                                                      \
-    void launch_attn_many<DP>(const AttnArgs& a, const dim3& grid, hipStream_t s)                                    \
+    void launch_attn_many<DP>(const AttnArgs& a, hipStream_t s)                                                      \
     {                                                                                                                \
         constexpr int G = DP > 128 ? 1 : 2; /* (two groups of the widest heads run out of registers) */                 \
+        const dim3 grid(a.many_wgs, a.many_parts);                                                                   \
         if (a.c.kv_bits == 8) attn_many_kernel<DP, true, G><<<grid, 256 * G, 0, s>>>(a);                             \
         else attn_many_kernel<DP, false, G><<<grid, 256 * G, 0, s>>>(a);                                             \
+    }                                                                                                                \
+    }
+#define ABQ_ATTN_INSTANTIATE_BOTH(DP)                                                                                \
+    namespace abq {                                                                                                  \
+    template <>                                                                                                      \
+    void launch_attn_both<DP>(const AttnArgs& a, hipStream_t s)                                                      \
+    {                                                                                                                \
+        const dim3 grid(a.many_wgs * a.many_parts + (unsigned)a.c.heads * a.b.seqs * a.few_parts);                   \
+        if (a.c.kv_bits == 8) attn_both_kernel<DP, true><<<grid, 512, 0, s>>>(a);                                    \
+        else attn_both_kernel<DP, false><<<grid, 512, 0, s>>>(a);                                                    \
     }                                                                                                                \
     }
 

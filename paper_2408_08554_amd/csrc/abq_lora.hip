@@ -367,15 +367,18 @@ __global__ __launch_bounds__(256, MT == 4 && FAST ? 2 : 1) void lora_expand_kern
 }
 
 // Tiles of rows that share a workgroup: many rows (prompts, whose tiles have one or few adapters) as many as the accumulators allow.
+// (Rank 16, 4096 to 4096, one tile against four: 160 rows of 2 adapters 9.7 and 12.3 us, of 64 adapters 14 and 31; 320 rows 15.1 and 12.4,
+// of 64 adapters 43 and 24.)
 static int lora_tiles(int M, int rank) { return M < 256 || rank > 128 ? 1 : rank > 64 ? 2 : 4; }
 
 // Parts of K, each a whole number of steps for four waves: few tiles of rows leave the chip idle and want many short parts, but the
-// second kernel adds them up once per workgroup.
+// second kernel adds them up once per workgroup.  (A workgroup to a compute unit: 160 rows 9.7 us, half as many 14.0, twice as many 8.9;
+// 2048 rows of rank 64, 5120 to 13824, half as many 53.6, 56.1, 58.3.)
 struct LoraPlan { int slice, parts; };
 static LoraPlan lora_plan(int M, int K, int rank)
 {
     const int each = 16 * lora_tiles(M, rank), tiles = (M + each - 1) / each, wgs = M < 256 ? tiles * std::min(M, 8) : tiles;   // (a tile of a few requests has as many adapters)
-    const int want = std::max(1, std::min({(M < 256 ? 256 : 512) / std::max(wgs, 1), (K + 255) / 256, 16}));
+    const int want = std::max(1, std::min({256 / wgs, (K + 255) / 256, 16}));
     LoraPlan p;
     p.slice = ((K + want - 1) / want + 127) / 128 * 128;
     p.parts = (K + p.slice - 1) / p.slice;
@@ -408,9 +411,12 @@ static void launch_lora(int M, int N, int K, int rank, int adapters, const uint1
     };
     if (lora_split(M)) {
         lora_split_kernel<<<(M + 3) / 4, 256, 0, s>>>(M, rank, 16 * RT, adapters, p.parts, ids, scale, u, halves, factors);
-        const int blocks = columns * tiles >= 8192 ? 4 : 1;
+        // two blocks a wave where that leaves two workgroups to a compute unit (4096 rows, rank 64, 11008 columns: 79 us, with one 84, with
+        // four 92; 1024 rows, 4096 columns: 29 us, with one 26), but not with shorter tiles (rank 128, 2048 rows: 100 us, with one 94)
+        const int blocks = MT == 4 && columns * tiles >= 4096 ? 2 : 1;
         expand(!fast ? lora_expand_kernel<RT, MT, false, false, true> : lora_expand_kernel<RT, MT, false, true, true>, (unsigned)((columns + 4 * blocks - 1) / (4 * blocks)), blocks);
     } else if constexpr (MT == 1) {
+        // (16 rows of as many adapters, rank 64: 18 us, 38 with the adapters one after the other; two adapters in 160 rows: 9.7 and 9.3)
         if (M > 1 && adapters > 1) expand(!fast ? lora_expand_kernel<RT, 1, true, false, false> : lora_expand_kernel<RT, 1, true, true, false>, (unsigned)columns, 1);
         else expand(!fast ? lora_expand_kernel<RT, 1, false, false, false> : lora_expand_kernel<RT, 1, false, true, false>, (unsigned)((columns + 3) / 4), 1);
     }

@@ -61,6 +61,21 @@ def test_long_contexts(abq, bits, past):
     check(abq, Paged([(2, past), (1, 7)], 8, 2, 64, 64, bits, seed=past + 1))
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 128, 144])
+def test_chunks_over_long_contexts(abq, bits, dim):
+    check(abq, Paged([(70, 1500)], 2, 2, dim, 16, bits, seed=dim))      # in three parts, in ten
+    check(abq, Paged([(40, 5000), (1, 900), (0, 3)], 4, 2, dim, 32, bits, seed=dim + 1))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 128, 144])
+def test_long_contexts_in_one_part(abq, bits, dim):
+    """So many workgroups that nothing is shared out: each goes over more pages than it holds the numbers of."""
+    check(abq, Paged([(33, 4000)] + [(33, 0)] * 63 + [(1, 9000)], 4, 4, dim, 16, bits, seed=dim, extra_rows=1))
+    check(abq, Paged([(1, 5000)] + [(1, 3)] * 63, 16, 16, dim if dim > 128 else dim // 4, 16, bits, seed=dim + 1))
+
+
 @pytest.mark.parametrize("page", [16, 32, 256, 4096])
 def test_page_sizes(abq, page):
     check(abq, Paged([(40, 90), (1, 30)], 2, 2, 64, page, seed=page))
