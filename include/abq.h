@@ -384,7 +384,7 @@ typedef struct abq_kv_cache {
  *   row_start [seqs+1] int32, ascending from 0;  lens [seqs] int32: tokens of each sequence, the new ones among them
  *   pages     [seqs][max_pages] int32: token t of sequence s lies in page pages[s][t / page_size], at offset t % page_size
  *   max_new   no sequence has more rows in this step;  max_len: no sequence has more tokens.  They size the launches
- *             (abq_attn_paged): close bounds are faster ones.  1 <= max_new <= rows, 1 <= max_len.
+ *             (abq_attn_paged): close bounds are faster ones.  1 <= max_new <= rows <= 2^22, 1 <= seqs <= 65535, 1 <= max_len.
  * The arrays are device memory and never checked on the host.  Whatever they hold, nothing outside the tensors is read or
  * written: rows behind row_start[seqs] are left as they were; a page number outside 0..num_pages-1 (-1, say) is a page
  * that is not there - nothing is appended to it and attention does not see its tokens; tokens beyond max_pages pages and
@@ -401,7 +401,7 @@ typedef struct abq_batch {
  * (x[2j], x[2j+1]).  The angle is formed and reduced in binary64 (positions are exact however far), sine and cosine are
  * within 2^-23, products and sum in binary32, one rounding to binary16.  A cache of codes quantizes the rotated binary16
  * vector.
- *   heads_q    query heads (with q), a multiple of cache->heads, rows * heads_q <= 2^30;  rotary_dim a multiple of 16, 0..head_dim
+ *   heads_q    query heads (with q), a multiple of cache->heads, rows * heads_q <= 2^28, seqs * heads <= 2^21;  rotary_dim a multiple of 16, 0..head_dim
  *   q [rows][heads_q * head_dim] (NULL to skip), k, v [rows][heads * head_dim] with row strides ldq, ldk, ldv in elements
  *   inv_freq   [rotary_dim / 2] float
  *   q_out      [rows][heads_q * head_dim], contiguous; it may be q itself where that is contiguous too
@@ -413,7 +413,8 @@ int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q
 
 /* Reads vectors back out of the cache (exporting a prefix, checks): for each slot = page * page_size + offset the keys and
  * values of all heads as binary16, codes as half_rne(scale * (code - zero)).  A slot outside the cache reads as zeros.
- *   slots [count] int32 (device);  k_out, v_out [count][heads * head_dim];  page numbers up to INT32_MAX / page_size */
+ *   slots [count] int32 (device);  k_out, v_out [count][heads * head_dim];  page numbers up to INT32_MAX / page_size,
+ *   count <= 2^22 */
 int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint16_t* k_out, uint16_t* v_out, void* stream);
 
 /* Attention of the rows over what the cache holds of their sequences (the new tokens' keys and values among it: append
@@ -423,6 +424,7 @@ int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint
  * Scores, running maximum, sums and the weighted sum are binary32; the weights are rounded to binary16 for the product with
  * the values.  What lies in pages beyond a sequence's length, or in tokens that a row does not see, does not reach its output
  * (NaN and infinities included).
+ *   heads_q    as for abq_kv_append
  *   q [rows][heads_q * head_dim], row stride ldq;  y [rows][heads_q * head_dim], contiguous, not overlapping q
  *   workspace  at least abq_attn_paged_workspace_bytes(cache, batch, heads_q) bytes (may be 0): the parts of long sequences
  *              that several workgroups share.  Contents on entry are irrelevant; calls that may overlap need one each.
@@ -435,7 +437,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
  *   out[m,:] = half_rne( y[m,:] + scale[i] * B_i (A_i x[m,:]) ),  i = ids[m];   out[m,:] = y[m,:] where ids[m] is outside 0..adapters-1
  * x is the projection's input before quantization (y_fp16_out of the producers above), y its output.  A_i x is summed in
  * binary32 and enters the second product with 21 bits or more of its row's largest element.
- *   rank       1..256 (pad smaller adapters of a pool with zeros);  1 <= M <= 2^19, N >= 1, 1 <= K <= ABQ_MAX_K
+ *   rank       1..256 (pad smaller adapters of a pool with zeros);  1 <= M <= 2^19, 1 <= N <= 2^28, 1 <= K <= ABQ_MAX_K
  *   x [M][K] row stride ldx;  ids [M] int32 (device);  a [adapters][rank][K], b [adapters][N][rank] binary16;
  *   scale [adapters] float;  y [M][N] row stride ldy;  out [M][N] row stride ldout: y itself (same stride), or no overlap
  *   (strides in elements, any value >= K or N)

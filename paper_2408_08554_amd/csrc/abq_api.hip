@@ -881,15 +881,17 @@ static int check_cache(const abq_kv_cache* c)
 static int check_batch(const abq_batch* b)
 {
     if (!b || !b->row_start || !b->lens || !b->pages) return ABQ_ERR_NULL;
-    if (b->rows < 1 || b->seqs < 1 || b->seqs > 65535 || b->max_pages < 1 || b->max_new < 1 || b->max_new > b->rows || b->max_len < 1) return ABQ_ERR_SHAPE;
+    if (b->rows < 1 || b->rows > (1 << 22) || b->seqs < 1 || b->seqs > 65535 || b->max_pages < 1 || b->max_new < 1 || b->max_new > b->rows || b->max_len < 1) return ABQ_ERR_SHAPE;
     if (misaligned(b->row_start) || misaligned(b->lens) || misaligned(b->pages)) return ABQ_ERR_ALIGN;
     return ABQ_OK;
 }
 
-// Query heads: a multiple of the cache's, rows that stay below 2^20 elements, and at most 2^30 of all rows.
+// Query heads: a multiple of the cache's, rows that stay below 2^20 elements, and at most 2^28 of all rows; with at most 2^21 heads of
+// all sequences an attention launch has fewer than 2^23 workgroups of 512, which is what a launch can have.
 static int check_heads_q(const abq_kv_cache* c, const abq_batch* b, int heads_q)
 {
-    return heads_q < 1 || heads_q % c->heads != 0 || (int64_t)heads_q * c->head_dim >= (1 << 20) || (int64_t)b->rows * heads_q > (1 << 30) ? ABQ_ERR_SHAPE : ABQ_OK;
+    return heads_q < 1 || heads_q % c->heads != 0 || (int64_t)heads_q * c->head_dim >= (1 << 20) || (int64_t)b->rows * heads_q > (1 << 28) ||
+           (int64_t)b->seqs * c->heads > (1 << 21) ? ABQ_ERR_SHAPE : ABQ_OK;
 }
 
 int abq_kv_append(const abq_kv_cache* cache, const abq_batch* batch, int heads_q, int rotary_dim, int interleaved, const float* inv_freq,
@@ -914,7 +916,7 @@ int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint
 {
     if (!slots || !k_out || !v_out) return ABQ_ERR_NULL;
     if (int e = check_cache(cache)) return e;
-    if (count < 1) return ABQ_ERR_SHAPE;
+    if (count < 1 || count > (1 << 22)) return ABQ_ERR_SHAPE;
     if (misaligned(slots) || misaligned(k_out) || misaligned(v_out)) return ABQ_ERR_ALIGN;
     return hip_status(launch_kv_read(*cache, count, slots, k_out, v_out, (hipStream_t)stream));
 }
@@ -942,7 +944,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
 
 static int check_lora_shape(int M, int N, int K, int rank)
 {
-    return M < 1 || M > (1 << 19) || N < 1 || K < 1 || K > ABQ_MAX_K || rank < 1 || rank > 256 ? ABQ_ERR_SHAPE : ABQ_OK;
+    return M < 1 || M > (1 << 19) || N < 1 || N > (1 << 28) || K < 1 || K > ABQ_MAX_K || rank < 1 || rank > 256 ? ABQ_ERR_SHAPE : ABQ_OK;
 }
 
 size_t abq_lora_add_workspace_bytes(int M, int N, int K, int rank)

@@ -135,8 +135,6 @@ hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int head
                              uint16_t* y, void* workspace, hipStream_t s)
 {
     const AttnPlan p = attn_plan(c, b, heads_q);
-    const int64_t few_wgs = (int64_t)c.heads * b.seqs * p.few_parts;
-    if (p.many_wgs * p.many_parts + few_wgs > INT32_MAX) return hipErrorInvalidConfiguration;
     AttnArgs a{};
     a.c = c;
     a.b = b;

@@ -137,6 +137,18 @@ def test_the_module_refuses_what_is_no_operand():
         B.abq_lora_add(half(1).expand(1, (1 << 32) + 16), i32(4), half(2, 8, 8), half(2, 8, 8), torch.zeros(2), half(4, 8))
 
 
+def test_launches_that_no_grid_can_have():
+    """Sizes that a tensor could still have, but whose threads would pass 2^32 in one launch."""
+    wide, most = dict(heads=1 << 15, head_dim=16), dict(rows=1 << 22, max_new=1)
+    assert append(cache(), batch(rows=(1 << 22) + 1)) == attend(cache(), batch(rows=(1 << 22) + 1)) == B.ABQ_ERR_SHAPE
+    assert append(cache(**wide), batch(**most), heads_q=1 << 15, ldq=1 << 19, ldk=1 << 19, ldv=1 << 19) == B.ABQ_ERR_SHAPE
+    assert attend(cache(**wide), batch(**most), heads_q=1 << 15, ldq=1 << 19) == B.ABQ_ERR_SHAPE
+    assert attend(cache(**wide), batch(rows=100, seqs=65), heads_q=1 << 15, ldq=1 << 19) == B.ABQ_ERR_SHAPE
+    assert read(cache(), count=(1 << 22) + 1) == B.ABQ_ERR_SHAPE
+    assert B.load().abq_lora_add(*{**GOOD, "N": (1 << 28) + 1, "ldy": 1 << 29, "ldout": 1 << 29}.values(), None) == B.ABQ_ERR_SHAPE
+    assert B.abq_lora_add_workspace_bytes(4, (1 << 28) + 1, 60, 8) == 0
+
+
 @pytest.mark.gpu
 def test_the_module_refuses_operands_that_do_not_fit(abq):
     """Types, shapes, layouts on the device: refused before anything is launched."""
