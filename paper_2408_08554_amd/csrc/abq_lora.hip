@@ -178,8 +178,8 @@ __global__ __launch_bounds__(256) void lora_split_kernel(int M, int rank, int pa
 }
 
 // The rows of the output.  A workgroup: MT tiles of sixteen rows; its waves take blocks of 64 columns, `blocks` each (SPREAD: one block
-// for all four, and every fourth adapter each).  The rows of B are dealt to the operand's rows so that a lane ends with sixteen
-// neighbouring columns of one row.  FAST: a rank of whole eights, columns of whole blocks; the branches that the others need for their
+// for all four, and every fourth adapter each).  The rows of B are dealt to the operand's rows so that a lane ends with twice eight
+// neighbouring columns of one row, and four lanes with twice 32.  FAST: a rank of whole eights, columns of whole blocks; the branches that the others need for their
 // ends cost a third of the time.  SPLIT: u comes split, else in parts.
 template <int RT, int MT, bool SPREAD, bool FAST, bool SPLIT>
 __global__ __launch_bounds__(256, MT == 4 && FAST ? 2 : 1) void lora_expand_kernel(int M, int N, int rank, int adapters, int parts, int blocks, const int32_t* __restrict__ ids, const uint16_t* __restrict__ b,
@@ -197,16 +197,16 @@ __global__ __launch_bounds__(256, MT == 4 && FAST ? 2 : 1) void lora_expand_kern
     // y of the first block, on its way early
     lu4 yv[MT][2];
     auto load_y = [&](int at) {
-        const int n = at + 16 * g;
+        const int n = at + 8 * g;
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
             const uint16_t* const yr = y + (size_t)min(m0 + 16 * j + n16, M - 1) * ldy;
             if (FAST || at + 64 <= N) {
                 yv[j][0] = load_whole(yr + n);
-                yv[j][1] = load_whole(yr + n + 8);
+                yv[j][1] = load_whole(yr + n + 32);
             } else {
                 yv[j][0] = load_eight(yr, n, N);
-                yv[j][1] = load_eight(yr, n + 8, N);
+                yv[j][1] = load_eight(yr, n + 32, N);
             }
         }
     };
@@ -264,21 +264,21 @@ __global__ __launch_bounds__(256, MT == 4 && FAST ? 2 : 1) void lora_expand_kern
     const uint16_t* const mine = us + n16 * US + (g < 2 ? 0 : RP) + 8 * (g & 1);
 
     for (int blk = 0; blk < blocks; ++blk) {
-        const int at = n0 + blk * 256, n = at + 16 * g;
+        const int at = n0 + blk * 256, n = at + 8 * g;
         if (at >= N) return;
         if (blk) load_y(at);
         auto store = [&](int j) {
             uint16_t* const dst = out + (size_t)(m0 + 16 * j + n16) * ldout;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if constexpr (FAST) *reinterpret_cast<u32x4_half*>(dst + n + 8 * h) = u32x4_half{yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]};
-                else if (n + 8 * h < N) store_row_part8(dst + n + 8 * h, n + 8 * h, N, yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]);
+                if constexpr (FAST) *reinterpret_cast<u32x4_half*>(dst + n + 32 * h) = u32x4_half{yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]};
+                else if (n + 32 * h < N) store_row_part8(dst + n + 32 * h, n + 32 * h, N, yv[j][h][0], yv[j][h][1], yv[j][h][2], yv[j][h][3]);
             }
         };
-        // operand row n16 of tile t: column at + 16 (n16 / 4) + 4 t + n16 % 4
+        // operand row n16 of tile t: column at + 32 (t / 2) + 8 (n16 / 4) + 4 (t % 2) + n16 % 4
         int nb[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) nb[t] = min(at + 16 * (n16 >> 2) + 4 * t + (n16 & 3), N - 1);
+        for (int t = 0; t < 4; ++t) nb[t] = min(at + 32 * (t >> 1) + 8 * (n16 >> 2) + 4 * (t & 1) + (n16 & 3), N - 1);
         auto load = [&](int i, int rt, lu4* v) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
