@@ -24,15 +24,17 @@ template <>
 void launch_attn_both<128>(const AttnArgs&, hipStream_t);
 
 // The parts of a row and head that was shared out as one.  What bounds it is latency (sequence, maxima and sums, parts: three
-// dependent loads), so WAVES waves of a workgroup take the parts in turn, four at a time (few parts: a wave for each of four heads); a
-// wave holds up to 64 parts' maxima and sums in its lanes.
-template <int WAVES>
+// dependent loads).  LP lanes take a row and head, four columns each, and hold its parts' maxima and sums, one each.  WAVES = 4:
+// many parts, which the waves of a workgroup take in turn, four at a time; else a workgroup has 256 / LP heads, and a wave one of
+// up to 64 / LP of them.  (341 rows, 32 heads of 128 in up to two parts: 5.9 us, 9.4 with a wave for each head.)
+template <int WAVES, int LP>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
 {
+    static_assert(WAVES == 1 || LP == 64);
     __shared__ __align__(16) f4 s_o[WAVES][64];
-    const int lane = threadIdx.x & 63, nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = WAVES == 4 ? nth : 0, D = a.c.head_dim;
-    const int row = blockIdx.x, hq = WAVES == 4 ? blockIdx.y : 4 * blockIdx.y + nth;
-    if (hq >= a.heads_q) return;
+    const int lane = threadIdx.x & 63, wave = WAVES == 4 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, D = a.c.head_dim;
+    const int sl = lane & (LP - 1), group0 = lane & ~(LP - 1);
+    const int row = blockIdx.x, hq = WAVES == 4 ? blockIdx.y : blockIdx.y * (256 / LP) + threadIdx.x / LP;
     int seq = 0;
     for (int s0 = 0; s0 < a.b.seqs; s0 += 64) {
         const int s = s0 + lane;
@@ -47,29 +49,32 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
     const int last = few ? nrows : min(nrows, ((i * a.group + hq % a.group) / kManyRows + 1) * kManyRows);
     const int top = sq.seen((last - 1) / a.group, a.causal);
     const int per = few ? part_tokens(top, a.few_parts, kFewTokens, kFewLeast) : part_tokens(top, a.many_parts, kManyTokens, kManyLeast);
-    const int nparts = (top + per - 1) / per;
-    if (nparts <= 1) return;   // (written by its workgroup)
+    int nparts = (top + per - 1) / per;
+    if (nparts <= 1 || hq >= a.heads_q) nparts = 0;   // (written by its workgroup)
+    if (!any(nparts != 0)) return;
     const int64_t yrow = (int64_t)row * a.heads_q + hq;
     const int64_t place = few ? a.few_part(seq, hq / a.group, i * a.group + hq % a.group) : a.many_part(yrow);
-    const float* const o = (few ? a.few_o : a.many_o) + place * D + 4 * lane;
-    const float2 ml = lane < nparts ? (few ? a.few_ml : a.many_ml)[place + lane] : float2{kFloor, 0.0f};
-    const bool mine = 4 * lane < D;
+    const float* const o = (few ? a.few_o : a.many_o) + place * D + 4 * sl;
+    const float2 ml = sl < nparts ? (few ? a.few_ml : a.many_ml)[place + sl] : float2{kFloor, 0.0f};
+    const bool mine = 4 * sl < D;
     // this wave's parts: its first four are on their way before their weights are known
     f4 x[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) x[u] = mine && wave + WAVES * u < nparts ? *reinterpret_cast<const f4*>(o + (int64_t)(wave + WAVES * u) * D) : f4{0, 0, 0, 0};
     float m = ml.x;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    for (int off = LP / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     const float f = __builtin_amdgcn_exp2f(ml.x - m);
     float l = f * ml.y;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
+    for (int off = LP / 2; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
     f4 v = {0, 0, 0, 0};
-    for (int p0 = wave; p0 < nparts; p0 += 4 * WAVES) {
+    for (int p0 = wave; any(p0 < nparts); p0 += 4 * WAVES) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (p0 + WAVES * u < nparts) v += __shfl(f, p0 + WAVES * u, 64) * x[u];
+        for (int u = 0; u < 4; ++u) {
+            const float w = __shfl(f, (group0 + p0 + WAVES * u) & 63, 64);
+            if (p0 + WAVES * u < nparts) v += w * x[u];
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (mine && p0 + WAVES * (4 + u) < nparts) x[u] = *reinterpret_cast<const f4*>(o + (int64_t)(p0 + WAVES * (4 + u)) * D);
@@ -80,10 +85,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
         if (wave != 0) return;
         v = s_o[0][lane] + s_o[1][lane] + (s_o[2][lane] + s_o[3][lane]);
     }
-    if (!mine) return;
+    if (!mine || nparts == 0) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (l == 0.0f) v = f4{0, 0, 0, 0};
-    *reinterpret_cast<uint2*>(a.y + yrow * D + 4 * lane) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+    *reinterpret_cast<uint2*>(a.y + yrow * D + 4 * sl) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
 }
 
 // Which kernels a step needs, and into how many parts sequences are cut at most; from the sizes that the host knows alone, so that a
@@ -112,13 +117,13 @@ static AttnPlan attn_plan(const abq_kv_cache& c, const abq_batch& b, int heads_q
     // have one.  More parts balance better but have to be joined (us at 256, 512, 1024 workgroups; heads of 128: 32 sequences of 2048 on
     // 8 heads 41, 47, 47, 8 of 1000 on 32 21, 25, 26, 40 of 2048 on 8 62, 62, 59; codes, 4 of 32768 on 8 58, 50, 54; a prompt of 333
     // with eight decoding requests at 128 and 256: 30, 33).
-    if (p.few) {
+    if (p.few && !stays_whole(tokens, kFewLeast)) {
         const int64_t wgs = (int64_t)b.seqs * c.heads, want = p.both ? 128 : c.kv_bits == 8 ? 512 : 256;
         p.few_parts = (int)std::min<int64_t>({(want + wgs - 1) / wgs, (tokens + kFewLeast - 1) / kFewLeast, 64});
     }
     if (most > p.few) {   // a workgroup to a compute unit (256 tokens over 4096, 8 heads: 37 us; of two, 47)
         p.many_wgs = (all / kManyRows + std::min<int64_t>(b.seqs, all / (p.few + 1))) * c.heads;
-        p.many_parts = (int)std::min<int64_t>({(256 + p.many_wgs - 1) / p.many_wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
+        if (!stays_whole(tokens, kManyLeast)) p.many_parts = (int)std::min<int64_t>({(256 + p.many_wgs - 1) / p.many_wgs, (tokens + kManyLeast - 1) / kManyLeast, 32});
     }
     p.few_places = p.few_parts > 1 ? (size_t)b.seqs * c.heads * p.few_rows * p.few_parts : 0;
     p.many_places = p.many_parts > 1 ? (size_t)b.rows * heads_q * p.many_parts : 0;
@@ -162,10 +167,12 @@ hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int head
         if (p.few) c.head_dim <= 64 ? launch_attn_few<64>(a, p.nr, s) : c.head_dim <= 128 ? launch_attn_few<128>(a, p.nr, s) : launch_attn_few<256>(a, p.nr, s);
     }
     const int parts = std::max(p.few_parts, p.many_parts);
-    // (A prompt's rows fill the chip with a wave for each head; where a few rows have many parts, four waves share one.  One request of
-    // 32000 tokens: 44 us with one, 29 with four; a prompt of 256 over 4096 in up to eight parts: 37 and 49.)
-    if (parts > 8) attn_join_kernel<4><<<dim3(b.rows, heads_q), 256, 0, s>>>(a);
-    else if (parts > 1) attn_join_kernel<1><<<dim3(b.rows, (heads_q + 3) / 4), 256, 0, s>>>(a);
+    // (A prompt's rows fill the chip with less than a wave for each head; where a few rows have many parts, four waves share one.  One
+    // request of 32000 tokens: 44 us with one, 29 with four; a prompt of 256 over 4096 in up to eight parts: 37 and 49.)
+    if (parts > 8) attn_join_kernel<4, 64><<<dim3(b.rows, heads_q), 256, 0, s>>>(a);
+    else if (parts > 1 && c.head_dim <= 64) attn_join_kernel<1, 16><<<dim3(b.rows, (heads_q + 15) / 16), 256, 0, s>>>(a);
+    else if (parts > 1 && c.head_dim <= 128) attn_join_kernel<1, 32><<<dim3(b.rows, (heads_q + 7) / 8), 256, 0, s>>>(a);
+    else if (parts > 1) attn_join_kernel<1, 64><<<dim3(b.rows, (heads_q + 3) / 4), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -28,7 +28,9 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kManyRows = 128;    // rows of a workgroup of the kernel for many rows
 constexpr int kManyTokens = 64;   // tokens of one of its steps
 constexpr int kFewTokens = 32;    // tokens of a wave's step of the kernel for few rows
-constexpr int kFewLeast = 256, kManyLeast = 512;   // tokens of a part at least, where a sequence is shared out
+// Tokens of a part at least, where a sequence is shared out.  (Many rows at 384, 512, 768: 64 over 1000, 8 key heads, 20, 21, 25 us, 256 over
+// 1000 27, 27, 29.5, a prompt of 512 20, 16, 16.)
+constexpr int kFewLeast = 256, kManyLeast = 512;
 
 struct AttnArgs {
     abq_kv_cache c;
@@ -70,12 +72,14 @@ struct Sequence {
     }
 };
 
-// Tokens of one part of `top` when up to `parts` share them, in whole steps, at least `least`; the number of parts is then what covers
-// top.  (Up to half as much again stays whole: joining costs as much as two steps of a lone workgroup.  One token, 32 heads, context
-// of 400: 9.9 us whole, 11.2 in two parts; of 512: 12.9 whole, 10.7 in three.)
-__host__ __device__ __forceinline__ int part_tokens(int top, int parts, int step, int least)
+// Up to half as much again as the least tokens of a part stay whole: joining costs as much as two steps of a lone workgroup.  (One
+// token, 32 heads, context of 400: 9.9 us whole, 11.2 in two parts; of 512: 12.9 whole, 10.7 in three.  A prompt of 700 on 8 key heads:
+// 19.0 whole, 22.6 where parts are launched.)
+__host__ __device__ __forceinline__ bool stays_whole(int top, int least) { return top <= least + least / 2; }
+// Tokens of one part of `top` when up to `parts` share them, in whole steps, at least `least`; the number of parts is then what covers top.
+__device__ __forceinline__ int part_tokens(int top, int parts, int step, int least)
 {
-    if (top <= least + least / 2) return max(top, 1);
+    if (stays_whole(top, least)) return max(top, 1);
     const int per = (int)(((int64_t)top + parts - 1) / parts);
     return (max(per, least) + step - 1) / step * step;
 }
@@ -924,7 +928,7 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_many_kernel(AttnArg
     attn_many<DP, CODES, GROUPS>(a, lds, blockIdx.x, blockIdx.y);
 }
 // Prompts beside single tokens: the workgroups of both parts in one launch, the longer ones (of many rows) first; one after the
-// other they would each leave the chip half empty (a chunk of 333 tokens and eight decoding requests: 24 + 9 us).
+// other they would each leave the chip half empty (a chunk of 333 tokens and eight decoding requests: 24 us together, 24 + 9 in two launches).
 template <int DP, bool CODES>
 __global__ __launch_bounds__(512, 2) void attn_both_kernel(AttnArgs a)
 {
