@@ -487,8 +487,9 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t* p) { return (uin
 // half a step behind the first, so that of the two waves of a SIMD one has matrix and the other vector work.  Each group has two
 // buffers for K and two for V, of steps in turn; binary16 goes into them straight from memory, the next but one while this is used.
 // What bounds it: of a step's 3400 clocks the matrix half takes 1500 and the rest 1900 (1150 of them softmax),
-// which the other group's matrix half hides all but 400 of.  1024 tokens over 15360, 32 heads on 8 of 128: 275 us (969 TFLOP/s; one group alone 370), as codes 354 (750);
-// a prompt of 2048, 32 heads on 8: 53 us (645, its causal edge and 256 tiles for 256 units included).
+// which the other group's matrix half hides all but 400 of.  1024 tokens over 15360, 32 heads on 8 of 128: 275 us (969 TFLOP/s; one
+// group alone 370), as codes 354 (750);
+// a prompt of 2048, 32 heads: 53 us (650: two workgroups a unit, one after the other, each with its start and end).
 template <int DP, bool CODES, int GROUPS>
 constexpr int kManyLds = GROUPS * 2 * kManyTokens * (CODES ? 2 * DP + 40 : 2 * DP);   // halves
 template <int DP, bool CODES, int GROUPS>

@@ -5,9 +5,9 @@
 // the rows, and a row takes the result of its own adapter alone (the others' are discarded lane by lane, not multiplied by zero, so that
 // an infinity in one request's adapter stays there).
 //
-// What bounds it: one token is latency (two launches and what each waits for: rank 16, 4096 to 4096, 3.2 + 4.3 us); 64 rows of 32
-// adapters too, though less (rank 16, 4096 to 11008: 18.8 MB in 4.7 + 7.2 us, 1.6 TB/s); a prompt is reading and writing y, at half the
-// rate of a copy (2048 rows, rank 64, 5120 to 13824: 113 MB of y in 33 of 51 us, the rest u): a workgroup's waves wait for ids, u and B
+// What bounds it: one token is latency (two launches and what each waits for: rank 16, 4096 to 4096, 3.3 + 4.1 us); 64 rows of 32
+// adapters too, though less (rank 16, 4096 to 11008: 18.8 MB in 5.3 + 7.7 us, 1.4 TB/s); a prompt is reading and writing y, at 3 TB/s
+// (2048 rows, rank 64, 5120 to 13824: 113 MB of y in 37 us, u in 12 + 4): a workgroup's waves wait for ids, u and B
 // before their y can leave, and the accumulators of 64 x 64 leave room for two of them on a unit.
 #include "abq_kv.h"
 #include "abq_rows.h"
