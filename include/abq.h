@@ -365,6 +365,7 @@ int abq_gemm_grouped(int p, int q, int M, int count, const abq_problem* host_pro
  * ((page * heads + head) * page_size + offset) * head_dim elements.
  *   kv_bits    16: binary16 values.  8: codes 0..255 (one byte each) with a scale and a zero-point per vector, the
  *              quantizer of abq_quant_pack_act with q = 8 on the binary16 vector; value = scale * (code - zero), scale > 0.
+ *              (A vector of zeros has scale 2^-32: attention keeps what is 2^-24 of the largest weight times scale of V.)
  *   page_size  tokens per page: a power of two, 16..4096;  head_dim a multiple of 16, 16..256;  num_pages, heads >= 1,
  *              heads * head_dim < 2^20
  *   k, v       [num_pages][heads][page_size][head_dim] binary16 or uint8

@@ -138,7 +138,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a)
             }
             const TokenQuantizer tq(lo, hi, 255);
             if (lane == 0) {
-                (is_v ? a.c.v_scale : a.c.k_scale)[vec] = tq.delta;
+                // (zeros take the quantizer's smallest scale: attention's weights carry the scale of V into binary16, where a token that
+                // adds nothing must not push out the others)
+                (is_v ? a.c.v_scale : a.c.k_scale)[vec] = hi == lo ? 0x1p-32f : tq.delta;
                 (is_v ? a.c.v_zero : a.c.k_zero)[vec] = (uint8_t)tq.z;
             }
             if (inside) {

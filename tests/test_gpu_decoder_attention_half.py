@@ -129,3 +129,20 @@ def test_a_decoding_step_as_a_graph(abq):
         torch.cuda.synchronize()
         assert torch.equal(y, want), i
         assert all(torch.equal(a, b) for a, b in zip(*caches)), i
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_codes_of_a_token_whose_values_are_zero(abq, n):
+    """Such a token, looked at most of all, leaves the others' small values their digits: it is held with the smallest scale."""
+    p = Paged([(200, 0)], 4, 2, 64, 16, bits=8, seed=n)
+    cache, (starts, lens, pages), _ = p.device()
+    k, v = p.normal(200, 128), p.normal(200, 128) * 0.01
+    q = p.normal(200, 256)
+    k[7], v[7] = q[199, :64].repeat(2) * 0.5, 0.0
+    abq.abq_kv_append(cache, (starts, lens, pages), k.cuda(), v.cuda())
+    p.cache = [t.cpu() for t in cache]
+    assert (p.cache[4][int(p.pages[0, 0]), :, 7] == 2.0 ** -32).all() and (p.cache[1][int(p.pages[0, 0]), :, 7] == 0).all()
+    p.news, p.rows, p.row_start, p.q = [n], n, torch.tensor([0, n], dtype=torch.int32), q[200 - n:]
+    y = abq.abq_attn_paged(cache, (p.row_start.cuda(), lens, pages), p.q.cuda(), 0.125).cpu().view(n, 4, 64).double()
+    want, bound = p.attention(0.125)
+    assert ((y - want).abs() <= bound).all() and bound.max() < 2.0 ** -10   # (values of up to 2^-4)
