@@ -164,6 +164,10 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
     }
 }
 
+// Columns of the DP that a kernel goes over which every head that comes to it has.
+template <int DP>
+constexpr int kSureColumns = DP == 64 ? 16 : DP / 2 + 16;
+
 constexpr float kFloor = -1e30f;   // m of a row that has seen nothing: any score passes it, and 2^(floor - m) is 0
 
 // ---- few rows ------------------------------------------------------------------------------------
@@ -253,7 +257,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
 #pragma unroll
             for (int u = 0; u < KV; ++u) {
                 int d = CODES ? 64 * u + 16 * g : 32 * u + 8 * g;
-                if (d >= D) d = 0;   // (the queries are zero there)
+                if (d >= D) d = 0;   // (codes: the queries are zero there)
                 kr[j][u] = *reinterpret_cast<const u4*>((const uint8_t*)a.c.k + ((vec[j] + n16) * D + d) * (CODES ? 1 : 2));
             }
             if constexpr (CODES) {
@@ -319,8 +323,10 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
 #pragma unroll
                         for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w[e]), qv[t][2 * u + e], s[t][j], 0, 0, 0);
                 } else {
+                    u4 k = kr[j][u];
+                    if (32 * u + 32 > kSureColumns<DP> && 32 * u + 8 * g >= D) k = u4{0, 0, 0, 0};   // (zero queries do not rid the sum of an infinity)
 #pragma unroll
-                    for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kr[j][u]), qv[t][u], s[t][j], 0, 0, 0);
+                    for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, k), qv[t][u], s[t][j], 0, 0, 0);
                 }
             }
         }
@@ -574,7 +580,7 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
     for (int u = 0; u < LV; ++u) {
         const int r = u * TPL + lane / LPT;
         int dk = ((lane % LPT) ^ turn_k(r)) * (CODES ? 16 : 8), dv = ((lane % LPT) ^ turn_v(r)) * (CODES ? 16 : 8);
-        if (dk >= D) dk = 0;   // (the queries are zero there, and the columns of V are not stored)
+        if (dk >= D) dk = 0;   // (K: left out of the product, or of codes against zero queries; V: columns that are not stored)
         if (dv >= D) dv = 0;
         const uint32_t less = DIRECT ? kBias - 1024u * (u & 3) : 0u;
         place_k[u] = (uint32_t)(r * D + dk) * BYTES + less;
@@ -725,7 +731,15 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                if constexpr (S) s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[st & 1][k], qv[st], st ? s[k] : f16{}, 0, 0, 0);
+                if constexpr (S) {
+                    // Binary16: zero queries do not rid the sum of an infinity in the columns behind the head.  The product stops there; of the
+                    // widest heads, which have no register for what a branch keeps apart, it goes over zeros.  (1024 tokens over 15360, 32 heads
+                    // on 8: of 80, 255 us with all columns, 239 so, 256 over zeros; of 256, 581 with all columns, 582 so, 991 with the branch.)
+                    const bool behind = !CODES && 16 * st >= kSureColumns<DP> && 16 * st >= D;
+                    u4 kv = __builtin_bit_cast(u4, ko[st & 1][k]);
+                    if (GROUPS == 1 && behind) kv = u4{0, 0, 0, 0};
+                    if (GROUPS == 1 || !behind) s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, kv), qv[st], st ? s[k] : f16{}, 0, 0, 0);
+                }
                 if constexpr (V) o[(2 * st + k) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vo[st & 1][k], w[(2 * st + k) / DT], o[(2 * st + k) % DT], 0, 0, 0);
             }
         }
