@@ -169,6 +169,10 @@ template <int DP>
 constexpr int kSureColumns = DP == 64 ? 16 : DP / 2 + 16;
 
 constexpr float kFloor = -1e30f;   // m of a row that has seen nothing: any score passes it, and 2^(floor - m) is 0
+// Whether a row's largest score makes its m move, and m after it.  Each row decides for itself: were m raised along with another row's, a
+// token that only that one sees would change how this one's weights are rounded.
+__device__ __forceinline__ bool passes(float m, float score) { return score > m + 8.0f; }
+__device__ __forceinline__ float moved(float m, float score) { return passes(m, score) ? score : m; }
 
 // ---- few rows ------------------------------------------------------------------------------------
 // One workgroup per sequence, key head and part of the tokens; NR tiles of sixteen rows (token * group + query head).  Its
@@ -359,9 +363,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
             float lm = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-            if (any(lm > m[t] + 8.0f)) {
+            if (any(passes(m[t], lm))) {
                 lm = fmaxf(lm, __shfl_xor(lm, 16, 64));
-                lm = fmaxf(fmaxf(lm, __shfl_xor(lm, 32, 64)), m[t]);
+                lm = moved(m[t], fmaxf(lm, __shfl_xor(lm, 32, 64)));
                 const float fade = __builtin_amdgcn_exp2f(m[t] - lm);
                 m[t] = lm;
                 l[t] *= fade;
@@ -775,8 +779,8 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
 #pragma unroll
         for (int e = 1; e < 16; ++e) lm = fmaxf(fmaxf(lm, s[0][e]), s[1][e]);
         if constexpr (!CODES) lm *= scale2;
-        if (any(lm > m + 8.0f)) {
-            lm = fmaxf(fmaxf(lm, __shfl_xor(lm, 32, 64)), m);
+        if (any(passes(m, lm))) {
+            lm = moved(m, fmaxf(lm, __shfl_xor(lm, 32, 64)));
             const float fade = __builtin_amdgcn_exp2f(m - lm);
             m = lm;
             l *= fade;

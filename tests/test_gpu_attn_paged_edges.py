@@ -52,3 +52,54 @@ def test_a_key_whose_score_is_infinite_makes_its_row_nan(abq, dim, n):
     p.cache[0][page, 0, o, 1] = float("inf")
     y = run(abq, p)
     assert y[n - 1, :2].isnan().all() and y[n - 1, 2:].isfinite().all() and y[:n - 1].isfinite().all()
+
+
+# ---- tokens that a row does not see ----------------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("n,hq,past", [(4, 4, 300), (3, 10, 330), (5, 10, 350), (100, 2, 700), (60, 4, 400), (70, 4, 1500)])
+def test_hidden_tokens_do_not_reach_the_bits(abq, n, hq, past, dim, bits):
+    """Other keys and values in the last new tokens: the rows before them keep every bit, whatever the later rows' scores do."""
+    p = Paged([(n, past), (1, 20)], hq, 2, dim, 16, bits, seed=n + dim)
+    first = run(abq, p)
+    for t in range(past + n - 2, past + n):
+        page, o = place(p, 0, t)
+        aim = p.q[n - 1].view(2, hq // 2, dim)[:, 0].float().sign()
+        if bits == 16:
+            p.cache[0][page, :, o] = (aim * 8).half()
+            p.cache[1][page, :, o] = 3.0
+        else:
+            p.cache[0][page, :, o] = (128 + 127 * aim).to(torch.uint8)
+            p.cache[2][page, :, o], p.cache[3][page, :, o] = 0.06, 128
+            p.cache[4][page, :, o] = 0.5
+    then = run(abq, p)
+    assert torch.equal(first[:n - 2], then[:n - 2]) and torch.equal(first[n:], then[n:])
+    assert not torch.equal(first[n - 1], then[n - 1])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 0.0, -float("inf")])
+@pytest.mark.parametrize("dim", [64, 80, 256])
+@pytest.mark.parametrize("n", [1, 20, 90])
+def test_scales_of_codes_in_hidden_places_stay_there(abq, n, dim, bad):
+    """The rest of the last page, pages of no sequence (the first one stands in where a page is missing), and later tokens."""
+    p = Paged([(n, 50), (2, 11), (40, 300)], 4, 2, dim, 16, bits=8, seed=n)
+    p.pages[2, 3], p.pages[0, 1] = -1, 1 << 30
+    used = torch.zeros(p.cache[0].shape[0], 16, dtype=torch.bool)
+    for s, length in enumerate(p.lens.tolist()):
+        for t in range(length):
+            if 0 <= int(p.pages[s, t // 16]) < len(used):
+                used[int(p.pages[s, t // 16]), t % 16] = True
+    for i in (2, 4):
+        p.cache[i].permute(0, 2, 1)[~used] = bad
+    for causal in (True, False):
+        y = run(abq, p, causal=causal)
+        want, bound = p.attention(dim ** -0.5, causal)
+        assert ((y.double() - want).abs() <= bound).all()
+    before = run(abq, p)
+    for s, t in ((0, 50 + n - 1), (2, 339)):
+        page, o = place(p, s, t)
+        p.cache[2][page, :, o] = p.cache[4][page, :, o] = bad
+    after = run(abq, p)
+    mine = [n - 1, p.rows - 1]
+    keep = torch.tensor([r for r in range(p.rows) if r not in mine])
+    assert torch.equal(before[keep], after[keep])
