@@ -309,6 +309,14 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (other lanes' rows are read below)
+        if (!CODES && DP != D) {   // zero queries do not rid the sum of an infinity in the columns behind the head
+            asm volatile("");      // (a branch, not a selection that heads of DP go through too)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int u = 0; u < KV; ++u)
+                    if (32 * u + 32 > kSureColumns<DP> && 32 * u + 8 * g >= D) kr[j][u] = u4{0, 0, 0, 0};
+        }
         // scores
         f4 s[NR][2];
 #pragma unroll
@@ -327,10 +335,8 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
 #pragma unroll
                         for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, w[e]), qv[t][2 * u + e], s[t][j], 0, 0, 0);
                 } else {
-                    u4 k = kr[j][u];
-                    if (32 * u + 32 > kSureColumns<DP> && 32 * u + 8 * g >= D) k = u4{0, 0, 0, 0};   // (zero queries do not rid the sum of an infinity)
 #pragma unroll
-                    for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, k), qv[t][u], s[t][j], 0, 0, 0);
+                    for (int t = 0; t < NR; ++t) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kr[j][u]), qv[t][u], s[t][j], 0, 0, 0);
                 }
             }
         }
