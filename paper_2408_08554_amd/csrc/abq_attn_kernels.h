@@ -168,7 +168,10 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
 template <int DP>
 constexpr int kSureColumns = DP == 64 ? 16 : DP / 2 + 16;
 
-constexpr float kFloor = -1e30f;   // m of a row that has seen nothing: any score passes it, and 2^(floor - m) is 0
+constexpr float kFloor = -3.40282347e+38f;   // m of a row that has seen nothing, the lowest number: any other score passes it, and 2^(floor - m) is 0
+// Scores from here on are rounded before m is taken from them.  2^(c x - m) of one operation has the product unrounded, which lies up to
+// |m| 2^-24 above an m that is rounded: beyond the 2^8 that a weight may reach, and at 2^28 beyond binary16.
+constexpr float kFarScore = 0x1p22f;
 // Whether a row's largest score makes its m move, and m after it.  Each row decides for itself: were m raised along with another row's, a
 // token that only that one sees would change how this one's weights are rounded.
 __device__ __forceinline__ bool passes(float m, float score) { return score > m + 8.0f; }
@@ -793,6 +796,19 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= fade;
         }
+        float factor = scale2, base = m;
+        if constexpr (!CODES) {
+            const bool far = fabsf(m) >= kFarScore && m != kFloor;   // (each row for itself)
+            if (any(far)) {
+                asm volatile("");   // (a branch)
+                factor = far ? 1.0f : scale2;
+                base = far ? 0.0f : m;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[k][e] = far ? s[k][e] * scale2 - m : s[k][e];
+            }
+        }
         float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -805,7 +821,7 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float v = s[c >> 1][8 * (c & 1) + 2 * e + r];
-                    x[r] = __builtin_amdgcn_exp2f(CODES ? v - m : fmaf(v, scale2, -m));
+                    x[r] = __builtin_amdgcn_exp2f(CODES ? v - m : fmaf(v, factor, -base));
                     const float part = !CODES ? x[r] : x[r] != 0.0f || !masked ? x[r] * inv[r] : 0.0f;   // (a masked token's scale may be anything)
                     (r & 1 ? sum1 : sum0) += part;
                 }

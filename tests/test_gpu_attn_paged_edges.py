@@ -103,3 +103,28 @@ def test_scales_of_codes_in_hidden_places_stay_there(abq, n, dim, bad):
     mine = [n - 1, p.rows - 1]
     keep = torch.tensor([r for r in range(p.rows) if r not in mine])
     assert torch.equal(before[keep], after[keep])
+
+
+# ---- scores of any size ----------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("past", [30, 1500])
+@pytest.mark.parametrize("n", [1, 5, 90])
+@pytest.mark.parametrize("ahead", ["last", "first"])
+@pytest.mark.parametrize("scale", [0.125, -0.3, 1e12, 1e28])
+def test_large_scores(abq, n, past, bits, ahead, scale):
+    """Scores of 2^17 to 2^124, whole multiples of their difference: the token that is ahead, a row's own or the first, has all the weight, and
+    its value comes out as it is."""
+    p = Paged([(n, past)], 4, 2, 64, 16, bits, seed=n)
+    sign = torch.where(torch.randn(64, generator=p.gen) < 0, -1.0, 1.0)
+    p.q[:] = (sign * (8192.0 if (scale > 0) == (ahead == "last") else -8192.0)).half().repeat(4)
+    for t in range(past + n):
+        page, o = place(p, 0, t)
+        if bits == 16:
+            p.cache[0][page, :, o] = ((t + 1) * 2.0 * sign).half()
+        else:
+            p.cache[0][page, :, o] = (128 + sign * 100).to(torch.uint8)
+            p.cache[2][page, :, o], p.cache[3][page, :, o] = (t + 1) / 64, 128
+    y = run(abq, p, scale)
+    for i in range(n):
+        want = p.held(1, 0, past + i if ahead == "last" else 0)[:, None]
+        assert ((y[i].double().view(2, 2, 64) - want).abs() <= (2.0 ** -11 + 2.0 ** -20) * want.abs()).all(), i
