@@ -421,7 +421,8 @@ int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint
 /* Attention of the rows over what the cache holds of their sequences (the new tokens' keys and values among it: append
  * first).  Query head h reads key head h / (heads_q / heads):
  *   y[row,h,:] = half_rne( sum_t w_t v_t / sum_t w_t ),  w_t = exp(scale * q . k_t),  over the tokens t the row sees:
- *   all of its sequence up to its own position (causal), or all of its sequence (causal = 0).  A row that sees none is zero.
+ *   all of its sequence up to its own position (causal), or all of its sequence (causal = 0).  A row that sees none is zero;
+ *   one whose scores are all minus infinity (keys of a binary16 cache can be infinite) is 0 / 0, NaN.
  * Scores, running maximum, sums and the weighted sum are binary32; the weights are rounded to binary16 for the product with
  * the values.  What lies in pages beyond a sequence's length, or in tokens that a row does not see, does not reach its output
  * (NaN and infinities included).

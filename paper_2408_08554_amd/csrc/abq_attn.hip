@@ -86,8 +86,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
         v = s_o[0][lane] + s_o[1][lane] + (s_o[2][lane] + s_o[3][lane]);
     }
     if (!mine || nparts == 0) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (l == 0.0f) v = f4{0, 0, 0, 0};
+    const float inv = l == 0.0f ? 1.0f : 1.0f / l;
+    if (l == 0.0f) v = f4{} + without_weight(a, sq, seq, i);
     *reinterpret_cast<uint2*>(a.y + yrow * D + 4 * sl) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
 }
 

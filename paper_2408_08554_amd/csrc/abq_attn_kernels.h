@@ -164,6 +164,15 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
     }
 }
 
+// Each element of a row whose weights add up to nothing: zero if it sees no token; else its scores are all minus infinity, and it is 0 / 0.
+__device__ __forceinline__ float without_weight(const AttnArgs& a, const Sequence& sq, int seq, int i)
+{
+    const int seen = sq.seen(i, a.causal), pages = (int)(((int64_t)seen + a.c.page_size - 1) >> a.page_shift);
+    for (int p = 0; p < pages; ++p)
+        if (page_of(a.b, a.c, a.page_shift, seq, p << a.page_shift) >= 0) return __builtin_nanf("");
+    return 0.0f;
+}
+
 // Columns of the DP that a kernel goes over which every head that comes to it has.
 template <int DP>
 constexpr int kSureColumns = DP == 64 ? 16 : DP / 2 + 16;
@@ -427,8 +436,8 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
                 if (nparts > 1) {
                     *reinterpret_cast<f4*>(a.few_o + (a.few_part(seq, head, R) + part) * D + d) = v;
                 } else {
-                    const float inv_sum = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    if (sum == 0.0f) v = f4{0, 0, 0, 0};
+                    const float inv_sum = sum == 0.0f ? 1.0f : 1.0f / sum;
+                    if (sum == 0.0f) v = f4{} + without_weight(a, sq, seq, R / a.group);
                     *reinterpret_cast<uint2*>(a.y + yrow * D + d) = uint2{pack2(v[0] * inv_sum, v[1] * inv_sum), pack2(v[2] * inv_sum, v[3] * inv_sum)};
                 }
             }
@@ -933,7 +942,7 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
     }
     if (grp == 0 && R < nrows) {
         const int64_t yrow = (int64_t)(sq.first + tok) * a.heads_q + hq;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = l == 0.0f ? 1.0f : 1.0f / l, otherwise = nparts == 1 && l == 0.0f ? without_weight(a, sq, seq, tok) : 0.0f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -944,7 +953,7 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
                 if (nparts > 1) {
                     *reinterpret_cast<f4*>(a.many_o + (a.many_part(yrow) + part) * D + at) = v;
                 } else {
-                    if (l == 0.0f) v = f4{0, 0, 0, 0};
+                    if (l == 0.0f) v = f4{} + otherwise;
                     *reinterpret_cast<uint2*>(a.y + yrow * D + at) = uint2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
                 }
             }

@@ -128,3 +128,21 @@ def test_large_scores(abq, n, past, bits, ahead, scale):
     for i in range(n):
         want = p.held(1, 0, past + i if ahead == "last" else 0)[:, None]
         assert ((y[i].double().view(2, 2, 64) - want).abs() <= (2.0 ** -11 + 2.0 ** -20) * want.abs()).all(), i
+
+
+# ---- rows without a weight -------------------------------------------------------------------------
+@pytest.mark.parametrize("past", [20, 1500])
+@pytest.mark.parametrize("n", [1, 3, 40, 90])
+@pytest.mark.parametrize("dim", [64, 80, 256])
+def test_rows_whose_scores_are_all_minus_infinity(abq, dim, n, past):
+    """0 / 0 there, as by the formula; zeros where a row sees no token."""
+    p = Paged([(n, past), (n, -n), (2, 11)], 4, 2, dim, 16, seed=dim + n)
+    p.q.view(p.rows, 4, dim)[..., 2] = 1.0
+    for t in range(past + n):
+        page, o = place(p, 0, t)
+        p.cache[0][page, 1, o, 2] = -float("inf")
+    y = run(abq, p)
+    assert y[:n, 2:].isnan().all() and y[:n, :2].isfinite().all()
+    assert (y[n:2 * n] == 0).all() and y[2 * n:].isfinite().all()
+    p.pages[0] = -1
+    assert (run(abq, p)[:2 * n] == 0).all()
