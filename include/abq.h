@@ -389,7 +389,8 @@ typedef struct abq_kv_cache {
  * The arrays are device memory and never checked on the host.  Whatever they hold, nothing outside the tensors is read or
  * written: rows behind row_start[seqs] are left as they were; a page number outside 0..num_pages-1 (-1, say) is a page
  * that is not there - nothing is appended to it and attention does not see its tokens; tokens beyond max_pages pages and
- * positions below 0 likewise.  abq_attn_paged leaves rows from max_new on as they were and sees no token from max_len on. */
+ * positions below 0 likewise.  abq_attn_paged leaves rows from max_new on as they were and sees no token from max_len on, nor
+ * from 2^30 on. */
 typedef struct abq_batch {
     int rows, seqs, max_pages, max_new, max_len;
     const int32_t *row_start, *lens, *pages;

@@ -143,6 +143,7 @@ hipError_t launch_attn_paged(const abq_kv_cache& c, const abq_batch& b, int head
     AttnArgs a{};
     a.c = c;
     a.b = b;
+    a.b.max_len = std::min(b.max_len, 1 << 30);   // (steps, and windows of steps, are counted past a sequence's end in 32 bits)
     a.heads_q = heads_q;
     a.group = heads_q / c.heads;
     a.page_shift = __builtin_ctz(c.page_size);

@@ -146,3 +146,17 @@ def test_rows_whose_scores_are_all_minus_infinity(abq, dim, n, past):
     assert (y[n:2 * n] == 0).all() and y[2 * n:].isfinite().all()
     p.pages[0] = -1
     assert (run(abq, p)[:2 * n] == 0).all()
+
+
+# ---- the longest sequences -------------------------------------------------------------------------
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_sequence_of_more_than_2_to_the_30_tokens(abq, n):
+    """2^31 - 1 tokens in a table that names one page over and over: the first 2^30 are seen, as if it were the one page."""
+    p = Paged([(n, 4096 - n)], 1, 1, 16, 4096, seed=n)
+    (k, v), (starts, lens, pages), q = p.device()
+    many = torch.full((1, 1 << 19), int(p.pages[0, 0]), dtype=torch.int32, device="cuda")
+    lens.fill_((1 << 31) - 1)
+    y = abq.abq_attn_paged((k, v), (starts, lens, many), q, 0.25).cpu().view(n, 1, 16).double()
+    want, bound = p.attention(0.25, causal=False)
+    # (sums: 2^15 to 2^20 additions of about the same in binary32 each, off by as many times 2^-24 at most)
+    assert ((y - want).abs() <= bound + 2.0 ** -4 * want.abs() + 2.0 ** -6).all()
