@@ -400,7 +400,7 @@ typedef struct abq_batch {
  * rows' queries (optional):
  *   (x[j], x[j + r/2]) -> (x[j] cos a - x[j + r/2] sin a, x[j + r/2] cos a + x[j] sin a),  a = position * inv_freq[j],  j < r/2
  * with r = rotary_dim (0: no rotation, inv_freq not read; elements from r on are kept); `interleaved`: the pairs are
- * (x[2j], x[2j+1]).  The angle is formed and reduced in binary64 (positions are exact however far), sine and cosine are
+ * (x[2j], x[2j+1]).  The angle is reduced from its exact value (positions are exact however far; angles up to 2^48), sine and cosine are
  * within 2^-23, products and sum in binary32, one rounding to binary16.  A cache of codes quantizes the rotated binary16
  * vector.
  *   heads_q    query heads (with q), a multiple of cache->heads, rows * heads_q <= 2^28, seqs * heads <= 2^21;  rotary_dim a multiple of 16, 0..head_dim

@@ -34,13 +34,16 @@ __device__ __forceinline__ int sequence_of_row(const abq_batch& b, int row)
 }
 
 // Sine and cosine of position * frequency.  The angle in quarter turns and its distance from the nearest whole one are formed in
-// binary64 (a position of 2^20 at frequency 1 would lose all but four bits of the fraction in binary32); the remaining eighth
-// of a turn goes through the Taylor polynomials of sine and cosine in binary32, whose first missing terms are below 2^-28 there.
+// binary64 (a position of 2^20 at frequency 1 would lose all but four bits of the fraction in binary32), the angle and the quotient
+// each with what its rounding left (55 bits of product, 2 / pi in two parts: at a position of 2^31 the roundings alone are 2^-22); the
+// remaining eighth of a turn goes through the Taylor polynomials of sine and cosine in binary32, whose first missing terms are below
+// 2^-28 there.
 __device__ __forceinline__ float2 sine_cosine(int position, float frequency)
 {
-    const double quarters = (double)position * (double)frequency * 0.63661977236758134308;   // 2 / pi
-    const double whole = rint(quarters);
-    const float x = (float)(quarters - whole) * 1.57079632679489661923f, z = x * x;
+    constexpr double kTwoByPi = 0.63661977236758134308, kRest = -3.935735335036497e-17;   // (their sum is 2 / pi to 2^-108)
+    const double angle = (double)position * (double)frequency, quarters = angle * kTwoByPi, whole = rint(quarters);
+    const double left = fma(fma((double)position, (double)frequency, -angle), kTwoByPi, fma(angle, kRest, fma(angle, kTwoByPi, -quarters)));
+    const float x = (float)(quarters - whole + left) * 1.57079632679489661923f, z = x * x;
     const int quadrant = (int)(whole - 4.0 * floor(whole * 0.25));
     float s = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
     s = fmaf(fmaf(fmaf(s, z, 8.33333333e-3f), z, -1.66666667e-1f) * z, x, x);

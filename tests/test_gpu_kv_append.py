@@ -174,3 +174,30 @@ def test_offsets_beyond_32_bits(abq):
     kr, vr = abq.abq_kv_read((k, v), i32(pages * page - 1))
     assert torch.equal(kr, new) and torch.equal(vr, 2 * new)
     assert int(k.count_nonzero()) == int(new.count_nonzero())
+
+
+def test_sine_and_cosine_of_far_positions(abq):
+    """Each within 2^-23 of the exact angle's, up to the last position: pairs of (1, 0) come out as them, after one rounding to binary16.  The
+    exact angle is reduced in whole numbers of 2^-180 by pi / 2; sine and cosine of what is left are off by 2^-52."""
+    half_pi = 2407238366421696601854996748563021104914972029442149625   # pi / 2 in those
+    g = torch.Generator().manual_seed(5)
+    rows = 2000
+    at = torch.randint(1 << 30, (1 << 31) - 2, (rows,), generator=g)
+    at[:4] = torch.tensor([(1 << 31) - 2, (1 << 31) - 3, 1 << 30, 5])
+    freq = 1.0 - torch.rand(32, generator=g) / 8
+    freq[0], freq[1] = 1.0, 0.5
+    x = torch.cat([torch.ones(rows, 32), torch.zeros(rows, 32)], 1).half().cuda()
+    cache = tuple(torch.zeros(1, 1, 16, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    batch = (torch.arange(rows + 1, dtype=torch.int32).cuda(), (at + 1).to(torch.int32).cuda(), torch.full((rows, 1), -1, dtype=torch.int32).cuda())
+    y = abq.abq_kv_append(cache, batch, x, x, q=x, inv_freq=freq.cuda()).cpu().double()
+    mant = [int(f * 2.0 ** 40) for f in freq.double()]
+    rest = np.empty((rows, 32, 2))
+    for i, p in enumerate(at.tolist()):
+        for j, m in enumerate(mant):
+            a = p * m << 140
+            turns = (a + half_pi // 2) // half_pi
+            rest[i, j] = (a - turns * half_pi) / 2 ** 180, turns % 4
+    sine, cosine, quadrant = np.sin(rest[..., 0]), np.cos(rest[..., 0]), rest[..., 1]
+    want = [np.select([quadrant == i for i in range(4)], c) for c in ((cosine, -sine, -cosine, sine), (sine, cosine, -sine, -cosine))]
+    want = torch.from_numpy(np.concatenate(want, 1))
+    assert ((y - want).abs() <= 2.0 ** -23 + 2.0 ** -11 * want.abs() + 2.0 ** -25).all()
