@@ -148,6 +148,88 @@ def test_rows_whose_scores_are_all_minus_infinity(abq, dim, n, past):
     assert (run(abq, p)[:2 * n] == 0).all()
 
 
+# ---- every token for itself ------------------------------------------------------------------------
+LONG = [([(1, 5000)], 2, 2), ([(1, 2049)], 8, 1), ([(3, 3000), (2, 700)], 16, 2), ([(1, 2600), (1, 90)], 24, 1), ([(90, 1500)], 2, 2), ([(40, 5000), (1, 900), (0, 3)], 4, 2),
+        ([(33, 4000)] + [(33, 0)] * 63 + [(1, 3000)], 4, 4), ([(2, 1200), (20, 600)], 20, 1), ([(1, 1700)] * 3 + [(300, 40)], 32, 1)]
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 112, 128, 256])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_every_token_counts_once(abq, case, dim, bits):
+    """Equal weights (scale 0), and column d of head h one for the tokens t with t % (heads dim) = h dim + d: a row's result is how many
+    of those it sees over how many it sees in all, so that a token lost or taken twice shows.  The weights, their sums and products are
+    exact, the quotient takes a rounding of binary32, the result one of binary16."""
+    seqs, hq, h = LONG[case]
+    page = 64 if case % 2 else 16
+    p = Paged(seqs, hq, h, dim, page, bits, seed=case)
+    every = h * dim
+    p.cache[1].zero_()
+    if bits == 8:
+        p.cache[4].fill_(1.0), p.cache[5].zero_()
+    for s, length in enumerate(p.lens.tolist()):
+        t = torch.arange(length)
+        at = t % every
+        p.cache[1][p.pages[s, t // page].long(), at // dim, t % page, at % dim] = 1
+    y = run(abq, p, 0.0).double()
+    cls = torch.arange(every).view(h, dim)
+    for s, n in enumerate(p.news):
+        for i in range(n):
+            seen = int(p.lens[s]) - n + i + 1
+            count = ((seen - 1 - cls) // every + 1).clamp(min=0)
+            want = (count / seen)[:, None].expand(h, hq // h, dim).reshape(hq, dim)
+            assert ((y[int(p.row_start[s]) + i] - want).abs() <= want * (2.0 ** -11 + 2.0 ** -22) + 2.0 ** -25).all(), (s, i)
+
+
+EDGES = [0, 1, 15, 16, 31, 32, 33, 63, 64, 127, 128, 255, 256, 257, 511, 512, 513, 767, 768, 895, 896, 1023, 1024, 1025, 1791, 1792, 2048]
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 112, 128, 256])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_every_key_is_its_tokens(abq, case, dim, bits):
+    """Each row and head points at one token's key, those at edges of steps, parts and pages from either end among them, with a score of 80; the
+    others', products with random vectors at up to 13 a standard deviation, stay below 60, and 6000 of them have 2^-16 of the weight."""
+    seqs, hq, h = LONG[case]
+    page, g = 16 if case % 2 else 64, hq // h
+    p = Paged(seqs, hq, h, dim, page, bits, seed=case + 1)
+    if bits == 8:
+        p.cache[2].fill_(0.01)
+    want = torch.empty(p.rows, h, g, dim, dtype=torch.float64)
+    q = p.q.view(p.rows, h, g, dim)
+    head = torch.arange(h)[None, :, None]
+    for s, n in enumerate(p.news):
+        row = int(p.row_start[s]) + torch.arange(n)
+        seen = (int(p.lens[s]) - n + torch.arange(n) + 1)[:, None, None]
+        r = (row[:, None, None] * 31 + head * 7 + torch.arange(g)) % (3 * len(EDGES))
+        edge = torch.tensor(EDGES)[r % len(EDGES)]
+        t = torch.where(r < len(EDGES), edge, torch.where(r < 2 * len(EDGES), seen - 1 - edge, -1))
+        t = torch.where((t < 0) | (t >= seen), (torch.rand(t.shape, generator=p.gen) * seen).long(), t)
+        pg, o = p.pages[s][t // page].long(), t % page
+        key, value = (p.cache[i][pg, head, o].double() for i in (0, 1))
+        if bits == 8:
+            key = (key - p.cache[3][pg, head, o, None].double()) * 0.01
+            value = (value - p.cache[5][pg, head, o, None].double()) * p.cache[4][pg, head, o, None].double()
+        q[row] = (key * (80.0 * dim ** 0.5 / (key * key).sum(-1, keepdim=True))).half()
+        want[row] = value
+    y = run(abq, p).double().view(want.shape)
+    own = torch.arange(p.rows) < int(p.row_start[-1])
+    assert ((y - want).abs() <= 2.0 ** -10 * want.abs() + 2.0 ** -13)[own].all()
+
+
+# ---- two tiles of few rows -------------------------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_two_tiles_of_few_rows(abq, dim, bits):
+    """17 to 32 rows of a sequence and key head: over long contexts in parts, and beside sequences with more."""
+    for p, kw in ((Paged([(3, 3000), (2, 700)], 16, 2, dim, 16, bits, seed=dim), dict(max_new=3)), (Paged([(1, 2600), (1, 90), (0, 5)], 20, 1, dim, 64, bits, seed=dim + 1), dict(max_new=1)),
+                  (Paged([(1, 2600), (1, 90), (40, 500)], 20, 1, dim, 16, bits, seed=dim + 2), {}), (Paged([(1, 1000), (5, 30), (1, 0), (9, 1500)], 32, 1, dim, 16, bits, seed=dim + 3, extra_rows=2), {})):
+        y = run(abq, p, **kw)
+        want, bound = p.attention(dim ** -0.5)
+        left = want.isnan().all(-1).all(-1)
+        assert ((y.double() - want).abs() <= bound)[~left].all()
+
+
 # ---- the longest sequences -------------------------------------------------------------------------
 @pytest.mark.parametrize("n", [1, 40])
 def test_a_sequence_of_more_than_2_to_the_30_tokens(abq, n):

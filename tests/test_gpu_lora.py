@@ -135,3 +135,63 @@ def test_same_inputs_same_bits_and_replays(abq):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("M,N,K,rank", [(300, 192, 160, 16), (300, 200, 161, 24), (290, 128, 264, 100), (290, 136, 264, 128), (270, 192, 96, 200), (700, 1000, 96, 8)])
+def test_in_place_and_strided_many_rows(abq, M, N, K, rank):
+    """The shapes of many rows (tiles of 64, 32 and 16), in place and on rows off 16-byte boundaries."""
+    t = make(M, N, K, rank, 5, seed=M + rank)
+    d = [v.cuda() for v in t]
+    want = check(abq, t).cuda()
+    x = torch.zeros(M, K + 9, dtype=torch.float16, device="cuda")
+    x[:, :K] = d[0]
+    wide = torch.full((M, N + 13), 7.0, dtype=torch.float16, device="cuda")
+    wide[:, 8:8 + N] = d[5]
+    y = wide[:, 8:8 + N]
+    assert abq.abq_lora_add(x[:, :K], *d[1:5], y, out=y) is y
+    assert torch.equal(y, want) and (wide[:, :8] == 7).all() and (wide[:, 8 + N:] == 7).all()
+    assert abq.abq_lora_add(*d, out=d[5]) is d[5]
+    assert torch.equal(d[5], want)
+
+
+@pytest.mark.parametrize("M,rank", [(300, 16), (300, 64), (290, 128), (270, 200), (1100, 8)])
+def test_other_rows_do_not_matter_many_rows(abq, M, rank):
+    t = make(M, 192, 200, rank, 6, seed=rank)
+    t[1] = torch.randperm(M, generator=torch.Generator().manual_seed(M)).to(torch.int32) % 7 - 1
+    want = abq.abq_lora_add(*(v.cuda() for v in t)).cpu()
+    bad = [v.clone() for v in t]
+    bad[2][2], bad[3][4, 50:], bad[4][1] = float("nan"), float("inf"), float("nan")
+    bad[0][7] = float("inf")
+    got = abq.abq_lora_add(*(v.cuda() for v in bad)).cpu()
+    rows = torch.tensor([m for m in range(M) if int(t[1][m]) not in (1, 2, 4) and m != 7])
+    assert torch.equal(got[rows].view(torch.int16), want[rows].view(torch.int16))
+    four = torch.tensor([m for m in range(M) if int(t[1][m]) == 4 and m != 7])
+    assert torch.equal(got[four][:, :50], want[four][:, :50])
+
+
+@pytest.mark.parametrize("N", [8256, 8250])
+@pytest.mark.parametrize("rank", [8, 20, 64])
+def test_two_blocks_a_wave(abq, N, rank):
+    """Rows and columns enough for two blocks of columns a wave, the last waves with one or none; adapters in runs and in any order."""
+    for ids in (None, torch.arange(2048) * 5 // 2048 - 1):
+        t = make(2048, N, 64, rank, 4, seed=N + rank, ids=ids)
+        d = [v.cuda() for v in t]
+        got = abq.abq_lora_add(*d)
+        u = torch.zeros(2048, N, dtype=torch.float64, device="cuda")
+        size = torch.zeros_like(u)
+        for i in range(4):
+            at = (d[1] == i).nonzero()[:, 0]
+            A, B, s = d[2][i].double(), d[3][i].double(), float(d[4][i])
+            x = d[0][at].double()
+            a = x @ A.T.contiguous()
+            u[at] = s * (a @ B.T.contiguous())
+            off = (64 + 2) * 2.0 ** -24 * (x.abs() @ A.abs().T.contiguous()) + 2.0 ** -21 * a.abs().amax(1, keepdim=True)
+            size[at] = abs(s) * ((off + (rank + 4) * 2.0 ** -24 * a.abs()) @ B.abs().T.contiguous())
+        want = d[5].double() + u
+        bound = size + 2.0 ** -23 * want.abs()
+        bound = bound + 2.0 ** -11 * (want.abs() + bound) + 2.0 ** -25
+        assert ((got.double() - want).abs() <= bound).all()
+        none = d[1] < 0
+        assert torch.equal(got[none], d[5][none])
+        assert abq.abq_lora_add(*d, out=d[5]) is d[5]
+        assert torch.equal(d[5], got)
