@@ -424,8 +424,9 @@ int abq_kv_read(const abq_kv_cache* cache, int count, const int32_t* slots, uint
  *   y[row,h,:] = half_rne( sum_t w_t v_t / sum_t w_t ),  w_t = exp(scale * q . k_t),  over the tokens t the row sees:
  *   all of its sequence up to its own position (causal), or all of its sequence (causal = 0).  A row that sees none is zero;
  *   one whose scores are all minus infinity (keys of a binary16 cache can be infinite) is 0 / 0, NaN.
- * Scores, running maximum, sums and the weighted sum are binary32; the weights are rounded to binary16 for the product with
- * the values.  What lies in pages beyond a sequence's length, or in tokens that a row does not see, does not reach its output
+ * Scores, running maximum, sums and the weighted sum are binary32.  For the product with the values the weights have 21 bits
+ * or more where a sequence has few rows to a key head (new tokens times heads_q / heads: up to 16 or 32, by the sizes of the
+ * step), and are rounded to binary16 in longer chunks.  What lies in pages beyond a sequence's length, or in tokens that a row does not see, does not reach its output
  * (NaN and infinities included).
  *   heads_q    as for abq_kv_append
  *   q [rows][heads_q * head_dim], row stride ldq;  y [rows][heads_q * head_dim], contiguous, not overlapping q

@@ -10,6 +10,12 @@
 // is, with the tokens in that order, what the second product wants as its operand: the weights never leave the lane.  V^T comes
 // from row-major V in LDS by the transposing LDS read.  m moves only when a score passes it by 2^8 (a weight of up to 256 loses
 // nothing in binary16), so that most steps need no exchange between lanes and no pass over the sums.
+//
+// Roundings: the second product takes the weights as halves.  Few rows wait for memory, and take what that leaves of a weight as a second
+// half: 22 bits for up to 2 % of the time (32 sequences of 2000 tokens 34.1 and 34.4 us; codes, 4 of 32768, 42.5 and 43.4).  Many rows
+// take one half: the matrix pipe is what they wait for, and the second one's registers are not there (two groups of waves with heads of
+// 128 go to scratch).  A weight is then off by 2^-11 of itself at most, either way, which over many tokens averages out below the result's
+// own rounding.
 #pragma once
 #include "abq_kv.h"
 
@@ -399,10 +405,18 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
             }
             const u4 pw = {pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])};
             const h8 p = __builtin_bit_cast(h8, pw);
+            // what the rounding left is a second operand: the matrix pipe has room for it beside the loads
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] -= (float)p[e];
+            const u4 rw = {pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])};
+            const h8 rest = __builtin_bit_cast(h8, rw);
             const uint16_t* src = lv + (4 * g + (n16 >> 2)) * VS + 4 * (n16 & 3);
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(read_transposed(src + 16 * d), read_transposed(src + 16 * VS + 16 * d)), p, o[t][d], 0, 0, 0);
+            for (int d = 0; d < DT; ++d) {
+                const h8 v = join(read_transposed(src + 16 * d), read_transposed(src + 16 * VS + 16 * d));
+                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, o[t][d], 0, 0, 0);
+                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest, o[t][d], 0, 0, 0);
+            }
         }
     }
 

@@ -54,6 +54,33 @@ def test_a_key_whose_score_is_infinite_makes_its_row_nan(abq, dim, n):
     assert y[n - 1, :2].isnan().all() and y[n - 1, 2:].isfinite().all() and y[:n - 1].isfinite().all()
 
 
+# ---- weights in more bits than binary16 has ----------------------------------------------------------
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("hq,beside", [(4, 0), (40, 0), (4, 100)])
+def test_weights_of_few_rows_are_not_rounded_to_binary16(abq, hq, beside, dim, bits):
+    """Two, four or six tokens of nearly the same weight whose values, of size 1, cancel but for 2^-7.  With 21 bits of a weight, 2^-21 for its
+    exponential and, of codes, 2^-18 for the logarithm of a scale: a result is off by 2^-17 at most, and by half a step of its own."""
+    p = Paged([(1, 1 + 2 * (s % 3)) for s in range(24)] + ([(beside, 0)] if beside else []), hq, 2, dim, 16, bits, seed=dim + hq)
+    p.q.zero_()
+    p.q.view(p.rows, hq, dim)[..., 5] = 1.0
+    sign = torch.where(torch.rand(p.cache[1].shape, generator=p.gen) < 0.5, 1.0, -1.0)
+    sign[:, :, 1::2] = -sign[:, :, ::2]
+    if bits == 16:
+        p.cache[0].copy_(torch.rand(p.cache[0].shape, generator=p.gen) * 2.0 ** -6)
+        p.cache[1].copy_(sign)
+    else:
+        p.cache[2].fill_(2.0 ** -13), p.cache[3].fill_(128)
+        level = torch.randint(1, 120, p.cache[4].shape, generator=p.gen)   # one value's codes and scale, of size 1 together
+        p.cache[1].copy_((128 + sign * level[..., None]).to(torch.uint8))
+        p.cache[4].copy_(1.0 / level.float()), p.cache[5].fill_(128)
+    y = run(abq, p, 1.0).double()[:24]
+    want = p.attention(1.0)[0][:24]
+    assert want.abs().max() < 2.0 ** -5
+    assert ((y - want).abs() <= 2.0 ** -17 + 2.0 ** -11 * want.abs() + 2.0 ** -25).all()
+    assert not torch.equal(y, torch.zeros_like(y))
+
+
 # ---- tokens that a row does not see ----------------------------------------------------------------
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("dim", [64, 80, 128, 256])
