@@ -708,7 +708,7 @@ bool call_on(const char* where, at::Device device, F&& f)
 }
 bool truth(PyObject* o, int otherwise, int* out)
 {
-    *out = o ? PyObject_IsTrue(o) : otherwise;
+    *out = is_none(o) ? otherwise : PyObject_IsTrue(o);
     return *out >= 0;
 }
 

@@ -269,3 +269,9 @@ def test_a_sequence_of_more_than_2_to_the_30_tokens(abq, n):
     want, bound = p.attention(0.25, causal=False)
     # (sums: 2^15 to 2^20 additions of about the same in binary32 each, off by as many times 2^-24 at most)
     assert ((y - want).abs() <= bound + 2.0 ** -4 * want.abs() + 2.0 ** -6).all()
+
+
+def test_none_is_the_default_mask(abq):
+    p = Paged([(5, 20), (40, 3)], 4, 2, 64, 16, seed=1)
+    y = run(abq, p, causal=None)
+    assert torch.equal(y, run(abq, p, causal=True)) and torch.equal(y, run(abq, p)) and not torch.equal(y, run(abq, p, causal=False))
