@@ -135,7 +135,7 @@ __device__ __forceinline__ float only_not_finite(const uint16_t* p)
 }
 
 // A value that is infinite or NaN in a step that some rows see only in part: 0 times it is none, so it stays out of the product
-// there, and the tokens that hold one are kept track of ...
+// there, and the tokens that hold one (not those without a page, for which another's is loaded) are kept track of ...
 struct OddTokens {
     int first, last;
     __device__ __forceinline__ void clear() { first = INT32_MAX; last = -1; }
@@ -157,7 +157,8 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Sequence
         float x = 0.0f;
         for (int t = first; t < end; ++t) {
             const int page = page_of(a.b, a.c, a.page_shift, seq, t);
-            if (page >= 0) x += only_not_finite((const uint16_t*)a.c.v + vector_of(a.c, page, head, t & (a.c.page_size - 1)) * D + d);
+            if (page < 0) t |= a.c.page_size - 1;   // (the next page's first comes then)
+            else x += only_not_finite((const uint16_t*)a.c.v + vector_of(a.c, page, head, t & (a.c.page_size - 1)) * D + d);
         }
         if (x == 0.0f) continue;
         const int64_t yrow = (int64_t)(sq.first + R / a.group) * a.heads_q + head * a.group + R % a.group;
@@ -322,7 +323,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, uint16_t* lds, int h
                 *reinterpret_cast<u4*>(dst + 8) = w[1];
             } else {
                 u4 v = vr[u];
-                if (masked && drop_not_finite(v)) s_odd.found(t0 + u * TPL + lane / LPT, to);
+                if (masked && drop_not_finite(v) && !(u * TPL < 16 ? gone0 : gone1)) s_odd.found(t0 + u * TPL + lane / LPT, to);
                 *reinterpret_cast<u4*>(dst) = v;
             }
         }
@@ -701,7 +702,7 @@ __device__ __forceinline__ void attn_many(const AttnArgs& a, uint16_t* lds, unsi
                     u4* const p = reinterpret_cast<u4*>(lv + (j & 1) * VL + (u * TPL + row_at) * VS + col_at);
                     u4 v = *p;
                     if (drop_not_finite(v)) {
-                        s_odd.found(t_of(j) + u * TPL + row_at, to);
+                        if (!(gone_at(j) >> wave & 1u)) s_odd.found(t_of(j) + u * TPL + row_at, to);
                         *p = v;
                     }
                 }

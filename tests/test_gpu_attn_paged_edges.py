@@ -275,3 +275,33 @@ def test_none_is_the_default_mask(abq):
     p = Paged([(5, 20), (40, 3)], 4, 2, 64, 16, seed=1)
     y = run(abq, p, causal=None)
     assert torch.equal(y, run(abq, p, causal=True)) and torch.equal(y, run(abq, p)) and not torch.equal(y, run(abq, p, causal=False))
+
+
+@pytest.mark.parametrize("n", [1, 60])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_missing_pages_cost_nothing_more_where_the_first_page_is_not_finite(abq, n, dim):
+    """A sequence whose pages are gone but for the last (a window over a long context): the cache's first page, which stands in for them,
+    may hold anything; results and time are as if it held numbers."""
+    p = Paged([(n, 8000), (1, 3)], 8, 2, dim, 16, seed=dim)
+    p.pages[0, :480] = -1
+    p.pages[0, 480:], p.pages[1, 0] = 1 + torch.arange(p.pages.shape[1] - 480), 100   # (none of them the first)
+    cache, batch, q = p.device()
+    want, bound = p.attention(dim ** -0.5)
+
+    def timed():
+        best = 1e9
+        for _ in range(3):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            for _ in range(4):
+                y = abq.abq_attn_paged(cache, batch, q, dim ** -0.5)
+            e[1].record()
+            torch.cuda.synchronize()
+            best = min(best, e[0].elapsed_time(e[1]))
+        assert ((y.cpu().view(want.shape).double() - want).abs() <= bound).all()
+        return best
+
+    timed()
+    before = timed()
+    cache[0][0], cache[1][0] = float("nan"), float("inf")
+    assert timed() < 4 * before
