@@ -445,7 +445,7 @@ int abq_attn_paged(const abq_kv_cache* cache, const abq_batch* batch, int heads_
  *   x [M][K] row stride ldx;  ids [M] int32 (device);  a [adapters][rank][K], b [adapters][N][rank] binary16;
  *   scale [adapters] float;  y [M][N] row stride ldy;  out [M][N] row stride ldout: y itself (same stride), or no overlap
  *   (strides in elements, any value >= K or N)
- * A row's result does not depend on the other rows' adapters or inputs.
+ * A row's result does not depend on the other rows' adapters or inputs; infinities in its own come out as infinities or NaN.
  *   workspace  at least abq_lora_add_workspace_bytes(M, N, K, rank) bytes; contents on entry are irrelevant, calls that may
  *              overlap need one each. */
 size_t abq_lora_add_workspace_bytes(int M, int N, int K, int rank);

@@ -114,9 +114,14 @@ static AttnPlan attn_plan(const abq_kv_cache& c, const abq_batch& b, int heads_q
     const int tokens = (int)std::min<int64_t>(b.max_len, (int64_t)b.max_pages * c.page_size);
     p.few_parts = p.many_parts = 1;
     // Parts until each compute unit has a workgroup (of codes two, which have half the bytes in flight); beside prompts half of them
-    // have one.  More parts balance better but have to be joined (us at 256, 512, 1024 workgroups; heads of 128: 32 sequences of 2048 on
-    // 8 heads 41, 47, 47, 8 of 1000 on 32 21, 25, 26, 40 of 2048 on 8 62, 62, 59; codes, 4 of 32768 on 8 58, 50, 54; a prompt of 333
-    // with eight decoding requests at 128 and 256: 30, 33).
+    // have one.  More parts balance better but have to be joined.  us, heads of 128, n sequences of two thirds of L to L tokens on h key heads:
+    //   binary16, at 128, 256, 512 workgroups: 4 of 32000 on 8 106, 90, 89; 4 of 8000 on 8 29, 28, 26; 16 of 1000 on 8 17, 18, 18; 32 of 2000 on
+    //     8 38, 38, 42; 8 of 2000 on 32 38, 38, 42; 8 of 8000 on 32 162, 162, 167
+    //   codes, at 256, 512, 1024: 4 of 32000 on 8 54, 47, 48; 4 of 8000 on 8 23, 20, 22; 1 of 32000 on 32 56, 50, 52; 8 of 2000 on 8 15.0,
+    //     15.5, 15.3; 32 of 2000 on 8 27, 28, 29; 8 of 2000 on 32 28, 30, 31
+    //   beside a prompt's chunk of 333 over 1000, at 128, 256, 512: 8 of 1000 on 8 30, 32, 33 (codes 35, 37, 38); 2 of 4000 on 8 37, 55, 59;
+    //     32 of 2000 on 32 166, 167, 166; beside a prompt of 1000: 2 of 4000 on 8 35, 67, 68; but few long ones would have more:
+    //     4 of 16000 on 32 229, 193, 191
     if (p.few && !stays_whole(tokens, kFewLeast)) {
         const int64_t wgs = (int64_t)b.seqs * c.heads, want = p.both ? 128 : c.kv_bits == 8 ? 512 : 256;
         p.few_parts = (int)std::min<int64_t>({(want + wgs - 1) / wgs, (tokens + kFewLeast - 1) / kFewLeast, 64});

@@ -198,9 +198,9 @@ __device__ __forceinline__ float moved(float m, float score) { return passes(m, 
 // WAVES waves take 32 tokens in turn, each with a maximum, sums and an LDS region of its own (no barrier in the loop), and are
 // joined at the end.  K goes from memory straight into the matrix operand's registers, V through LDS for the transposition.
 // What bounds it: memory.  A wave has 16 KB in flight (32 tokens of K and V, 128 halves each) from the moment it has used the
-// last ones, and two to four workgroups share a compute unit.  32 sequences of 2048 tokens, 32 heads on 8 of 128: 148 us, 5.5 TB/s (a
-// large copy: 5.1); as codes, 4 of 32768: 41 us and 5 for the joining, 219 MB at 5.3 TB/s.  One sequence of 513 is latency: 7.6 us
-// (6.5 for a lone workgroup's one step) and 2.8 for the joining.
+// last ones, and two to four workgroups share a compute unit.  32 sequences of 1..2 thousand tokens, 32 heads on 32 of 128, 814 MB:
+// 148 us, 5.5 TB/s (a large copy: 5.1); as codes, four of 19..32 thousand, 103088 tokens on 8 heads, 219 MB: 41 us, 5.3 TB/s, and 5 for
+// the joining.  One sequence of 513 on 32 heads is latency: 7.5 us, and 3.2 for the joining.
 template <int DP, int WAVES>
 constexpr int kFewLds = WAVES * kFewTokens * (DP + 16);   // halves
 template <int DP, bool CODES, int NR, int WAVES>
@@ -530,9 +530,11 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t* p) { return (uin
 // half a step behind the first, so that of the two waves of a SIMD one has matrix and the other vector work.  Each group has two
 // buffers for K and two for V, of steps in turn; binary16 goes into them straight from memory, the next but one while this is used.
 // What bounds it: of a step's 3400 clocks the matrix half takes 1500 and the rest 1900 (1150 of them softmax),
-// which the other group's matrix half hides all but 400 of.  1024 tokens over 15360, 32 heads on 8 of 128: 275 us (969 TFLOP/s; one
-// group alone 370), as codes 354 (750);
-// a prompt of 2048, 32 heads: 53 us (650: two workgroups a unit, one after the other, each with its start and end).
+// which the other group's matrix half hides all but 400 of.  1024 tokens over 15360, 32 heads on 8 of 128: 272 us (980 TFLOP/s; one
+// group alone 370), as codes 363 (735), both 6 % longer on some cards.
+// A prompt of 2048, 32 heads, takes 54..57 us (600..640 TFLOP/s): two workgroups a unit, one after the other, 17 rounds of two steps at
+// 1.6 us together, and about 12 us for each one's start and end (a prompt of 128, one round, takes 13; 16 heads, one workgroup a unit of
+// up to 16 rounds, 37).
 template <int DP, bool CODES, int GROUPS>
 constexpr int kManyLds = GROUPS * 2 * kManyTokens * (CODES ? 2 * DP + 40 : 2 * DP);   // halves
 template <int DP, bool CODES, int GROUPS>

@@ -2,7 +2,7 @@
 // on the way; and the way back.
 //
 // What bounds it: a step of few rows is latency (row -> sequence -> position -> page -> store, three dependent loads beside
-// the operands' own): one row of 32 heads of 128 takes 3.0 us, 64 rows with 8 key heads as codes 4.1, reading them back 2.4.  A prompt is
+// the operands' own): one row of 32 heads of 128 takes 3.0 us, 64 rows with 8 key heads as codes 4.3, reading them back 2.7.  A prompt is
 // the copy of its vectors: two prompts of up to 2048 tokens, 40 heads on 40, 213 MB in 48 us, 4.4 TB/s (a large copy: 5.1; 34 us where
 // the last-level cache holds them).
 #include "abq_kv.h"
