@@ -146,3 +146,48 @@ def test_codes_of_a_token_whose_values_are_zero(abq, n):
     y = abq.abq_attn_paged(cache, (p.row_start.cuda(), lens, pages), p.q.cuda(), 0.125).cpu().view(n, 4, 64).double()
     want, bound = p.attention(0.125)
     assert ((y - want).abs() <= bound).all() and bound.max() < 2.0 ** -10   # (values of up to 2^-4)
+
+
+def test_a_step_of_prompts_over_codes_as_graphs(abq):
+    """Adapters of many rows, append to a cache of codes, reading back and attention of prompts beside single tokens, in parts: two graphs of their
+    own workspaces, replayed at once on two streams, with eager work between, on inputs and lengths that change."""
+    p = Paged([(300, 900), (1, 3000), (2, 40)], HQ, H, 128, PAGE, bits=8, seed=8, extra_rows=2)
+    g = torch.Generator().manual_seed(8)
+    start, pages = p.row_start.cuda(), p.pages.cuda()
+    lens = p.lens.cuda()
+    x, ids = torch.zeros(p.rows, 256, dtype=torch.float16, device="cuda"), torch.randint(-1, 3, (p.rows,), generator=g).to(torch.int32).cuda()
+    a, b = (torch.randn(3, 8, 256, generator=g) / 16).half().cuda(), (torch.randn(3, HQ * 128, 8, generator=g) * 0.3).half().cuda()
+    scale, freq = torch.ones(3, device="cuda"), (10000.0 ** (-torch.arange(0, 128, 2).double() / 128)).float().cuda()
+    k, v, base = (p.normal(p.rows, n * 128).cuda() for n in (H, H, HQ))
+    slots = torch.arange(0, 200, 7, dtype=torch.int32).cuda()
+
+    def step(cache):
+        q = abq.abq_lora_add(x, ids, a, b, scale, base)
+        q = abq.abq_kv_append(cache, (start, lens, pages), k, v, q=q, inv_freq=freq, q_out=torch.zeros_like(q))
+        return abq.abq_attn_paged(cache, (start, lens, pages), q, 128 ** -0.5, y=torch.zeros_like(q)), *abq.abq_kv_read(cache, slots)
+
+    caches = [tuple(t.cuda() for t in p.cache) for _ in range(3)]
+    step(caches[0])
+    torch.cuda.synchronize()
+    for c in caches[1:]:
+        for to, t in zip(c, caches[0]):
+            to.copy_(t)
+    graphs = []
+    for c in caches[1:]:
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=stream):
+            out = step(c)
+        graphs.append((graph, stream, out))
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=g).half())
+        k.copy_(p.normal(*k.shape)), v.copy_(p.normal(*v.shape))
+        lens -= i
+        want = step(caches[0])
+        torch.cuda.synchronize()
+        for graph, stream, _ in graphs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (_, _, out), c in zip(graphs, caches[1:]):
+            assert all(torch.equal(y, w) for y, w in zip(out, want)), i
+            assert all(torch.equal(t, w) for t, w in zip(c, caches[0])), i
