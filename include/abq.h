@@ -453,6 +453,62 @@ int abq_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x,
                  const uint16_t* a, const uint16_t* b, const float* scale, const uint16_t* y, int ldy, uint16_t* out, int ldout,
                  void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A layer of experts (a block's MLP as many small ones, a few of which each token goes through): the router's choice, the
+ * products with the experts' quantized weights, and the weighted sum.  The pieces between are the calls above:
+ * abq_rmsnorm_quant_act makes the codes that the up projections take, abq_silu_mul_quant_act those of the down projection.
+ * A row is (token, choice), numbered token * top + choice ("slot"); rows sorted by expert have a place.
+ * ------------------------------------------------------------------------------------------ */
+#define ABQ_MOE_MAX_EXPERTS 1024
+#define ABQ_MOE_MAX_TOP 16
+
+/* The router: from each token's logits the `top` experts it goes to, their weights, and the rows sorted by expert.
+ *   choice   the largest logits, largest first, ties to the lowest expert; with a bias the largest score + bias[e] (scores and sum in
+ *            binary64).  An expert whose logit is minus infinity or NaN (or whose score + bias is) is not there: a token with
+ *            fewer than `top` experts, a padding row with none, has -1 and weight 0 in its last choices.
+ *   score    softmax over all of the token's experts (sigmoid = 0) or the sigmoid of the logit
+ *   weight   score, with renormalize score / (sum of the chosen ones' scores); times scale.  Binary32, exponentials of differences from
+ *            the largest logit.  (A logit of plus infinity makes NaN of its token's softmax weights, and with a bias its softmax
+ *            scores too.)
+ *   logits   [tokens][experts], row stride ld in elements, binary16 (logits_bits = 16) or float (32);  bias [experts] float or NULL
+ *   ids, places [tokens][top] int32: expert, place of each choice (-1: none);  weights [tokens][top] float
+ *   starts   [experts + 1] int32: expert e has the places starts[e] .. starts[e+1] - 1, in the order of their slots
+ *   order    [tokens * top] int32: the slot at each place, -1 behind the last one
+ *   1 <= experts <= ABQ_MOE_MAX_EXPERTS, 1 <= top <= min(experts, ABQ_MOE_MAX_TOP), tokens * top <= 2^22
+ *   workspace at least abq_moe_route_workspace_bytes(...) bytes (0 for few tokens); contents on entry are irrelevant, calls that
+ *            may overlap need one each. */
+size_t abq_moe_route_workspace_bytes(int tokens, int experts, int top);
+int abq_moe_route(int tokens, int experts, int top, const void* logits, int logits_bits, int ld, const float* bias, int sigmoid,
+                  int renormalize, float scale, int32_t* ids, float* weights, int32_t* starts, int32_t* order, int32_t* places,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* One linear layer of all experts: place r, which starts[e] <= r < starts[e+1] gives to expert e, is row r of Y:
+ *   Y[r,:] = dequant( A[s] . W_e^T ),   s = order[r] / top, or r where order is NULL
+ * with accumulator and epilogue of abq_gemm, to the bit (the int32 accumulator is not returned).
+ *   a_codes  [tokens][K] uint8 (bits above q are dropped), a_scale [tokens] float, a_zero [tokens] int32
+ *   packed_w one blob of abq_pack_weights(p, N, K, ..., w_layout) for each expert, w_stride bytes apart (a multiple of 16, at least the
+ *            blob's size); field-packed per-channel blobs (AUTO, FIELDS, BOTH), else ABQ_ERR_LAYOUT
+ *   starts   [experts + 1] int32, ascending from 0 (device);  order [rows] int32 (device) or NULL, then tokens = rows
+ *   y_fp16   [rows][N] binary16: rows from starts[experts] on are left as they were
+ * starts and order are never checked on the host.  Whatever they hold, nothing outside the tensors is read or written; starts that do
+ * not ascend, and entries of order that name no row of A, leave the rows concerned with unspecified contents.
+ *   1 <= rows, tokens <= 2^22;  tokens * K (K rounded up to 512) < 2^32;  (rows / 64 + experts) * ceil(N / 128) < 2^24;
+ *   the rest as for abq_gemm.  Workspace: at least abq_moe_gemm_workspace_bytes(...) bytes (0 where an expert has few rows: the codes
+ *   are packed on the way there); contents on entry are irrelevant, calls that may overlap need one each. */
+size_t abq_moe_gemm_workspace_bytes(int p, int q, int rows, int N, int K, int tokens, int experts);
+int abq_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int top,
+                 const uint8_t* a_codes, const float* a_scale, const int32_t* a_zero, const void* packed_w, size_t w_stride, int w_layout,
+                 const int32_t* starts, const int32_t* order, uint16_t* y_fp16, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Back to one row a token:
+ *   out[t,:] = half_rne( add[t,:] + sum_j weights[t,j] * y[places[t,j],:] ),   j < top in this order, in binary32
+ * over the choices whose place is in 0..rows-1 (add NULL: without it; a shared expert's output, or the residual).
+ *   y [rows][N] row stride ldy, add, out [tokens][N] row strides ldadd, ldout (binary16, strides in elements, any value >= N); out may be add
+ *   itself (same stride), and overlaps nothing else;  weights [tokens][top] float, places [tokens][top] int32 (device)
+ *   1 <= tokens, rows <= 2^22, 1 <= N <= 2^20, tokens * ceil(N / 2048) < 2^24 */
+int abq_moe_combine(int tokens, int N, int rows, int top, const uint16_t* y, int ldy, const int32_t* places, const float* weights,
+                    const uint16_t* add, int ldadd, uint16_t* out, int ldout, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ ABQ_LAYOUT_AUTO, ABQ_LAYOUT_PLANES, ABQ_LAYOUT_FIELDS, ABQ_LAYOUT_BOTH = 0, 1, 2
 ABQ_LAYOUT_FIELDS_G128 = 4
 ABQ_USE_PLANES, ABQ_USE_FIELDS = 0x10, 0x20
 ABQ_MAX_K = 131072
+ABQ_MOE_MAX_EXPERTS, ABQ_MOE_MAX_TOP = 1024, 16
 ABQ_STATIC_SCRATCH_BYTES = 32 << 20
 
 # every symbol include/abq.h declares: (restype, argtypes)
@@ -64,6 +65,11 @@ _SIGNATURES = {
                                   _c.c_size_t, _c.c_void_p]),
     "abq_lora_add_workspace_bytes": (_c.c_size_t, [_c.c_int] * 4),
     "abq_lora_add": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p, _c.c_int] + [_c.c_void_p] * 4 + [_c.c_void_p, _c.c_int] * 2 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "abq_moe_route_workspace_bytes": (_c.c_size_t, [_c.c_int] * 3),
+    "abq_moe_route": (_c.c_int, [_c.c_int] * 3 + [_c.c_void_p, _c.c_int, _c.c_int, _c.c_void_p, _c.c_int, _c.c_int, _c.c_float] + [_c.c_void_p] * 6 + [_c.c_size_t, _c.c_void_p]),
+    "abq_moe_gemm_workspace_bytes": (_c.c_size_t, [_c.c_int] * 7),
+    "abq_moe_gemm": (_c.c_int, [_c.c_int] * 8 + [_c.c_void_p] * 4 + [_c.c_size_t, _c.c_int] + [_c.c_void_p] * 4 + [_c.c_size_t, _c.c_void_p]),
+    "abq_moe_combine": (_c.c_int, [_c.c_int] * 4 + [_c.c_void_p, _c.c_int] + [_c.c_void_p] * 2 + [_c.c_void_p, _c.c_int] * 2 + [_c.c_void_p]),
     "abq_gemm_act_codes_static": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p] * 4 + [_c.c_int, _c.c_void_p, _c.c_void_p, _c.c_void_p]),
 }
 
@@ -162,6 +168,32 @@ def abq_pack_weights_g128(p, w_codes, w_scale_fp16, w_zero, out=None):
     _check(lib.abq_pack_weights_g128(p, N, K, _ptr(w_codes), _ptr(w_scale_fp16), _ptr(w_zero), _ptr(out), out.numel(),
                                      _stream()), "abq_pack_weights_g128")
     return out
+
+
+def abq_pack_experts(p, w_codes, w_scale, w_zero, layout=ABQ_LAYOUT_AUTO, out=None):
+    """The weights of a layer of experts: w_codes uint8 [experts,N,K], w_scale float32 [experts,N], w_zero int32 [experts,N] (device)
+    -> uint8 [experts, bytes of a blob], each row a blob of abq_pack_weights, as abq_moe_gemm takes them."""
+    E, N, K = w_codes.shape
+    _dev(w_codes, torch.uint8), _dev(w_scale, torch.float32, (E, N)), _dev(w_zero, torch.int32, (E, N))
+    nbytes = max(abq_packed_weight_bytes(p, N, K, layout), 16)
+    if out is None:
+        out = torch.empty((E, nbytes), dtype=torch.uint8, device=w_codes.device)
+    lib = load()
+    with torch.cuda.device(w_codes.device):
+        _dev(out, torch.uint8, (E, nbytes))
+        whole = lambda x: x if x.data_ptr() % 16 == 0 else x.clone()   # (a row of the stacked operands may start off a 16-byte boundary)
+        for e in range(E):
+            codes, scale, zero = whole(w_codes[e]), whole(w_scale[e]), whole(w_zero[e])
+            _check(lib.abq_pack_weights(p, N, K, _ptr(codes), _ptr(scale), _ptr(zero), layout, _ptr(out[e]), nbytes, _stream()), "abq_pack_experts")
+    return out
+
+
+def abq_moe_route_workspace_bytes(tokens, experts, top):
+    return load().abq_moe_route_workspace_bytes(tokens, experts, top)
+
+
+def abq_moe_gemm_workspace_bytes(p, q, rows, N, K, tokens, experts):
+    return load().abq_moe_gemm_workspace_bytes(p, q, rows, N, K, tokens, experts)
 
 
 def abq_check_packed(kind, bits, rows, K, layout, packed):
@@ -274,7 +306,8 @@ def abq_plan_clear():
 # The online calls, from abq_native; their docstrings say what they take and return.
 _NATIVE = ("abq_quant_pack_act", "abq_pack_act_codes", "abq_f4_pack_codes", "abq_rmsnorm_quant_act", "abq_add_rmsnorm_quant_act",
            "abq_silu_mul_quant_act", "abq_gemm", "abq_gemm_act_codes", "abq_gemm_act_codes_requant", "abq_gemm_act_codes_static",
-           "abq_gemm_grouped", "abq_f4_gemm", "abq_kv_append", "abq_kv_read", "abq_attn_paged", "abq_lora_add")
+           "abq_gemm_grouped", "abq_f4_gemm", "abq_kv_append", "abq_kv_read", "abq_attn_paged", "abq_lora_add",
+           "abq_moe_route", "abq_moe_gemm", "abq_moe_combine")
 
 
 def _bind():

@@ -4,6 +4,7 @@
 #include "abq_internal.h"
 #include "../../include/abq.h"
 #include "abq_kv.h"
+#include "abq_moe.h"
 
 #include <limits.h>
 #include <stdlib.h>
@@ -965,6 +966,80 @@ int abq_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x,
     if (need && !workspace) return ABQ_ERR_NULL;
     if (workspace_bytes < need) return ABQ_ERR_SIZE;
     return hip_status(launch_lora_add(M, N, K, rank, adapters, x, ldx, ids, a, b, scale, y, ldy, out, ldout, workspace, (hipStream_t)stream));
+}
+
+// ---- a layer of experts: router, products, weighted sum -------------------------------------------
+static int check_route_shape(int tokens, int experts, int top)
+{
+    return tokens < 1 || experts < 1 || experts > ABQ_MOE_MAX_EXPERTS || top < 1 || top > ABQ_MOE_MAX_TOP || top > experts || (int64_t)tokens * top > (1 << 22) ? ABQ_ERR_SHAPE : ABQ_OK;
+}
+
+size_t abq_moe_route_workspace_bytes(int tokens, int experts, int top)
+{
+    return check_route_shape(tokens, experts, top) ? 0 : moe_route_workspace_bytes(tokens, experts);
+}
+
+int abq_moe_route(int tokens, int experts, int top, const void* logits, int logits_bits, int ld, const float* bias, int sigmoid, int renormalize,
+                  float scale, int32_t* ids, float* weights, int32_t* starts, int32_t* order, int32_t* places, void* workspace,
+                  size_t workspace_bytes, void* stream)
+{
+    if (!logits || !ids || !weights || !starts || !order || !places) return ABQ_ERR_NULL;
+    if (logits_bits != 16 && logits_bits != 32) return ABQ_ERR_BITS;
+    if (int e = check_route_shape(tokens, experts, top)) return e;
+    if (ld < experts) return ABQ_ERR_SHAPE;
+    if (misaligned(logits) || misaligned(bias) || misaligned(ids) || misaligned(weights) || misaligned(starts) || misaligned(order) || misaligned(places) || misaligned(workspace))
+        return ABQ_ERR_ALIGN;
+    const size_t need = moe_route_workspace_bytes(tokens, experts);
+    if (need && !workspace) return ABQ_ERR_NULL;
+    if (workspace_bytes < need) return ABQ_ERR_SIZE;
+    const MoeRouteArgs g{tokens, experts, top, logits_bits, ld, logits, bias, sigmoid != 0, renormalize != 0, scale, ids, weights, starts, order, places, workspace};
+    return hip_status(launch_moe_route(g, (hipStream_t)stream));
+}
+
+// Rows, and workgroups of 64 x 128 outputs, that a launch can have; packed rows of A below 4 GiB (their offsets have 32 bits).
+static int check_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int w_layout)
+{
+    if (int e = check_gemm_shape(p, q, rows, N, K)) return e;
+    if (rows > (1 << 22) || tokens < 1 || tokens > (1 << 22) || experts < 1 || experts > ABQ_MOE_MAX_EXPERTS) return ABQ_ERR_SHAPE;
+    if (((int64_t)rows / 64 + (experts < rows ? experts : rows)) * (((int64_t)N + 127) / 128) >= (1 << 24)) return ABQ_ERR_SHAPE;
+    if ((int64_t)tokens * ((K + kSuperK - 1) / kSuperK * kSuperK) >= (1LL << 32)) return ABQ_ERR_SHAPE;
+    return w_layout == ABQ_LAYOUT_AUTO || w_layout == ABQ_LAYOUT_FIELDS || w_layout == ABQ_LAYOUT_BOTH ? ABQ_OK : ABQ_ERR_LAYOUT;
+}
+
+size_t abq_moe_gemm_workspace_bytes(int p, int q, int rows, int N, int K, int tokens, int experts)
+{
+    return check_moe_gemm(p, q, rows, N, K, tokens, experts, ABQ_LAYOUT_AUTO) ? 0 : moe_gemm_workspace_bytes(p, q, rows, N, K, tokens, experts);
+}
+
+int abq_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int top, const uint8_t* a_codes, const float* a_scale,
+                 const int32_t* a_zero, const void* packed_w, size_t w_stride, int w_layout, const int32_t* starts, const int32_t* order,
+                 uint16_t* y_fp16, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!a_codes || !a_scale || !a_zero || !packed_w || !starts || !y_fp16) return ABQ_ERR_NULL;
+    if (int e = check_moe_gemm(p, q, rows, N, K, tokens, experts, w_layout)) return e;
+    if (order ? top < 1 : tokens != rows) return ABQ_ERR_SHAPE;
+    WeightLayout W;
+    if (!make_weight_layout(p, N, K, w_layout, &W)) return ABQ_ERR_SHAPE;
+    if (misaligned(a_codes) || misaligned(a_scale) || misaligned(a_zero) || misaligned(packed_w) || w_stride % 16 != 0 || misaligned(starts) || misaligned(order) ||
+        misaligned(y_fp16) || misaligned(workspace))
+        return ABQ_ERR_ALIGN;
+    if (w_stride < W.total && experts > 1) return ABQ_ERR_SIZE;
+    const size_t need = moe_gemm_workspace_bytes(p, q, rows, N, K, tokens, experts);
+    if (need && !workspace) return ABQ_ERR_NULL;
+    if (workspace_bytes < need) return ABQ_ERR_SIZE;
+    const MoeGemmArgs g{p, q, rows, N, K, tokens, experts, order ? top : 1, a_codes, a_scale, a_zero, (const uint8_t*)packed_w, w_stride, starts, order, y_fp16, workspace};
+    return hip_status(launch_moe_gemm(g, W, (hipStream_t)stream));
+}
+
+int abq_moe_combine(int tokens, int N, int rows, int top, const uint16_t* y, int ldy, const int32_t* places, const float* weights,
+                    const uint16_t* add, int ldadd, uint16_t* out, int ldout, void* stream)
+{
+    if (!y || !places || !weights || !out) return ABQ_ERR_NULL;
+    if (tokens < 1 || tokens > (1 << 22) || N < 1 || N > (1 << 20) || rows < 1 || rows > (1 << 22) || top < 1 || top > ABQ_MOE_MAX_EXPERTS ||
+        (int64_t)tokens * ((N + 2047) / 2048) >= (1 << 24) || ldy < N || ldout < N || (add && ldadd < N) || (add && out == add && ldout != ldadd))
+        return ABQ_ERR_SHAPE;
+    if (misaligned(y) || misaligned(places) || misaligned(weights) || misaligned(add) || misaligned(out)) return ABQ_ERR_ALIGN;
+    return hip_status(launch_moe_combine(tokens, N, rows, top, y, ldy, places, weights, add, ldadd, out, ldout, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -16,6 +16,7 @@
 // Before / now (tiled kernel / this one, rows packed, replays): W4A4 M=2048 5120->13824 135 / 111 us, W8A8 147 / 119, M=1024 70 / 51 and
 // 79 / 60, W8A8 M=512 4096->11008 32.5 / 26.5, 11008->4096 42 / 29.
 #pragma once
+#include "abq_moe.h"
 #include "abq_rows.h"
 
 #include <type_traits>
@@ -36,6 +37,13 @@ struct BlockParams {
     int tiles_m, tiles_n;        // workgroup tiles along M and N (1-D grid of tiles_m * tiles_n workgroups)
     int band_m;                  // row blocks per band of the tile order
     int narrow_sums;             // 1: every row sum of codes is below 2^23 (the epilogue then multiplies at the 24-bit rate)
+};
+
+// The same for a layer of experts: workgroup tiles of rows that chose one expert, against that expert's weights.  Fields, wparams: of expert 0;
+// M: rows of A there are; tiles_m: row tiles there can be at most.
+struct BlockExpertParams : BlockParams {
+    MoeGroups g;
+    size_t w_stride;
 };
 
 constexpr int kBkStep = 128;     // k per step: one chunk of a 4-bit group, two 64-k slices
@@ -76,10 +84,11 @@ __device__ __forceinline__ int32_t bk_mad24(int32_t a, int32_t b, int32_t c)
 // What the epilogue needs of a channel: the sum over the codes less their zero-points is acc + raw0 + wz sumA - az cw.
 struct alignas(16) ColParams { int32_t raw0, cw, wz; float scale; };
 
-// OCC: waves per SIMD that the registers are held to.
-template <int P, int RW, int CW, int MT, int NT, int S, int OCC>
-__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams prm)
+// OCC: waves per SIMD that the registers are held to.  PRM: BlockParams or BlockExpertParams.
+template <int P, int RW, int CW, int MT, int NT, int S, int OCC, class PRM = BlockParams>
+__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
 {
+    constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kWaves = RW * CW, kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
     constexpr int kABytes = kBM * kBkStep, kBuf = kABytes + kTW * bk_fast_chunks(P) * 1024;
     constexpr int kSlow = kTW * bk_slow_groups(P) * 1024;
@@ -91,13 +100,33 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave / CW, cw = wave % CW;
     const int r = lane & 15, G = lane >> 4;
-    // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD)
-    const int nwg = prm.tiles_m * prm.tiles_n;
-    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-    const int per = nwg >> 3, rem = nwg & 7;
-    const int vid = xcd * per + min(xcd, rem) + slot;
+    // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD); of experts: the tiles of one after the other, each in bands
+    int M = prm.M, tiles_m = prm.tiles_m, y_row0 = 0;
+    const uint8_t* fields[3] = {prm.fields[0], prm.fields[1], prm.fields[2]};
+    const RowParams* wparams = prm.wparams;
+    int vid;
+    if constexpr (kExperts) {
+        const ExpertUnits units(prm.g, kBM, prm.tiles_m);
+        const int nwg = units.total * prm.tiles_n, per = nwg >> 3, rem = nwg & 7;
+        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+        if (slot >= per + (xcd < rem ? 1 : 0)) return;   // (the grid is what there can be at most)
+        vid = xcd * per + min(xcd, rem) + slot;
+        const ExpertAt at = units.find(prm.g, kBM, vid / prm.tiles_n);
+        vid -= at.before * prm.tiles_n;
+        M = at.rows;
+        tiles_m = (at.rows + kBM - 1) / kBM;
+        y_row0 = at.first;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) fields[i] += (size_t)at.expert * prm.w_stride;
+        wparams = reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(wparams) + (size_t)at.expert * prm.w_stride);
+    } else {
+        const int nwg = prm.tiles_m * prm.tiles_n;
+        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+        const int per = nwg >> 3, rem = nwg & 7;
+        vid = xcd * per + min(xcd, rem) + slot;
+    }
     const int band = vid / (prm.band_m * prm.tiles_n), in_band = vid - band * prm.band_m * prm.tiles_n;
-    const int band_rows = min(prm.band_m, prm.tiles_m - band * prm.band_m);
+    const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
     const int m_blk = band * prm.band_m + in_band % band_rows, n_blk = in_band / band_rows;
     const int m0 = m_blk * kBM, n0 = n_blk * kBN, tile0 = n_blk * kTW;
     const int nsteps = prm.nsuper * 4;
@@ -119,9 +148,11 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
     for (int u = 0; u < kALoads; ++u) {
         const int row = 8 * (wave * kALoads + u) + (lane >> 3);
         const unsigned piece = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-        a_goff[u] = (unsigned)(min(m0 + row, prm.M - 1) - m0) * (unsigned)prm.lda + piece;
+        if constexpr (kExperts) a_goff[u] = (unsigned)moe_row_of(prm.g, y_row0 + min(m0 + row, M - 1)) * (unsigned)prm.lda + piece;
+        else a_goff[u] = (unsigned)(min(m0 + row, prm.M - 1) - m0) * (unsigned)prm.lda + piece;
     }
-    const uint8_t* a_tile = prm.a + (size_t)m0 * prm.lda;
+    const uint8_t* a_tile = prm.a;
+    if constexpr (!kExperts) a_tile += (size_t)m0 * prm.lda;
     // Chunks of W: as many loads from every wave, so that one count of outstanding loads holds for all (the last tile may be loaded twice).
     constexpr int kWLoads = (kTW + kWaves - 1) / kWaves, kChunks = bk_fast_chunks(P), kB0 = group_width(P, 0);
     int w_place[kWLoads], w_row[kWLoads];
@@ -130,7 +161,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
     for (int u = 0; u < kWLoads; ++u) {
         w_place[u] = min(u * kWaves + wave, kTW - 1);
         w_row[u] = min(tile0 + w_place[u], prm.ntiles - 1);
-        w_tile[u] = prm.fields[0] + (size_t)w_row[u] * (prm.nsuper * kB0) * 1024;
+        w_tile[u] = fields[0] + (size_t)w_row[u] * (prm.nsuper * kB0) * 1024;
     }
     constexpr int kLoads = kALoads + kWLoads * kChunks;
     auto load_piece = [&](int i, int step, const uint8_t* buf) {   // i-th load of a step
@@ -149,7 +180,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
                 constexpr int b = group_width(P, g);
 #pragma unroll
                 for (int u = 0; u < kWLoads; ++u)
-                    lds_load(prm.fields[g] + (size_t)w_row[u] * (prm.nsuper * b) * 1024, lane * 16 + (b == 2 ? step >> 1 : step >> 2) * 1024,
+                    lds_load(fields[g] + (size_t)w_row[u] * (prm.nsuper * b) * 1024, lane * 16 + (b == 2 ? step >> 1 : step >> 2) * 1024,
                              lds_addr(lds_slow) + (bk_slow_index(P, g) * kTW + w_place[u]) * 1024);
             }
         };
@@ -176,7 +207,8 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
 
     // the epilogue's records first: whatever waits for a later load waits for them
     for (int i = wave; i < kRecA + kRecW; i += kWaves) {
-        if (i >= kRecA) lds_load(prm.wparams, (unsigned)min(n0 + (i - kRecA) * 64 + lane, prm.N - 1) * 16u, lds_addr(par_w + (i - kRecA) * 64));
+        if (i >= kRecA) lds_load(wparams, (unsigned)min(n0 + (i - kRecA) * 64 + lane, prm.N - 1) * 16u, lds_addr(par_w + (i - kRecA) * 64));
+        else if constexpr (kExperts) lds_load(prm.aparams, (unsigned)moe_row_of(prm.g, y_row0 + min(m0 + i * 64 + lane, M - 1)) * 16u, lds_addr(par_a + i * 64));
         else lds_load(prm.aparams, (unsigned)min(m0 + i * 64 + lane, prm.M - 1) * 16u, lds_addr(par_a + i * 64));
     }
     load_slow(std::integral_constant<int, 0>{}, 0);
@@ -319,7 +351,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
         if constexpr (decltype(coded)::value) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const int m = min(wm0 + mt * 16 + r, prm.M - 1);
+                const int m = min(wm0 + mt * 16 + r, M - 1);
                 rq_scale[mt] = prm.rq.scale[m];
                 rq_zero[mt] = prm.rq.zero[m];
             }
@@ -366,7 +398,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
                     n = wn0 + (np + (G & 1)) * 16 + (G >> 1) * 8;
                     w4[0] = lo[0]; w4[1] = hi[0]; w4[2] = lo[1]; w4[3] = hi[1];
                 }
-                if (m >= prm.M || n >= prm.N) continue;
+                if (m >= M || n >= prm.N) continue;
                 if constexpr (decltype(coded)::value) {
                     uint32_t c8[2] = {0u, 0u};
 #pragma unroll
@@ -381,7 +413,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
                     }
                 }
                 if (!decltype(coded)::value || prm.y) {
-                    uint16_t* dst = prm.y + (size_t)m * prm.N + n;
+                    uint16_t* dst = prm.y + (size_t)(y_row0 + m) * prm.N + n;
                     if (two == 2) store_row_part8(dst, n, prm.N, w4[0], w4[1], w4[2], w4[3]);
                     else if (vec_ok) *reinterpret_cast<uint2*>(dst) = uint2{w4[0], w4[1]};
                     else {
@@ -393,7 +425,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams pr
             }
         }
     };
-    if (prm.rq.codes == nullptr) {                               // (the same for every thread, as is narrow_sums)
+    if (kExperts || prm.rq.codes == nullptr) {                   // (the same for every thread, as is narrow_sums)
         if (prm.narrow_sums) dequant(std::true_type{}, std::false_type{});
         else dequant(std::false_type{}, std::false_type{});
     } else {
@@ -427,6 +459,20 @@ static hipError_t block_launch(const BlockParams& prm, int shape, hipStream_t s)
     }
 }
 
+// Experts: 256 x 256 (p = 7: 192), 128 x 128 by four waves and 64 x 128 (shapes 0, 3, 4 above).
+template <int P>
+static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(prm.tiles_m * prm.tiles_n);
+    switch (shape) {
+        case 0: block_kernel<P, 2, 4, 8, P == 7 ? 3 : 4, 2, 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
+        case 3: block_kernel<P, 2, 2, 4, 4, P >= 4 ? 2 : 3, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        case 4: block_kernel<P, 1, 4, 4, 2, P >= 7 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
 #define ABQ_BLOCK_LAUNCH(P) hipError_t block_launch_p##P(const BlockParams& prm, int shape, hipStream_t s)
 ABQ_BLOCK_LAUNCH(1);
 ABQ_BLOCK_LAUNCH(2);
@@ -436,5 +482,15 @@ ABQ_BLOCK_LAUNCH(5);
 ABQ_BLOCK_LAUNCH(6);
 ABQ_BLOCK_LAUNCH(7);
 ABQ_BLOCK_LAUNCH(8);
+
+#define ABQ_BLOCK_EXPERTS_LAUNCH(P) hipError_t block_experts_launch_p##P(const BlockExpertParams& prm, int shape, hipStream_t s)
+ABQ_BLOCK_EXPERTS_LAUNCH(1);
+ABQ_BLOCK_EXPERTS_LAUNCH(2);
+ABQ_BLOCK_EXPERTS_LAUNCH(3);
+ABQ_BLOCK_EXPERTS_LAUNCH(4);
+ABQ_BLOCK_EXPERTS_LAUNCH(5);
+ABQ_BLOCK_EXPERTS_LAUNCH(6);
+ABQ_BLOCK_EXPERTS_LAUNCH(7);
+ABQ_BLOCK_EXPERTS_LAUNCH(8);
 
 }  // namespace abq

@@ -1,0 +1,8 @@
+// Products with experts' weights: the variants of 5-bit weights.
+#include "abq_block_kernels.h"
+#include "abq_moe_rows_kernels.h"
+
+namespace abq {
+ABQ_MOE_ROWS_LAUNCH(5) { return moe_rows_launch<5>(prm, R, MT, grid, s); }
+ABQ_BLOCK_EXPERTS_LAUNCH(5) { return block_experts_launch<5>(prm, shape, s); }
+}  // namespace abq

@@ -835,6 +835,122 @@ PyObject* lora_add(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject*
     END_HANDLE_TH_ERRORS
 }
 
+// ---- a layer of experts -----------------------------------------------------------------------------
+Signature<8> sig_moe_route{"abq_moe_route", 2, {"logits", "top", "bias", "sigmoid", "renormalize", "scale", "workspace", "out"}};
+PyObject* moe_route(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[8];
+    Operands t;
+    int T, E, top, ld, sigmoid, renormalize;
+    void* bp = nullptr;
+    double scale = 1.0;
+    if (!sig_moe_route.parse(args, nargs, kw, a) || !to_int(a[1], &top) || !truth(a[3], 0, &sigmoid) || !truth(a[4], 1, &renormalize)) return nullptr;
+    if (!is_none(a[5])) {
+        scale = PyFloat_AsDouble(a[5]);
+        if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    }
+    const at::Tensor* x = tensor(a[0]);
+    if (!x || !rows_cols(x, &T, &E)) return nullptr;
+    if (!x->is_cuda() || (x->scalar_type() != at::kHalf && x->scalar_type() != at::kFloat) || (E > 1 && x->stride(1) != 1)) return t.refuse(*x, "logits", "Half or Float, contiguous rows"), nullptr;
+    if (!fits_int(T > 1 ? x->stride(0) : E, &ld) || !t.same_device(*x, "logits")) return nullptr;
+    if (!is_none(a[2]) && !t.whole(a[2], "bias", at::kFloat, {E}, &bp)) return nullptr;
+    if (top < 1 || T < 1) return fail(ABQ_ERR_SHAPE, "abq_moe_route"), nullptr;
+    // (ids, weights, starts, order, places): the caller's, or new ones
+    Buffer out[5];
+    const at::ScalarType types[5] = {at::kInt, at::kFloat, at::kInt, at::kInt, at::kInt};
+    const char* names[5] = {"ids", "weights", "starts", "order", "places"};
+    const std::vector<int64_t> shapes[5] = {{T, top}, {T, top}, {(int64_t)E + 1}, {(int64_t)T * top}, {T, top}};
+    const bool given = !is_none(a[7]);
+    Py_ssize_t n;
+    if (given && !t.sequence(a[7], "out", 5, 5, &n)) return nullptr;
+    for (int i = 0; i < 5; ++i) {
+        out[i].wanted = !given;
+        if (given && !t.whole(PyTuple_GET_ITEM(a[7], i), names[i], types[i], shapes[i], &out[i].ptr)) return nullptr;
+    }
+    Workspace ws;
+    if (!t.workspace(a[6], abq_moe_route_workspace_bytes(T, E, top), &ws)) return nullptr;
+    if (!call_on("abq_moe_route", *t.on, [&] {
+            if (T > (1 << 22) || top > ABQ_MOE_MAX_TOP || top > E) return ABQ_ERR_SHAPE;   // (before anything of that size is allocated)
+            for (int i = 0; i < 5; ++i) out[i].make(shapes[i], types[i], *t.on);
+            void* wsp = ws.make(*t.on);
+            return abq_moe_route(T, E, top, x->data_ptr(), x->scalar_type() == at::kHalf ? 16 : 32, ld, (const float*)bp, sigmoid, renormalize, (float)scale, (int32_t*)out[0].ptr,
+                                 (float*)out[1].ptr, (int32_t*)out[2].ptr, (int32_t*)out[3].ptr, (int32_t*)out[4].ptr, wsp, ws.bytes, stream());
+        }))
+        return nullptr;
+    if (given) { Py_INCREF(a[7]); return a[7]; }
+    return pack({result(out[0]), result(out[1]), result(out[2]), result(out[3]), result(out[4])});
+    END_HANDLE_TH_ERRORS
+}
+
+Signature<13> sig_moe_gemm{"abq_moe_gemm", 8, {"p", "q", "N", "a_codes", "a_scale", "a_zero", "packed_w", "starts", "order", "top", "w_layout", "y", "workspace"}};
+PyObject* moe_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[13];
+    Operands t;
+    int n3[3], T, K, E, rows, blob, top = 1, layout = ABQ_LAYOUT_AUTO;
+    void *cp, *sp, *zp, *tp, *op = nullptr;
+    if (!sig_moe_gemm.parse(args, nargs, kw, a) || !to_ints(a, 3, n3) || (!is_none(a[9]) && !to_int(a[9], &top)) || (!is_none(a[10]) && !to_int(a[10], &layout))) return nullptr;
+    const int p = n3[0], q = n3[1], N = n3[2];
+    const at::Tensor* c = tensor(a[3]);
+    if (!c || !rows_cols(c, &T, &K) || !t.whole(a[3], "a_codes", at::kByte, c->sizes(), &cp) || !t.whole(a[4], "a_scale", at::kFloat, {T}, &sp) || !t.whole(a[5], "a_zero", at::kInt, {T}, &zp)) return nullptr;
+    const at::Tensor* w = tensor(a[6]);
+    if (!w || !rows_cols(w, &E, &blob)) return nullptr;
+    if (!w->is_cuda() || w->scalar_type() != at::kByte || w->stride(1) != 1) return t.refuse(*w, "packed_w", "Byte, contiguous rows"), nullptr;
+    if (!t.same_device(*w, "packed_w")) return nullptr;
+    if (!t.whole(a[7], "starts", at::kInt, {(int64_t)E + 1}, &tp)) return nullptr;
+    rows = T;
+    if (!is_none(a[8])) {
+        const at::Tensor* o = tensor(a[8]);
+        if (!o) return nullptr;
+        if (o->dim() != 1) return PyErr_SetString(PyExc_ValueError, "order: a tensor of one dimension"), nullptr;
+        if (!fits_int(o->size(0), &rows) || !t.whole(a[8], "order", at::kInt, o->sizes(), &op)) return nullptr;
+    }
+    const size_t need_w = abq_packed_weight_bytes(p, N, K, layout);
+    if (need_w && (size_t)blob < need_w) return fail(ABQ_ERR_SIZE, "abq_moe_gemm"), nullptr;   // (a blob's own end is the last expert's)
+    const int64_t stride = E > 1 ? w->stride(0) : blob;
+    if (stride < 0 || stride % 16 != 0) return fail(ABQ_ERR_ALIGN, "abq_moe_gemm"), nullptr;
+    Buffer y;
+    Workspace ws;
+    if (!t.output(a[11], "y", rows, N, &y) || !t.workspace(a[12], abq_moe_gemm_workspace_bytes(p, q, rows, N, K, T, E), &ws)) return nullptr;
+    if (!call_on("abq_moe_gemm", *t.on, [&] {
+            if (rows < 1 || N < 1) return ABQ_ERR_SHAPE;   // (sizes that no tensor has)
+            uint16_t* yp = y.half(rows, N, *t.on);
+            void* wsp = ws.make(*t.on);
+            return abq_moe_gemm(p, q, rows, N, K, T, E, top, (const uint8_t*)cp, (const float*)sp, (const int32_t*)zp, w->data_ptr(), (size_t)stride, layout, (const int32_t*)tp,
+                                (const int32_t*)op, yp, wsp, ws.bytes, stream());
+        }))
+        return nullptr;
+    return result(a[11], y);
+    END_HANDLE_TH_ERRORS
+}
+
+Signature<5> sig_moe_combine{"abq_moe_combine", 3, {"y", "places", "weights", "add", "out"}};
+PyObject* moe_combine(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw)
+{
+    HANDLE_TH_ERRORS
+    PyObject* a[5];
+    Operands t;
+    int rows, N, ldy, T, top, ldadd = 0, ldout;
+    void *yp, *pp, *wp, *ap = nullptr;
+    if (!sig_moe_combine.parse(args, nargs, kw, a) || !t.rows(a[0], "y", &rows, &N, &ldy, &yp)) return nullptr;
+    const at::Tensor* places = tensor(a[1]);
+    if (!places || !rows_cols(places, &T, &top) || !t.whole(a[1], "places", at::kInt, places->sizes(), &pp) || !t.whole(a[2], "weights", at::kFloat, places->sizes(), &wp)) return nullptr;
+    if (!is_none(a[3]) && !t.rows_of(a[3], "add", T, N, &ldadd, &ap)) return nullptr;
+    Buffer out;
+    out.wanted = is_none(a[4]);
+    ldout = N;
+    if (!out.wanted && !t.rows_of(a[4], "out", T, N, &ldout, &out.ptr)) return nullptr;
+    if (!call_on("abq_moe_combine", *t.on, [&] {
+            uint16_t* o = out.half(T, N, *t.on);
+            return abq_moe_combine(T, N, rows, top, (const uint16_t*)yp, ldy, (const int32_t*)pp, (const float*)wp, (const uint16_t*)ap, ldadd, o, ldout, stream());
+        }))
+        return nullptr;
+    return result(a[4], out);
+    END_HANDLE_TH_ERRORS
+}
+
 // binding.py hands over its exception class, make_problems and ctypes.Array once
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -888,6 +1004,19 @@ PyMethodDef methods[] = {
     ABQ_METHOD("abq_lora_add", lora_add,
                "abq_lora_add(x, ids, a, b, scale, y, out=None, workspace=None)\n--\n\nx float16 [M,K], ids int32 [M], a float16 [adapters, rank, K], b float16 [adapters, N, rank], scale float32 [adapters],\n"
                "y float16 [M,N] -> out = y + scale[id] * B[id] (A[id] x) float16 [M,N] (rows with an id outside 0..adapters-1: y)."),
+    ABQ_METHOD("abq_moe_route", moe_route,
+               "abq_moe_route(logits, top, bias=None, sigmoid=False, renormalize=True, scale=1.0, workspace=None, out=None)\n--\n\n"
+               "logits float16 or float32 [tokens, experts], bias float32 [experts] (steers the choice alone)\n"
+               "-> (ids int32 [tokens, top], weights float32 [tokens, top], starts int32 [experts + 1], order int32 [tokens * top], places int32 [tokens, top]):\n"
+               "the experts of each token and their weights, and the rows (token * top + choice) sorted by expert.  out: a tuple of five such tensors."),
+    ABQ_METHOD("abq_moe_gemm", moe_gemm,
+               "abq_moe_gemm(p, q, N, a_codes, a_scale, a_zero, packed_w, starts, order=None, top=1, w_layout=0, y=None, workspace=None)\n--\n\n"
+               "a_codes uint8 [tokens,K], a_scale float32 [tokens], a_zero int32 [tokens], packed_w uint8 [experts, bytes] (abq_pack_experts), starts int32 [experts + 1]\n"
+               "-> y float16 [rows,N]: rows starts[e] .. starts[e+1] - 1 times the weights of expert e; row r takes codes order[r] // top, or r without order."),
+    ABQ_METHOD("abq_moe_combine", moe_combine,
+               "abq_moe_combine(y, places, weights, add=None, out=None)\n--\n\n"
+               "y float16 [rows,N], places int32 [tokens, top] (-1: none), weights float32 [tokens, top], add float16 [tokens,N] -> out = add + sum_j weights[:, j] * y[places[:, j]]\n"
+               "float16 [tokens,N]."),
     {"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, "init(error, make_problems, array)"},
     {nullptr, nullptr, 0, nullptr}};
 
@@ -899,7 +1028,7 @@ PyMODINIT_FUNC PyInit_abq_native()
 {
     if (!(sig_quant_pack.intern() && sig_pack_codes.intern() && sig_f4_pack.intern() && sig_rmsnorm.intern() && sig_add_rmsnorm.intern() && sig_silu.intern() &&
           sig_gemm.intern() && sig_act_codes.intern() && sig_requant.intern() && sig_static.intern() && sig_f4_gemm.intern() && sig_grouped.intern() && sig_kv_append.intern() && sig_kv_read.intern() &&
-          sig_attn.intern() && sig_lora.intern()))
+          sig_attn.intern() && sig_lora.intern() && sig_moe_route.intern() && sig_moe_gemm.intern() && sig_moe_combine.intern()))
         return nullptr;
     return PyModule_Create(&module_def);
 }

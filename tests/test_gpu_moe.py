@@ -1,0 +1,353 @@
+"""A layer of experts on the GPU against its 64-bit form: router, products with the experts' weights, weighted sum, and all of it in a run."""
+import pytest
+import torch
+
+from moe_reference import INF, combined, gemm, groups, routed
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- router ----------------------------------------------------------------------------------------
+def check_route(abq, logits, top, **kw):
+    on = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+    got = [t.cpu() for t in abq.abq_moe_route(logits.cuda(), top, **on)]
+    want = routed(logits, top, **kw)
+    for name, g, w in zip(("ids", "starts", "order", "places"), (got[0], got[2], got[3], got[4]), (want[0], want[2], want[3], want[4])):
+        assert torch.equal(g.long(), w), f"{name}: {int((g.long() != w).sum())} of {g.numel()} differ"
+    off = (got[1].double() - want[1]).abs()
+    assert (off <= want[5]).all(), f"weights: off by {float((off / want[5]).nan_to_num().max()):.2f} bounds"
+    return got
+
+
+def some_logits(T, E, half, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, E, generator=g) * 2
+    return x.half() if half else x
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("E", [1, 2, 7, 8, 16, 17, 33, 60, 64, 100, 128, 160, 256, 257, 512, 513, 1000, 1024])
+def test_experts(abq, E, half):
+    g = torch.Generator().manual_seed(E)
+    for T in (1, 37):
+        x = some_logits(T, E, half, E + T)
+        for top in sorted({1, min(E, 3), min(E, 8), min(E, 16)}):
+            check_route(abq, x, top)
+        check_route(abq, x, min(E, 5), bias=torch.rand(E, generator=g) - 0.5, sigmoid=True, scale=2.5)
+        check_route(abq, x, min(E, 5), bias=(torch.rand(E, generator=g) - 0.5) * 0.1)
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 63, 64, 65, 255, 256, 257, 300, 1000, 4099, 16385])
+def test_tokens(abq, T):
+    """One launch and two, chunks of 64 and more, whole and with a rest."""
+    check_route(abq, some_logits(T, 16, T % 2 == 0, T), 2)
+    if T < 5000:
+        check_route(abq, some_logits(T, 130, T % 2 == 1, T), 7, renormalize=False)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("half", [False, True])
+def test_scores(abq, sigmoid, renormalize, biased, half):
+    x = some_logits(70, 48, half, 5)
+    x[3], x[4], x[5, ::2] = x[3] * 20, x[4] - 200, x[5, ::2] - 60000   # sharp rows; rows whose sigmoids underflow
+    bias = torch.rand(48, generator=torch.Generator().manual_seed(1)) - 0.5 if biased else None
+    check_route(abq, x, 6, bias=bias, sigmoid=sigmoid, renormalize=renormalize, scale=1.75)
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("kw", [{}, dict(sigmoid=True), dict(sigmoid=True, bias=torch.zeros(64)), dict(bias=torch.zeros(64))])
+def test_ties_go_to_the_lowest_expert(abq, half, kw):
+    x = torch.randint(-2, 3, (300, 64), generator=torch.Generator().manual_seed(3)).float()
+    x[7], x[8, ::2] = 0.0, -0.0
+    x[9] = -0.0
+    check_route(abq, x.half() if half else x, 8, **kw)
+
+
+@pytest.mark.parametrize("T", [40, 500])
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("kw", [{}, dict(renormalize=False), dict(sigmoid=True, bias=torch.linspace(-0.3, 0.3, 24)), dict(bias=torch.linspace(-0.3, 0.3, 24), renormalize=False)])
+def test_experts_that_are_not_there(abq, T, half, kw):
+    """Padding rows, rows with fewer experts than choices, NaN among the logits; the lowest value of the type is a value."""
+    x = some_logits(T, 24, half, 9)
+    x[::5] = -INF
+    x[1, 2:], x[2, 1:], x[3, :20] = -INF, -INF, -INF
+    x[4, ::3] = float("nan")
+    x[6] = float("nan")
+    x[7, :] = torch.finfo(x.dtype).min
+    x[8, 3:] = torch.finfo(x.dtype).min
+    got = check_route(abq, x, 4, **kw)
+    assert int((got[0][0] == -1).sum()) == 4 and (got[1][0] == 0).all() and int((got[0][2] >= 0).sum()) == 1
+    check_route(abq, torch.full((T, 24), -INF, dtype=x.dtype), 3, **kw)
+
+
+def test_a_bias_takes_experts_out(abq):
+    bias = torch.zeros(12)
+    bias[::2] = -INF
+    got = check_route(abq, some_logits(50, 12, True), 3, bias=bias, sigmoid=True)
+    assert (got[0] % 2 == 1).all()
+
+
+def test_strides_and_given_outputs(abq):
+    wide = torch.randn(90, 77, generator=torch.Generator().manual_seed(1)).cuda()
+    for x in (wide[:, :33], wide.half()[:, 40:73]):
+        if x.data_ptr() % 16:
+            x = x.clone()
+        want = abq.abq_moe_route(x.contiguous(), 4)
+        out = tuple(torch.full_like(t, -7) for t in want)
+        assert abq.abq_moe_route(x, 4, out=out) is out
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_every_token_to_the_same_experts(abq):
+    x = torch.zeros(3000, 32)
+    x[:, 5], x[:, 30] = 2.0, 1.0
+    got = check_route(abq, x, 2)
+    assert got[2].tolist() == [0] * 6 + [3000] * 25 + [6000] * 2
+
+
+# ---- products --------------------------------------------------------------------------------------
+def layer(p, q, E, N, K, T, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    u = lambda *s: torch.rand(s, generator=g)
+    i = lambda top, *s: torch.randint(0, top, s, generator=g)
+    return {"a": (i(256, T, K).to(torch.uint8), (u(T) + 0.5) * (4.0 / 2**q), i(2**q, T).to(torch.int32)),   # (bits above q are dropped)
+            "w": (i(2**p, E, N, K).to(torch.uint8), (u(E, N) + 0.5) * (2.0 / (K**0.5 * 2**p)), i(2**p, E, N).to(torch.int32))}
+
+
+POISON = 0x7E2A   # (a NaN's bits)
+
+
+def check_gemm(abq, p, q, counts, N, K, top=0, T=0, seed=0, behind=0, layout=0):
+    """counts: rows of each expert; top 0: without order.  Every bit of every row, and the rows behind the last one as they were."""
+    used = sum(counts)
+    rows, E = used + behind, len(counts)
+    g = torch.Generator().manual_seed(seed + 1)
+    if top:
+        T = T or -(-rows // top)
+        order = torch.cat([torch.randint(0, T * top, (used,), generator=g), torch.full((behind,), -1)]).to(torch.int32)
+    else:
+        T, order = rows, None
+    s = layer(p, q, E, N, K, T, seed)
+    starts = groups(counts)
+    w = abq.abq_pack_experts(p, *(t.cuda() for t in s["w"]), layout=layout)
+    y = torch.full((rows, N), POISON, dtype=torch.int16, device="cuda").view(torch.float16)
+    abq.abq_moe_gemm(p, q, N, *(t.cuda() for t in s["a"]), w, starts.cuda(), order=None if order is None else order.cuda(), top=max(top, 1), w_layout=layout, y=y)
+    got, want = y.cpu().view(torch.int16), gemm(*s["a"], *s["w"], p, q, starts, order, max(top, 1), rows)
+    want = torch.where(torch.arange(rows)[:, None] < used, want.view(torch.int16), torch.tensor(POISON, dtype=torch.int16))
+    bad = (got != want).nonzero()
+    assert not len(bad), f"{len(bad)} of {got.numel()} differ, rows {sorted(set(bad[:, 0].tolist()))[:8]}, columns {sorted(set(bad[:, 1].tolist()))[:8]}"
+
+
+@pytest.mark.parametrize("q", [1, 4, 7, 8])
+@pytest.mark.parametrize("p", range(1, 9))
+def test_widths(abq, p, q):
+    """Every weight width on every kernel: few rows (one and two tiles of rows, one to four super-chunks a wave), 64, 128 and 256 rows a workgroup."""
+    check_gemm(abq, p, q, [1, 0, 5, 16, 2], 80, 1024, top=2, seed=p)
+    check_gemm(abq, p, q, [1, 0, 5, 16, 2], 48, 8704, seed=p)
+    check_gemm(abq, p, q, [3, 1], 32, 14336, top=2, seed=p)
+    check_gemm(abq, p, q, [20, 32, 17], 96, 512, top=3, seed=p)
+    check_gemm(abq, p, q, [20, 32, 17], 64, 6656, seed=p)
+    check_gemm(abq, p, q, [70, 33, 64, 0], 144, 640, top=2, seed=p)
+    check_gemm(abq, p, q, [140, 0, 128, 97], 272, 512, seed=p)
+    check_gemm(abq, p, q, [300, 256], 528, 1024, top=2, seed=p)
+
+
+@pytest.mark.parametrize("K", [1, 7, 15, 16, 17, 31, 63, 64, 65, 100, 127, 500, 511, 512, 513, 1000, 1408, 2047, 4095, 5121, 8193, 12289, 16383])
+@pytest.mark.parametrize("top", [0, 3])
+def test_lengths_that_divide_nothing(abq, K, top):
+    for p, q in ((4, 8), (3, 5), (8, 8)):
+        check_gemm(abq, p, q, [2, 0, 1, 9], 40, K, top=top, seed=K)
+        check_gemm(abq, p, q, [40, 60], 40, K, top=top, seed=K)
+    check_gemm(abq, 4, 8, [1], 16, K, top=top)
+
+
+@pytest.mark.parametrize("N", [1, 2, 7, 15, 16, 17, 33, 127, 129, 255, 257, 1003])
+def test_columns_that_divide_nothing(abq, N):
+    for counts in ([1], [3, 0, 12], [40, 25], [100, 150], [500, 230]):
+        check_gemm(abq, 4, 8, counts, N, 320, top=2, seed=N)
+        check_gemm(abq, 6, 6, counts, N, 200, seed=N, behind=3)
+
+
+@pytest.mark.parametrize("counts", [[0, 0, 0, 5], [5, 0, 0, 0], [0] * 70 + [3] + [0] * 60 + [1, 2], [1] * 64, [1] * 65, [17] + [1] * 40, [100] + [1] * 12, [1000] + [0] * 40 + [1] * 3,
+                                    [1] * 300, [0] * 1023 + [4], [2] * 1024, [16] * 9, [65, 0, 64, 63], [128, 129, 1], [257, 255, 0, 256], [600] + [0] * 100 + [8]])
+def test_ragged_groups(abq, counts):
+    check_gemm(abq, 4, 8, counts, 48, 192, top=2, seed=len(counts), behind=5)
+    check_gemm(abq, 2, 8, counts, 272 if len(counts) < 200 else 16, 64, seed=len(counts))
+
+
+def test_no_rows_at_all(abq):
+    check_gemm(abq, 4, 8, [0] * 8, 64, 256, top=2, behind=16)
+    check_gemm(abq, 4, 8, [0] * 8, 64, 256, top=2, behind=700)
+
+
+def test_blobs_that_hold_planes_too(abq):
+    check_gemm(abq, 4, 8, [3, 5], 64, 512, top=2, layout=abq.ABQ_LAYOUT_BOTH)
+    check_gemm(abq, 5, 8, [90, 50], 64, 512, top=2, layout=abq.ABQ_LAYOUT_BOTH)
+
+
+@pytest.mark.parametrize("p,q,counts,N,K", [(4, 8, [1, 1], 11008, 4096), (2, 8, [3, 9, 0, 1], 4096, 11008), (8, 8, [30, 22], 2048, 1408), (6, 6, [90, 75], 1003, 4096), (4, 4, [500, 612], 2048, 4096)])
+def test_same_bits_as_the_products_of_one_expert(abq, p, q, counts, N, K):
+    E, rows = len(counts), sum(counts)
+    s = {k: [t.cuda() for t in v] for k, v in layer(p, q, E, N, K, rows).items()}
+    s["a"][0] &= 2**q - 1
+    w = abq.abq_pack_experts(p, *s["w"])
+    got = abq.abq_moe_gemm(p, q, N, *s["a"], w, groups(counts).cuda())
+    at = 0
+    for e, n in enumerate(counts):
+        if n:
+            one = abq.abq_gemm_act_codes(p, q, n, N, K, *(t[at:at + n].clone() for t in s["a"]), w[e], 0)[0]
+            assert torch.equal(got[at:at + n].view(torch.int16), one.view(torch.int16))
+        at += n
+
+
+def test_arrays_that_name_nothing_touch_nothing_else(abq):
+    """Starts that do not ascend or point outside, order entries that name no row: rows without an expert, and what lies around Y, stay."""
+    N, K, T, E = 64, 256, 24, 6
+    s = layer(4, 8, E, N, K, T)
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    a = [t.cuda() for t in s["a"]]
+    for rows in (48, 640):
+        for starts in ([0, 5, -3, 1 << 30, 7, 40, 9], [-5, -4, -3, -2, -1, 0, 0], [1 << 30] * 7, [40, 30, 20, 10, 5, 2, 1], [0, rows, 0, rows, 0, rows, 0]):
+            around = torch.full((rows + 32, N), POISON, dtype=torch.int16, device="cuda")
+            y = around[16:16 + rows].view(torch.float16)
+            order = torch.randint(-(1 << 31), (1 << 31) - 1, (rows,), dtype=torch.int64).to(torch.int32).cuda()
+            abq.abq_moe_gemm(4, 8, N, *a, w, torch.tensor(starts, dtype=torch.int32).cuda(), order=order, top=2, y=y)
+            assert (around[:16] == POISON).all() and (around[16 + rows:] == POISON).all()
+            mine = torch.zeros(rows, dtype=torch.bool)
+            for lo, hi in zip(starts, starts[1:]):
+                mine[min(max(lo, 0), rows):min(max(hi, 0), rows)] = True
+            assert (y.view(torch.int16).cpu()[~mine] == POISON).all()
+
+
+def test_graphs_serve_whatever_the_arrays_hold_later(abq):
+    """Router, products and sum captured once; replayed for other logits, other codes."""
+    T, E, top, N, K = 40, 16, 3, 96, 512
+    s = layer(4, 8, E, N, K, T)
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    a = [t.cuda() for t in s["a"]]
+    x = some_logits(T, E, True).cuda()
+
+    def step():
+        ids, weights, starts, order, places = abq.abq_moe_route(x, top)
+        y = abq.abq_moe_gemm(4, 8, N, *a, w, starts, order=order, top=top)
+        return abq.abq_moe_combine(y, places, weights)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in range(4):
+        x.copy_(some_logits(T, E, True, seed + 10))
+        if seed == 2:
+            x[:, 1:] = -INF   # every token to one expert, the other choices none
+        a[0].copy_(layer(4, 8, 1, 16, K, T, seed)["a"][0])
+        graph.replay()
+        got = out.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, step())
+
+
+def test_two_streams_at_once(abq):
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    s = layer(4, 8, 8, 256, 1024, 300)
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    a = [t.cuda() for t in s["a"]]
+    x = some_logits(300, 8, False).cuda()
+
+    def step():
+        ids, weights, starts, order, places = abq.abq_moe_route(x, 2)
+        return abq.abq_moe_combine(abq.abq_moe_gemm(4, 8, 256, *a, w, starts, order=order, top=2), places, weights)
+
+    want = step()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for stream in (one, two):
+            with torch.cuda.stream(stream):
+                got.append(step())
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
+# ---- weighted sum ----------------------------------------------------------------------------------
+def check_combine(abq, T, top, N, rows, seed=0, add=True, missing=0.1):
+    g = torch.Generator().manual_seed(seed)
+    y = torch.randn(rows, N, generator=g).half()
+    places = torch.randint(0, rows, (T, top), generator=g).to(torch.int32)
+    places[torch.rand(T, top, generator=g) < missing] = -1
+    weights = torch.rand(T, top, generator=g)
+    base = torch.randn(T, N, generator=g).half() if add else None
+    got = abq.abq_moe_combine(y.cuda(), places.cuda(), weights.cuda(), add=base.cuda() if add else None).cpu()
+    want, bound = combined(y, places, weights, base)
+    off = (got.double() - want).abs()
+    assert (off <= bound).all(), f"{int((off > bound).sum())} of {off.numel()} off"
+
+
+@pytest.mark.parametrize("N", [1, 2, 7, 8, 9, 64, 100, 2047, 2048, 2049, 4096, 5121])
+@pytest.mark.parametrize("top", [1, 2, 3, 6, 8, 16, 33])
+def test_sums(abq, N, top):
+    for T in (1, 5):
+        check_combine(abq, T, top, N, 3 * T + 1, seed=N, add=bool(top % 2))
+    check_combine(abq, 130, top, N, 64, seed=top)
+
+
+def test_choices_that_are_none(abq):
+    y = torch.full((4, 40), float("nan"), dtype=torch.float16).cuda()
+    y[2] = 1.5
+    places = torch.tensor([[-1, -1], [2, -1], [4, 2], [-(1 << 31), (1 << 31) - 1]], dtype=torch.int32).cuda()
+    weights = torch.full((4, 2), 2.0).cuda()
+    weights[0] = float("nan")
+    assert abq.abq_moe_combine(y, places, weights).cpu()[:, 7].tolist() == [0.0, 3.0, 3.0, 0.0]
+    add = torch.full((4, 40), -0.5, dtype=torch.float16).cuda()
+    assert abq.abq_moe_combine(y, places, weights, add=add).cpu()[:, 39].tolist() == [-0.5, 2.5, 2.5, -0.5]
+    y[2, 3], y[2, 4] = INF, 60000.0
+    out = abq.abq_moe_combine(y, places, weights).cpu()
+    assert out[1, 3] == INF and out[1, 4] == INF and out[0, 3] == 0
+
+
+def test_sums_in_place_and_in_columns(abq):
+    g = torch.Generator().manual_seed(4)
+    y, places, weights = torch.randn(50, 100, generator=g).half().cuda(), torch.randint(0, 50, (20, 4), generator=g).to(torch.int32).cuda(), torch.rand(20, 4, generator=g).cuda()
+    add = torch.randn(20, 100, generator=g).half().cuda()
+    want = abq.abq_moe_combine(y, places, weights, add=add)
+    wide = torch.zeros(50, 333, dtype=torch.float16, device="cuda")
+    wide[:, 8:108], wide[:20, 128:228] = y, add
+    out = torch.full((20, 211), 7.0, dtype=torch.float16, device="cuda")
+    abq.abq_moe_combine(wide[:, 8:108], places, weights, add=wide[:20, 128:228], out=out[:, 16:116])
+    assert torch.equal(out[:, 16:116], want) and (out[:, :16] == 7).all() and (out[:, 116:] == 7).all()
+    assert abq.abq_moe_combine(y, places, weights, add=add, out=add) is add and torch.equal(add, want)
+
+
+# ---- a run of them ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,E,top,D,F,p,q", [(1, 8, 2, 512, 1024, 4, 8), (7, 16, 4, 520, 264, 2, 8), (33, 8, 2, 1024, 512, 6, 6), (300, 12, 3, 256, 384, 8, 8), (700, 4, 2, 512, 768, 4, 4)])
+def test_a_layer_of_experts(abq, T, E, top, D, F, p, q):
+    """Norm with its quantizer, router, gate and up, SiLU with its quantizer, down, weighted sum on the residual; every step against its own
+    64-bit form on what the steps before it gave, some of the tokens padding."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn(T, D, generator=g).half()
+    gamma = torch.ones(D).half()
+    logits = torch.randn(T, E, generator=g).half()
+    if T > 5:
+        logits[::4] = -INF
+    up, gate, down = layer(p, q, E, F, D, 1, 1)["w"], layer(p, q, E, F, D, 1, 2)["w"], layer(p, q, E, D, F, 1, 3)["w"]
+    w = [abq.abq_pack_experts(p, *(t.cuda() for t in m)) for m in (gate, up, down)]
+    codes, scale, zero, _ = abq.abq_rmsnorm_quant_act(q, x.cuda(), gamma.cuda(), 1e-5)
+    ids, weights, starts, order, places = abq.abq_moe_route(logits.cuda(), top)
+    gu = [abq.abq_moe_gemm(p, q, F, codes, scale, zero, m, starts, order=order, top=top) for m in w[:2]]
+    used = int(starts[-1])
+    for m, got in zip((gate, up), gu):
+        want = gemm(codes.cpu(), scale.cpu(), zero.cpu(), *m, p, q, starts.cpu(), order.cpu(), top, T * top)
+        assert torch.equal(got.cpu()[:used].view(torch.int16), want[:used].view(torch.int16))
+    hc, hs, hz, _ = abq.abq_silu_mul_quant_act(q, *gu)
+    y = abq.abq_moe_gemm(p, q, D, hc, hs, hz, w[2], starts)
+    want = gemm(hc.cpu(), hs.cpu(), hz.cpu(), *down, p, q, starts.cpu(), None, 1, T * top)
+    assert torch.equal(y.cpu()[:used].view(torch.int16), want[:used].view(torch.int16))
+    out = abq.abq_moe_combine(y, places, weights, add=x.cuda()).cpu()
+    full, bound = combined(y.cpu(), places.cpu(), weights.cpu(), x)
+    assert ((out.double() - full).abs() <= bound).all()
+    if T > 5:
+        assert torch.equal(out[::4], x[::4])   # padding: the residual
+    assert int((ids >= 0).sum()) == used
