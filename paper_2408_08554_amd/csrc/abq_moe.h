@@ -51,6 +51,7 @@ struct MoeRowsParams {
     int oa, ow;
     uint32_t a_mask;
     int kparts, tgroups;      // waves of a workgroup: parts of K, tiles side by side
+    int batch;                // tiles between two barriers
     int groups_n;             // tile groups of an expert
     int most;                 // groups of 16 MT rows there can be
 };
@@ -62,8 +63,7 @@ struct ExpertAt { int expert, before, first, rows; };   // the expert, the units
 
 __device__ __forceinline__ void moe_expert_rows(const MoeGroups& g, int e, int* first, int* rows)
 {
-    const bool there = e < g.experts;
-    const int a = there ? g.starts[e] : 0, b = there ? g.starts[e + 1] : 0;
+    const int a = g.starts[min(e, g.experts)], b = g.starts[min(e + 1, g.experts)];   // (no expert: none between them)
     const int lo = min(max(a, 0), g.rows), hi = min(max(b, 0), g.rows);
     *first = lo;
     *rows = max(hi - lo, 0);
@@ -116,11 +116,9 @@ struct ExpertUnits {
     }
 };
 
-// Row of A of a sorted row (an entry of `order` that names none takes the nearest there is).
-__device__ __forceinline__ int moe_row_of(const MoeGroups& g, int row)
-{
-    if (!g.order) return min(row, g.tokens - 1);
-    return min(max(g.order[row], 0) / g.top, g.tokens - 1);
-}
+// Row of A of a sorted row (an entry of `order` that names none takes the nearest there is): what there is to load, and what it says.
+__device__ __forceinline__ int moe_order(const MoeGroups& g, int row) { return g.order ? g.order[row] : row; }
+__device__ __forceinline__ int moe_row(const MoeGroups& g, int entry) { return min((int)((unsigned)max(entry, 0) / (unsigned)g.top), g.tokens - 1); }
+__device__ __forceinline__ int moe_row_of(const MoeGroups& g, int row) { return moe_row(g, moe_order(g, row)); }
 
 }  // namespace abq

@@ -424,6 +424,7 @@ hipError_t launch_moe_gemm(const MoeGemmArgs& g, const WeightLayout& W, hipStrea
         prm.ow = g.p == 8 ? 128 : 0;
         prm.a_mask = (uint32_t)((1 << g.q) - 1) * 0x01010101u;
         prm.kparts = pl.kparts; prm.tgroups = pl.tgroups;
+        prm.batch = pl.kparts >= 4 ? moe_batch(pl.MT) : 2;
         prm.groups_n = (W.NT + pl.tgroups - 1) / pl.tgroups;
         prm.most = most_groups(g.rows, g.experts, 16 * pl.MT);
         const int waves = pl.kparts * pl.tgroups, room = moe_max_waves(g.p, pl.R, pl.MT);   // (waves a unit holds)

@@ -11,6 +11,8 @@
 #include "abq_moe.h"
 #include "abq_rows.h"
 
+#include <atomic>
+
 namespace abq {
 
 typedef int mv4i __attribute__((ext_vector_type(4)));
@@ -82,28 +84,53 @@ __host__ __device__ constexpr int moe_max_waves(int P, int R, int MT)
     return R == 1 ? 16 : (R == 2 ? (P <= 6 ? 12 : 0) : (R == 3 ? (P >= 7 ? 8 : 0) : (R == 4 && P <= 4 ? 8 : 0)));
 }
 
+// Tiles in flight.
+__host__ __device__ constexpr int moe_depth(int P, int R, int MT)
+{
+    return P * R <= (MT == 1 ? 4 : 4) ? 2 : 1;
+}
+
+// Every wave's LDS accesses are done; loads stay in flight (a workgroup fence would wait for them).
+__device__ __forceinline__ void moe_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles between two barriers, at most: their parts of K meet in LDS together, and the waves share the work of adding them up.
+__host__ __device__ constexpr int moe_batch(int MT) { return MT == 1 ? 4 : 2; }
+// LDS: [2][batch][waves][MT][64] parts of tiles, [3][tgroups][64] channels' parameters.
+static size_t moe_rows_lds_bytes(const MoeRowsParams& prm, int MT) { return (size_t)(2 * prm.batch * prm.kparts * MT + 3) * prm.tgroups * 1024; }
+
 template <int P, int R, int MT>
 __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(MoeRowsParams prm)
 {
-    constexpr int kMax = moe_max_waves(P, R, MT);
-    __shared__ __align__(16) mv4i red[2][kMax][MT][64];
-    __shared__ int32_t part_sum[kMax][16 * MT];
+    constexpr int D = moe_depth(P, R, MT);
+    extern __shared__ __align__(16) mv4i lds[];
+    __shared__ int32_t row_sum[2][16 * MT];
     __shared__ __align__(16) RowParams par_a[16 * MT];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, G = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tg = wave / prm.kparts, kpart = wave - tg * prm.kparts;   // (blockDim = 64 kparts tgroups)
-    const int k0 = kpart * R * kSuperK;
+    const int k0 = kpart * R * kSuperK, waves = prm.kparts * prm.tgroups;
+    mv4i* const red = lds;                                               // part of tile b, buffer f: at ((f batch + b) waves + wave) MT 64
+    mv4i* const par_w = lds + 2 * prm.batch * waves * MT * 64;
 
     const ExpertUnits units(prm.g, 16 * MT, prm.most);
     // this workgroup's run: all units are dealt out evenly
-    const int64_t all = (int64_t)units.total * prm.groups_n;
-    int64_t u = all * blockIdx.x / gridDim.x;
-    const int64_t end = all * (blockIdx.x + 1) / gridDim.x;
+    const unsigned all = (unsigned)units.total * (unsigned)prm.groups_n, per = all / gridDim.x, rest = all - per * gridDim.x;   // (below 2^30)
+    unsigned u = blockIdx.x * per + min(blockIdx.x, rest);
+    const unsigned end = u + per + (blockIdx.x < rest ? 1u : 0u);
     const uint32_t flip = prm.oa ? 0x80808080u : 0u;
+    if (tid < 16 * MT) row_sum[0][tid] = 0;
+    int sums_at = 0, buf = 0, par_at = 0;   // buffers in turn: the runs' row sums, the batches' parts, their parameters
 
     while (u < end) {
-        const int block = (int)(u / prm.groups_n), g0 = (int)(u - (int64_t)block * prm.groups_n);
-        const int count = (int)min(end - u, (int64_t)(prm.groups_n - g0));
+        const int block = (int)(u / (unsigned)prm.groups_n), g0 = (int)u - block * prm.groups_n;
+        const int count = min((int)(end - u), prm.groups_n - g0);
         const ExpertAt at = units.find(prm.g, 16 * MT, block);
         const int local = (block - at.before) * 16 * MT;
         const int row0 = at.first + local, nrow = min(max(at.rows - local, 0), 16 * MT);
@@ -111,14 +138,49 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
         const RowParams* wparams = reinterpret_cast<const RowParams*>(blob + prm.off_params);
         u += count;
 
-        // ---- A: lane (r, G) holds bytes 16 G .. of slice s of rows r, r + 16; rows past the group's are its last one again.  Vectors past a row's
+        // ---- loads.  The rows' numbers first, then the weights of the run's first tiles, which need the expert alone, then what waits for the numbers.
+        int entry[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) entry[mt] = moe_order(prm.g, min(row0 + min(16 * mt + r, max(nrow - 1, 0)), prm.g.rows - 1));
+        const int par_entry = moe_order(prm.g, min(row0 + min(tid & (16 * MT - 1), max(nrow - 1, 0)), prm.g.rows - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        mv4i w[D][R][P];
+        // (past the run's end a load goes to the blob's first KiB, for nobody: a load under a condition would make every wait one for all)
+        auto load_super = [&](int d, int rr, int i) {
+            const int tile = min((g0 + i) * prm.tgroups + tg, prm.ntiles - 1), sc = min(kpart * R + rr, prm.nsuper - 1);
+            const size_t at = i < count ? (size_t)tile * prm.nsuper + sc : 0;
+#pragma unroll
+            for (int g = 0; g < group_count(P); ++g) {
+                const int b = group_width(P, g);
+                const mv4i* base = reinterpret_cast<const mv4i*>(blob + prm.off_fields[g]) + at * (b * 64) + lane;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (c < b) w[d][rr][moe_load_base(P, g) + c] = __builtin_nontemporal_load(base + c * 64);
+            }
+        };
+        // The channels' parameters of four tiles from i on, straight into LDS, by the first wave of a tile group.  A batch's are asked for a batch ahead and
+        // before that batch's refills: loads return in order, so they are there once the weights of the batch's last tile are.  (Written as the
+        // instruction: the compiler would wait for the builtin at every LDS access.)
+        auto load_params = [&](int i, int place) {
+            if (kpart != 0 || i >= count) return;   // (the same for the wave; what is asked for is always waited for)
+            const unsigned n = (unsigned)min(((g0 + i + G) * prm.tgroups + tg) * kTileN + r, prm.N - 1) * 16u;
+            const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(par_w + (place * prm.tgroups + tg) * 64);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(n), "s"(wparams) : "memory", "m0");
+        };
+        auto load_tile = [&](int d) {
+#pragma unroll
+            for (int rr = 0; rr < R; ++rr) load_super(d, rr, d);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        load_params(0, par_at);
+        load_tile(0);
+        // A: lane (r, G) holds bytes 16 G .. of slice s of rows r, r + 16; rows past the group's are its last one again.  Vectors past a row's
         // end hold what follows in memory; those past the last row's end are moved back.  Both are put right below.
         mv4i a[R][MT][8];
         uint32_t off[MT];
         const uint32_t a_end = (uint32_t)prm.g.tokens * (uint32_t)prm.K - 16u;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-            off[mt] = (uint32_t)moe_row_of(prm.g, min(row0 + min(16 * mt + r, max(nrow - 1, 0)), prm.g.rows - 1)) * (uint32_t)prm.K + G * 16u;
+        for (int mt = 0; mt < MT; ++mt) off[mt] = (uint32_t)moe_row(prm.g, entry[mt]) * (uint32_t)prm.K + G * 16u;
         const int last_slice = (prm.K - 1) / 64 * 64;
 #pragma unroll
         for (int rr = 0; rr < R; ++rr)
@@ -131,30 +193,12 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
                     a[rr][mt][s] = mv4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
                 }
             }
-        // ---- weights of the run's first tile
-        mv4i w[R][P];
-        RowParams pw, pw_next;
-        auto load_super = [&](int rr, int tile) {
-            const int sc = min(kpart * R + rr, prm.nsuper - 1);
-#pragma unroll
-            for (int g = 0; g < group_count(P); ++g) {
-                const int b = group_width(P, g);
-                const mv4i* base = reinterpret_cast<const mv4i*>(blob + prm.off_fields[g]) + ((size_t)tile * prm.nsuper + sc) * (b * 64) + lane;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < b) w[rr][moe_load_base(P, g) + i] = __builtin_nontemporal_load(base + i * 64);
-            }
-        };
-        auto tile_of = [&](int i) { return min((g0 + i) * prm.tgroups + tg, prm.ntiles - 1); };
-        auto load_params = [&](int tile) { return wparams[min(tile * kTileN + r, prm.N - 1)]; };
-        pw = load_params(tile_of(0));
-#pragma unroll
-        for (int rr = 0; rr < R; ++rr) load_super(rr, tile_of(0));
-        __syncthreads();   // (the tiles before are done with the row parameters)
-        if (tid < 16 * MT) {
-            const int row = moe_row_of(prm.g, min(row0 + min(tid, max(nrow - 1, 0)), prm.g.rows - 1));
-            par_a[tid] = RowParams{0, prm.a_scale[row], prm.a_zero[row], 0};
-        }
+        const int par_row = moe_row(prm.g, par_entry);
+        const float par_scale = prm.a_scale[par_row];
+        const int32_t par_zero = prm.a_zero[par_row];
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (D == 2) load_tile(1);
+        moe_barrier();   // (every wave is done with the run before: its rows' parameters and sums)
         int K = prm.K, k_lane = G * 16;
         asm volatile("" : "+s"(K), "+v"(k_lane));   // (or every slice's masks are made ahead of the loop over the runs, and spilled)
         uint32_t sums[MT];
@@ -176,65 +220,86 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
                     else moe_operand(a[rr][mt][s], prm.a_mask, flip, sums[mt]);
                 }
             }
+        if (tg == 0) {   // (the waves of the other tile groups hold the same parts of A)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            sums[mt] += __shfl_xor(sums[mt], 16);
-            sums[mt] += __shfl_xor(sums[mt], 32);
-            if (lane < 16) part_sum[wave][16 * mt + lane] = (int32_t)sums[mt];
+            for (int mt = 0; mt < MT; ++mt) {
+                sums[mt] += __shfl_xor(sums[mt], 16);
+                sums[mt] += __shfl_xor(sums[mt], 32);
+                if (lane < 16) atomicAdd(&row_sum[sums_at][16 * mt + lane], (int32_t)sums[mt]);   // (whole numbers: any order)
+            }
+        }
+        if (tid < 16 * MT) {
+            row_sum[sums_at ^ 1][tid] = 0;
+            par_a[tid] = RowParams{0, par_scale, par_zero, 0};
         }
 
-        // ---- the tiles
-        int buf = 0, turn = 0;
-        auto tile_step = [&](int i, auto more) {
+        // ---- the tiles, D of them in flight, a batch of them to a barrier
+        auto tile_step = [&](auto DC, int i, int b) {
+            constexpr int d = decltype(DC)::value;
             mv4i acc[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[mt] = mv4i{0, 0, 0, 0};
-            if constexpr (decltype(more)::value) pw_next = load_params(tile_of(i + 1));
 #pragma unroll
             for (int rr = 0; rr < R; ++rr) {
-                moe_super_chunk<P, MT>(w[rr], a[rr], acc);
-                if constexpr (decltype(more)::value) load_super(rr, tile_of(i + 1));
+                moe_super_chunk<P, MT>(w[d][rr], a[rr], acc);
+                load_super(d, rr, i + D);
             }
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) red[buf][wave][mt][lane] = acc[mt];
-            // every wave's parts are written; loads stay in flight (a workgroup fence would wait for them)
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            if (kpart == turn) {
+            for (int mt = 0; mt < MT; ++mt) red[(((buf * prm.batch + b) * waves + wave) * MT + mt) * 64 + lane] = acc[mt];
+        };
+        for (int i0 = 0; i0 < count; i0 += prm.batch) {
+            const int nb = min(prm.batch, count - i0), par_next = par_at == 2 ? 0 : par_at + 1;
+            load_params(i0 + prm.batch, par_next);
+            int b = 0;
+            for (; b + D <= nb; b += D) {   // (whole rounds: a step that may be left out would make every wait one for all loads)
+                tile_step(std::integral_constant<int, 0>{}, i0 + b, b);
+                if constexpr (D == 2) tile_step(std::integral_constant<int, 1>{}, i0 + b + 1, b + 1);
+            }
+            if constexpr (D == 2) { if (b < nb) tile_step(std::integral_constant<int, 0>{}, i0 + b, b); }
+            moe_barrier();
+            // tile b of rows mt of this tile group: its waves in turn
+            for (int t = kpart; t < nb * MT; t += prm.kparts) {
                 int own = lane;
                 asm volatile("" : "+v"(own));   // (or every address below is made ahead of the loop, in registers that the operands need)
-                const int tile = (g0 + i) * prm.tgroups + tg, n = tile * kTileN + (own & 15);
+                const int b = t / MT, mt = t - b * MT;
+                const mv4i* part = red + (((buf * prm.batch + b) * waves + tg * prm.kparts) * MT + mt) * 64 + own;
+                mv4i sum = mv4i{0, 0, 0, 0};
+                for (int k = 0; k < prm.kparts; k += 4) {
+                    mv4i v[4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mv4i sum = mv4i{0, 0, 0, 0};
-                    for (int k = 0; k < prm.kparts; ++k) sum += red[buf][tg * prm.kparts + k][mt][own];
+                    for (int j = 0; j < 4; ++j) v[j] = part[min(k + j, prm.kparts - 1) * (MT * 64)];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int m = 16 * mt + 4 * (own >> 4) + e;
-                        RowParams pa = par_a[m];
-                        for (int k = 0; k < prm.kparts; ++k) pa.sum += part_sum[k][m];
-                        int32_t raw;
-                        const uint16_t h = epilogue_value(sum[e], prm.oa, prm.ow, prm.K, pa, pw, &raw);
-                        if (m < nrow && n < prm.N) prm.y[(size_t)(row0 + m) * prm.N + n] = h;
-                    }
+                    for (int j = 0; j < 4; ++j) sum += v[j] & (k + j < prm.kparts ? -1 : 0);
+                }
+                const RowParams pw = reinterpret_cast<const RowParams*>(par_w)[(par_at * prm.tgroups + tg) * 64 + b * 16 + (own & 15)];
+                const int n = ((g0 + i0 + b) * prm.tgroups + tg) * kTileN + (own & 15);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int m = 16 * mt + 4 * (own >> 4) + e;
+                    RowParams pa = par_a[m];
+                    pa.sum = row_sum[sums_at][m];
+                    int32_t raw;
+                    const uint16_t h = epilogue_value(sum[e], prm.oa, prm.ow, prm.K, pa, pw, &raw);
+                    if (m < nrow && n < prm.N) prm.y[(size_t)(row0 + m) * prm.N + n] = h;
                 }
             }
             buf ^= 1;
-            turn = turn + 1 == prm.kparts ? 0 : turn + 1;
-            if constexpr (decltype(more)::value) pw = pw_next;
-        };
-        for (int i = 0; i + 1 < count; ++i) tile_step(i, std::true_type{});
-        tile_step(count - 1, std::false_type{});
+            par_at = par_next;
+        }
+        sums_at ^= 1;
     }
 }
 
 template <int P, int R, int MT>
 static hipError_t moe_rows_go(const MoeRowsParams& prm, unsigned grid, hipStream_t s)
 {
-    moe_rows_kernel<P, R, MT><<<grid, 64 * prm.kparts * prm.tgroups, 0, s>>>(prm);
+    static std::atomic<bool> attr_set{false};   // (an idempotent call: a lost race only repeats it)
+    if (!attr_set.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute((const void*)moe_rows_kernel<P, R, MT>, hipFuncAttributeMaxDynamicSharedMemorySize, 159 * 1024);
+        if (e != hipSuccess) return e;
+        attr_set.store(true, std::memory_order_release);
+    }
+    moe_rows_kernel<P, R, MT><<<grid, 64 * prm.kparts * prm.tgroups, moe_rows_lds_bytes(prm, MT), s>>>(prm);
     return hipGetLastError();
 }
 
