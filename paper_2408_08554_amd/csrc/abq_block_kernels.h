@@ -84,51 +84,30 @@ __device__ __forceinline__ int32_t bk_mad24(int32_t a, int32_t b, int32_t c)
 // What the epilogue needs of a channel: the sum over the codes less their zero-points is acc + raw0 + wz sumA - az cw.
 struct alignas(16) ColParams { int32_t raw0, cw, wz; float scale; };
 
-// OCC: waves per SIMD that the registers are held to.  PRM: BlockParams or BlockExpertParams.
-template <int P, int RW, int CW, int MT, int NT, int S, int OCC, class PRM = BlockParams>
-__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
+__host__ __device__ constexpr int bk_buf_bytes(int P, int bm, int tw) { return bm * kBkStep + tw * bk_fast_chunks(P) * 1024; }   // a place in the ring
+
+// Where a workgroup's tile lies: its rows m0 .. of the M that belong together, row y_row0 of Y the first of those; channels from n0 = 16 tile0 on.
+struct BlockTile {
+    const uint8_t* fields[3];
+    const RowParams* wparams;
+    int M, y_row0, m0, n0, tile0;
+};
+
+// A tile of 16 MT RW rows.  LDS: ring, the narrow groups' chunks, the epilogue's records (of a larger tile, it may be).
+template <int P, int RW, int CW, int MT, int NT, int S, class PRM>
+__device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, uint8_t* ring, uint8_t* lds_slow, RowParams* par_a, RowParams* par_w)
 {
     constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kWaves = RW * CW, kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
-    constexpr int kABytes = kBM * kBkStep, kBuf = kABytes + kTW * bk_fast_chunks(P) * 1024;
-    constexpr int kSlow = kTW * bk_slow_groups(P) * 1024;
+    constexpr int kABytes = kBM * kBkStep, kBuf = bk_buf_bytes(P, kBM, kTW);
     constexpr int kRecA = (kBM + 63) / 64, kRecW = (kBN + 63) / 64;   // wave loads of 64 records
-    __shared__ __align__(1024) uint8_t ring[S * kBuf];
-    __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
-    __shared__ __align__(16) RowParams par_a[64 * kRecA], par_w[64 * kRecW];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave / CW, cw = wave % CW;
     const int r = lane & 15, G = lane >> 4;
-    // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD); of experts: the tiles of one after the other, each in bands
-    int M = prm.M, tiles_m = prm.tiles_m, y_row0 = 0;
-    const uint8_t* fields[3] = {prm.fields[0], prm.fields[1], prm.fields[2]};
-    const RowParams* wparams = prm.wparams;
-    int vid;
-    if constexpr (kExperts) {
-        const ExpertUnits units(prm.g, kBM, prm.tiles_m);
-        const int nwg = units.total * prm.tiles_n, per = nwg >> 3, rem = nwg & 7;
-        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-        if (slot >= per + (xcd < rem ? 1 : 0)) return;   // (the grid is what there can be at most)
-        vid = xcd * per + min(xcd, rem) + slot;
-        const ExpertAt at = units.find(prm.g, kBM, vid / prm.tiles_n);
-        vid -= at.before * prm.tiles_n;
-        M = at.rows;
-        tiles_m = (at.rows + kBM - 1) / kBM;
-        y_row0 = at.first;
-#pragma unroll
-        for (int i = 0; i < 3; ++i) fields[i] += (size_t)at.expert * prm.w_stride;
-        wparams = reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(wparams) + (size_t)at.expert * prm.w_stride);
-    } else {
-        const int nwg = prm.tiles_m * prm.tiles_n;
-        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-        const int per = nwg >> 3, rem = nwg & 7;
-        vid = xcd * per + min(xcd, rem) + slot;
-    }
-    const int band = vid / (prm.band_m * prm.tiles_n), in_band = vid - band * prm.band_m * prm.tiles_n;
-    const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
-    const int m_blk = band * prm.band_m + in_band % band_rows, n_blk = in_band / band_rows;
-    const int m0 = m_blk * kBM, n0 = n_blk * kBN, tile0 = n_blk * kTW;
+    const int M = at.M, y_row0 = at.y_row0, m0 = at.m0, n0 = at.n0, tile0 = at.tile0;
+    const uint8_t* const fields[3] = {at.fields[0], at.fields[1], at.fields[2]};
+    const RowParams* const wparams = at.wparams;
     const int nsteps = prm.nsuper * 4;
 
     // ---- loads.  1 KiB a wave and instruction: 16 bytes per lane from base + off (all but off wave-uniform) to LDS address dst + 16 lane.
@@ -434,6 +413,64 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
     }
 }
 
+// OCC: waves per SIMD that the registers are held to.  PRM: BlockParams or BlockExpertParams.
+template <int P, int RW, int CW, int MT, int NT, int S, int OCC, class PRM = BlockParams>
+__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
+{
+    constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
+    constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
+    constexpr int kSlow = kTW * bk_slow_groups(P) * 1024;
+    __shared__ __align__(1024) uint8_t ring[S * bk_buf_bytes(P, kBM, kTW)];
+    __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
+    __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    BlockTile at;
+    if constexpr (kExperts) {
+        // Of experts: a tile's place in the order by the height of the body that it takes, tallest first (the bodies' times are their heights': the short
+        // ones fill the gaps at the end), of one height the experts one after the other, each in bands.
+        int left = prm.tiles_m, taken = 0, before = 0;   // units that may come yet; workgroups of the XCD's, and extra ones, that taller tiles have
+        auto some = [&](auto of) -> bool {
+            const ExpertUnits<decltype(of)> units(prm.g, of, left);
+            left -= units.total;
+            const int nwg = units.total * prm.tiles_n, per = nwg >> 3, rem = nwg & 7;
+            const int turn = (xcd - before) & 7, here = slot - taken;
+            taken += per + (turn < rem ? 1 : 0);
+            before += rem;
+            if (slot >= taken) return false;
+            const int vid = turn * per + min(turn, rem) + here;
+            const ExpertAt e = units.find(prm.g, vid / prm.tiles_n);
+            const int in_expert = vid - e.before * prm.tiles_n, tiles_m = of(e.rows), last = (e.rows + kBM - 1) / kBM;
+            const int band = in_expert / (prm.band_m * prm.tiles_n), in_band = in_expert - band * prm.band_m * prm.tiles_n;
+            const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
+            // (an expert has one block at most that is not of the tallest, its last)
+            const int m_blk = std::is_same<decltype(of), BlocksBetween<256, 0, 128>>::value || std::is_same<decltype(of), BlocksBetween<256, 128, 192>>::value ? last - 1 : band * prm.band_m + in_band % band_rows;
+            const int n_blk = in_band / band_rows;
+            at = BlockTile{{prm.fields[0] + (size_t)e.expert * prm.w_stride, prm.fields[1] + (size_t)e.expert * prm.w_stride, prm.fields[2] + (size_t)e.expert * prm.w_stride},
+                           reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(prm.wparams) + (size_t)e.expert * prm.w_stride),
+                           e.rows, e.first, m_blk * kBM, n_blk * kBN, n_blk * kTW};
+            return true;
+        };
+        if constexpr (MT == 8) {
+            static_assert(kBM == 256, "the heights");
+            if (some(BlocksBetween<256, 192, 256>{})) block_body<P, RW, CW, 8, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+        } else if (some(BlocksOf{kBM})) {   // (the grid is what there can be at most)
+            block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+        }
+    } else {
+        // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD)
+        const int nwg = prm.tiles_m * prm.tiles_n;
+        const int per = nwg >> 3, rem = nwg & 7;
+        const int vid = xcd * per + min(xcd, rem) + slot;
+        const int band = vid / (prm.band_m * prm.tiles_n), in_band = vid - band * prm.band_m * prm.tiles_n;
+        const int band_rows = min(prm.band_m, prm.tiles_m - band * prm.band_m);
+        const int m_blk = band * prm.band_m + in_band % band_rows, n_blk = in_band / band_rows;
+        at = BlockTile{{prm.fields[0], prm.fields[1], prm.fields[2]}, prm.wparams, prm.M, 0, m_blk * kBM, n_blk * kBN, n_blk * kTW};
+        block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+    }
+}
+
 template <int P, int RW, int CW, int MT, int NT, int S, int OCC>
 static hipError_t block_go(const BlockParams& prm, hipStream_t s)
 {
@@ -459,13 +496,15 @@ static hipError_t block_launch(const BlockParams& prm, int shape, hipStream_t s)
     }
 }
 
-// Experts: 256 x 256 (p = 7: 192), 128 x 128 by four waves and 64 x 128 (shapes 0, 3, 4 above).
+// 256 rows of experts: tiles of a wave along N (widths of more than one group of planes: 192 channels, or one of the bodies spills).
+__host__ __device__ constexpr int bk_expert_nt(int p) { return p == 3 || p == 6 || p == 7 ? 3 : 4; }
+// Experts: 256 x 256 (or 192), 128 x 128 by four waves and 64 x 128 (shapes 0, 3, 4 above).
 template <int P>
 static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, hipStream_t s)
 {
     const unsigned grid = (unsigned)(prm.tiles_m * prm.tiles_n);
     switch (shape) {
-        case 0: block_kernel<P, 2, 4, 8, P == 7 ? 3 : 4, 2, 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
+        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), 2, 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
         case 3: block_kernel<P, 2, 2, 4, 4, P >= 4 ? 2 : 3, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         case 4: block_kernel<P, 1, 4, 4, 2, P >= 7 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         default: return hipErrorInvalidValue;

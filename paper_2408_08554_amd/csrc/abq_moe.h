@@ -68,33 +68,38 @@ __device__ __forceinline__ void moe_expert_rows(const MoeGroups& g, int e, int* 
     *first = lo;
     *rows = max(hi - lo, 0);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moe_moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, true); }
 __device__ __forceinline__ int moe_scan(int x)   // sums over this lane and those before it
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(x, d, 64);
-        x += lane >= d ? v : 0;
-    }
+    x += moe_moved<0x111, 0xF>(x);   // inside the rows of sixteen, from 1, 2, 4 and 8 lanes before
+    x += moe_moved<0x112, 0xF>(x);
+    x += moe_moved<0x114, 0xF>(x);
+    x += moe_moved<0x118, 0xF>(x);
+    x += moe_moved<0x142, 0xA>(x);   // the last lane of the first and third row to the row behind
+    x += moe_moved<0x143, 0xC>(x);   // lane 31 to the upper half
     return x;
 }
+// UNITS: how many units so many rows are.
+template <class UNITS>
 struct ExpertUnits {
+    UNITS of;
     int first0, rows0, sum0, total;   // of lane's expert among the first 64: first row, rows, units up to and with it; all units
     // at most `most` units (starts that do not ascend could name more)
-    __device__ __forceinline__ ExpertUnits(const MoeGroups& g, int per, int most)
+    __device__ __forceinline__ ExpertUnits(const MoeGroups& g, UNITS of, int most) : of(of)
     {
         const int lane = threadIdx.x & 63;
         moe_expert_rows(g, lane, &first0, &rows0);
-        sum0 = moe_scan((rows0 + per - 1) / per);
+        sum0 = moe_scan(of(rows0));
         total = min(__builtin_amdgcn_readlane(sum0, 63), most);
         for (int e0 = 64; e0 < g.experts; e0 += 64) {
             int first, rows;
             moe_expert_rows(g, e0 + lane, &first, &rows);
-            total = min(total + __builtin_amdgcn_readlane(moe_scan((rows + per - 1) / per), 63), most);
+            total = min(total + __builtin_amdgcn_readlane(moe_scan(of(rows)), 63), most);
         }
     }
     // u < total
-    __device__ __forceinline__ ExpertAt find(const MoeGroups& g, int per, int u) const
+    __device__ __forceinline__ ExpertAt find(const MoeGroups& g, int u) const
     {
         const int lane = threadIdx.x & 63;
         int first = first0, rows = rows0, sum = sum0, before = 0;
@@ -111,9 +116,19 @@ struct ExpertUnits {
             }
             before += __builtin_amdgcn_readlane(sum, 63);
             moe_expert_rows(g, e0 + 64 + lane, &first, &rows);
-            sum = moe_scan((rows + per - 1) / per);
+            sum = moe_scan(of(rows));
         }
     }
+};
+// Blocks of `per` rows, the last one with what is left.
+struct BlocksOf {
+    int per;
+    __device__ __forceinline__ int operator()(int rows) const { return (rows + per - 1) / per; }
+};
+// Of those with LO + 1 .. HI rows.
+template <int PER, int LO, int HI>
+struct BlocksBetween {
+    __device__ __forceinline__ int operator()(int rows) const { return (HI == PER ? rows / PER : 0) + (rows % PER > LO && rows % PER <= HI ? 1 : 0); }
 };
 
 // Row of A of a sorted row (an entry of `order` that names none takes the nearest there is): what there is to load, and what it says.

@@ -356,7 +356,7 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
 // ---- the products: choice of kernel --------------------------------------------------------------
 // Workgroup shapes of the block kernel: 0 (256 x 256), 3 (128 x 128), 4 (64 x 128).
 static int expert_bm(int shape) { return shape == 0 ? 256 : (shape == 3 ? 128 : 64); }
-static int expert_bn(int p, int shape) { return shape == 0 ? (p == 7 ? 192 : 256) : 128; }
+static int expert_bn(int p, int shape) { return shape == 0 ? 64 * bk_expert_nt(p) : 128; }
 
 // Groups of `per` rows that `rows` rows of `experts` experts can make at most.
 static int most_groups(int rows, int experts, int per)

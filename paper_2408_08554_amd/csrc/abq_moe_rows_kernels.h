@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
     mv4i* const red = lds;                                               // part of tile b, buffer f: at ((f batch + b) waves + wave) MT 64
     mv4i* const par_w = lds + 2 * prm.batch * waves * MT * 64;
 
-    const ExpertUnits units(prm.g, 16 * MT, prm.most);
+    const ExpertUnits<BlocksOf> units(prm.g, BlocksOf{16 * MT}, prm.most);
     // this workgroup's run: all units are dealt out evenly
     const unsigned all = (unsigned)units.total * (unsigned)prm.groups_n, per = all / gridDim.x, rest = all - per * gridDim.x;   // (below 2^30)
     unsigned u = blockIdx.x * per + min(blockIdx.x, rest);
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
     while (u < end) {
         const int block = (int)(u / (unsigned)prm.groups_n), g0 = (int)u - block * prm.groups_n;
         const int count = min((int)(end - u), prm.groups_n - g0);
-        const ExpertAt at = units.find(prm.g, 16 * MT, block);
+        const ExpertAt at = units.find(prm.g, block);
         const int local = (block - at.before) * 16 * MT;
         const int row0 = at.first + local, nrow = min(max(at.rows - local, 0), 16 * MT);
         const uint8_t* blob = prm.w + (size_t)at.expert * prm.w_stride;
