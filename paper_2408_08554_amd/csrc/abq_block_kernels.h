@@ -52,11 +52,30 @@ constexpr int kBkStep = 128;     // k per step: one chunk of a 4-bit group, two 
 __host__ __device__ constexpr int bk_fast_chunks(int p) { return p == 8 ? 2 : (p >= 4 ? 1 : 0); }
 __host__ __device__ constexpr int bk_slow_groups(int p) { return group_count(p) - (p >= 4 ? 1 : 0); }
 __host__ __device__ constexpr int bk_slow_index(int p, int g) { return p >= 4 ? g - 1 : g; }
+// Places that the chunks of group g have where they are asked for `ahead` steps ahead: a chunk lies there until the step before its first has read it.
+__host__ __device__ constexpr int bk_slow_places(int p, int g, int ahead) { return group_width(p, g) == 2 ? (ahead + 1) / 2 : (ahead + 3) / 4; }
+__host__ __device__ constexpr int bk_slow_first(int p, int g, int ahead)   // the first place of group g
+{
+    int n = 0;
+    for (int i = p >= 4 ? 1 : 0; i < g; ++i) n += bk_slow_places(p, i, ahead);
+    return n;
+}
+__host__ __device__ constexpr int bk_slow_place(int p, int g, int ahead, int T)   // place of the chunk that a step = T modulo 4 begins
+{
+    return bk_slow_first(p, g, ahead) + (group_width(p, g) == 2 ? T / 2 % bk_slow_places(p, g, ahead) : 0);
+}
 // whether group g has a chunk that begins with a step = T modulo 4 of the super-chunk, and is not loaded with every step
 __host__ __device__ constexpr bool bk_slow_begins(int p, int g, int T)
 {
     return g < group_count(p) && ((group_width(p, g) == 2 && T % 2 == 0) || (group_width(p, g) == 1 && T == 0));
 }
+__host__ __device__ constexpr int bk_slow_count(int p, int T)   // such groups
+{
+    return (bk_slow_begins(p, 0, T) ? 1 : 0) + (bk_slow_begins(p, 1, T) ? 1 : 0) + (bk_slow_begins(p, 2, T) ? 1 : 0);
+}
+// Steps between the load of a narrow group's chunk and its first step: two, and as many as the ring has where an expert's weights come from memory
+// for a few rows alone (W2A8 32 experts of 4096->4096 with 32 rows each: two 50 us, four 43).
+__host__ __device__ constexpr int bk_slow_ahead(bool experts, int S) { return experts ? S : 2; }
 
 // Operand dword j of slice SL (0..7 inside a super-chunk): all plane groups merged into one byte per weight.  raw: the tile's chunks.
 template <int P, int SL, int G0 = 0>
@@ -99,6 +118,7 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
 {
     constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kWaves = RW * CW, kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
+    constexpr int kAhead = bk_slow_ahead(kExperts, S);
     constexpr int kABytes = kBM * kBkStep, kBuf = bk_buf_bytes(P, kBM, kTW);
     constexpr int kRecA = (kBM + 63) / 64, kRecW = (kBN + 63) / 64;   // wave loads of 64 records
     const int tid = threadIdx.x, lane = tid & 63;
@@ -160,7 +180,7 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
 #pragma unroll
                 for (int u = 0; u < kWLoads; ++u)
                     lds_load(fields[g] + (size_t)w_row[u] * (prm.nsuper * b) * 1024, lane * 16 + (b == 2 ? step >> 1 : step >> 2) * 1024,
-                             lds_addr(lds_slow) + (bk_slow_index(P, g) * kTW + w_place[u]) * 1024);
+                             lds_addr(lds_slow) + (bk_slow_place(P, g, kAhead, T) * kTW + w_place[u]) * 1024);
             }
         };
         group(std::integral_constant<int, 0>{});
@@ -190,11 +210,27 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
         else if constexpr (kExperts) lds_load(prm.aparams, (unsigned)moe_row_of(prm.g, y_row0 + min(m0 + i * 64 + lane, M - 1)) * 16u, lds_addr(par_a + i * 64));
         else lds_load(prm.aparams, (unsigned)min(m0 + i * 64 + lane, prm.M - 1) * 16u, lds_addr(par_a + i * 64));
     }
-    load_slow(std::integral_constant<int, 0>{}, 0);
+    // Loads that come behind those of step T, modulo 4: of the n - 1 steps after it, with their narrow groups' chunks.
+    constexpr auto behind = [](int T, int n) {
+        int loads = 0;
+        for (int u = 1; u < n; ++u) loads += kLoads + (kAhead == S ? kWLoads * bk_slow_count(P, (T + u) & 3) : 0);
+        return loads;
+    };
+    auto load_first = [&](auto SC) {
+        constexpr int s = decltype(SC)::value;
+        if constexpr (s < S) {
+            if constexpr (s < kAhead && (kAhead == S || s == 0)) load_slow(std::integral_constant<int, s & 3>{}, min(s, nsteps - 4 + (s & 3)));
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_piece(i, min(s, nsteps - 1), ring + s * kBuf);
+            for (int i = 0; i < kLoads; ++i) load_piece(i, min(s, nsteps - 1), ring + s * kBuf);
+        }
+    };
+    static_assert(S <= 6, "below");
+    load_first(std::integral_constant<int, 0>{});
+    load_first(std::integral_constant<int, 1>{});
+    load_first(std::integral_constant<int, 2>{});
+    load_first(std::integral_constant<int, 3>{});
+    load_first(std::integral_constant<int, 4>{});
+    load_first(std::integral_constant<int, 5>{});
 
     // ---- operands of a wave: the current slice's rows of A (replaced by the next slice's one by one), the expanded weights of both slices
     // of a step, the chunks that they are made from
@@ -212,14 +248,14 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
             if constexpr (g < group_count(P)) {
                 if constexpr (group_width(P, g) == 4) raw[nt][g] = *reinterpret_cast<const v4i*>(buf + kABytes + (cw * NT + nt) * 1024 + lane * 16);
                 else if constexpr (bk_slow_begins(P, g, T))
-                    raw[nt][g] = *reinterpret_cast<const v4i*>(lds_slow + (bk_slow_index(P, g) * kTW + cw * NT + nt) * 1024 + lane * 16);
+                    raw[nt][g] = *reinterpret_cast<const v4i*>(lds_slow + (bk_slow_place(P, g, kAhead, T) * kTW + cw * NT + nt) * 1024 + lane * 16);
             }
         };
         group(std::integral_constant<int, 0>{});
         group(std::integral_constant<int, 1>{});
         group(std::integral_constant<int, 2>{});
     };
-    sync(std::integral_constant<int, (S - 1) * kLoads>{});
+    sync(std::integral_constant<int, behind(0, S)>{});
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         if constexpr (P == 8) w0[nt] = read_w8(nt, 0, ring);
@@ -275,10 +311,9 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
             }
             __builtin_amdgcn_sched_barrier(0);
             if (j == -1) {
-                // The narrow groups' chunks of step + 1 were asked for a step ago, ahead of that step's kLoads.
-                constexpr bool slow = bk_slow_begins(P, 0, TN) || bk_slow_begins(P, 1, TN) || bk_slow_begins(P, 2, TN);
-                sync(std::integral_constant<int, S == 2 ? 0 : (slow ? kLoads : (S - 2) * kLoads)>{});
-                load_slow(std::integral_constant<int, (T + 2) & 3>{}, min(step + 2, nsteps - 4 + ((T + 2) & 3)));
+                // The narrow groups' chunks of step + 1 came right ahead of its other loads, or were asked for a step ago, ahead of that step's kLoads.
+                sync(std::integral_constant<int, (S > kAhead && bk_slow_count(P, TN) > 0 ? kLoads : behind(TN, S - 1))>{});
+                load_slow(std::integral_constant<int, (T + kAhead) & 3>{}, min(step + kAhead, nsteps - 4 + ((T + kAhead) & 3)));
             }
         }
     };
@@ -419,7 +454,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
 {
     constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
-    constexpr int kSlow = kTW * bk_slow_groups(P) * 1024;
+    constexpr int kSlow = kTW * bk_slow_first(P, group_count(P), bk_slow_ahead(kExperts, S)) * 1024;
     __shared__ __align__(1024) uint8_t ring[S * bk_buf_bytes(P, kBM, kTW)];
     __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
     __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
@@ -506,7 +541,7 @@ static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, 
     switch (shape) {
         case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), 2, 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
         case 3: block_kernel<P, 2, 2, 4, 4, P >= 4 ? 2 : 3, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
-        case 4: block_kernel<P, 1, 4, 4, 2, P >= 7 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        case 4: block_kernel<P, 1, 4, 4, 2, P >= 6 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

@@ -53,7 +53,7 @@ struct MoeRowsParams {
     int kparts, tgroups;      // waves of a workgroup: parts of K, tiles side by side
     int batch;                // tiles between two barriers
     int groups_n;             // tile groups of an expert
-    int most;                 // groups of 16 MT rows there can be
+    int most;                 // groups of 16 rows there can be
 };
 struct BlockExpertParams;     // (abq_block_kernels.h)
 

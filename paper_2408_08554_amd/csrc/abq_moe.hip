@@ -12,7 +12,9 @@ namespace abq {
 struct RouteParams {
     MoeRouteArgs g;
     int chunk, chunks, bits;   // tokens of a workgroup, workgroups, bits of an expert's number
-    int32_t* hist;             // [chunks][experts] (more than one chunk)
+    int each;                  // chunks that a workgroup of the second launch places
+    int padded;                // experts, to a multiple of eight
+    uint16_t* hist;            // [chunks][padded] (more than one chunk)
 };
 
 // Reductions over the 16 lanes of a row, every lane gets the result: two exchanges inside the quads, then the half row and the row mirrored.
@@ -52,33 +54,60 @@ __device__ __forceinline__ T reduce(T x, F f)
     return x;
 }
 
-// Keys: whole numbers in the order of the values, all above that of minus infinity, which like NaN is 0: an expert that is not there.
-__device__ __forceinline__ uint32_t key_of(float x)
-{
-    if (!(x > -INFINITY)) return 0;
-    const uint32_t b = __float_as_uint(x + 0.0f);   // (-0 is 0)
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ uint64_t key_of(double x)
-{
-    if (!(x > -(double)INFINITY)) return 0;
-    const uint64_t b = __builtin_bit_cast(uint64_t, x + 0.0);
-    return b >> 63 ? ~b : b | 1ull << 63;
-}
-
-__device__ __forceinline__ float logit(const MoeRouteArgs& g, int64_t token, int e)
-{
-    const int64_t at = token * g.ld + e;
-    return g.logits_bits == 16 ? __half2float(__ushort_as_half(((const unsigned short*)g.logits)[at])) : ((const float*)g.logits)[at];
-}
-
-// What decides between two experts, by KIND.  0: a binary16 logit's key and, in its last 13 bits, 0x1FFF - expert: one word whose maximum is the
-// choice, ties to the lowest expert.  1: the same of a binary32 logit in two words.  2: score + bias in binary64 (the expert's number is looked for afterwards).
-template <int KIND> struct KeyType { typedef uint64_t type; };
+// What decides between two experts, by KIND: its maximum is the choice, ties to the lowest expert.
+// 0, a binary16 logit: a whole number in the order of the values, above 0 (which is an expert that is not there: minus infinity or NaN), whose last 13
+//    bits are 0x1FFF - expert.  (A binary16 value's binary32 form has thirteen zeros at its end, ones where the key is its complement.)
+// 1, a binary32 logit: its binary64 form, which ends in 29 zeros, with the expert's number in the last 13 bits (of a negative value as it is, else
+//    0x1FFF - expert).  Plus infinity is 2^1023, not there is the lowest finite value.  One maximum is one instruction; on whole numbers of two words it is three.
+// 2: score + bias in binary64; the expert's number is looked for afterwards.  Not there is minus infinity.
+template <int KIND> struct KeyType { typedef double type; };
 template <> struct KeyType<0> { typedef uint32_t type; };
+constexpr uint32_t kNotThereHigh = 0xFFEFFFFFu;   // (KIND 1: the lowest finite value's upper word, whatever the lower)
+
+__device__ __forceinline__ double packed(uint32_t high, uint32_t low) { return __builtin_bit_cast(double, (uint64_t)high << 32 | low); }
+__device__ __forceinline__ uint32_t high_of(double x) { return (uint32_t)(__builtin_bit_cast(uint64_t, x) >> 32); }
+__device__ __forceinline__ uint32_t low_of(double x) { return (uint32_t)__builtin_bit_cast(uint64_t, x); }
+__device__ __forceinline__ uint32_t key_max(uint32_t a, uint32_t b) { return max(a, b); }
+__device__ __forceinline__ double key_max(double a, double b)   // (the instruction: fmax() makes quiet NaNs of its arguments first, and there are none)
+{
+    double d;
+    asm("v_max_f64 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+    return d;
+}
+template <int KIND>
+__device__ __forceinline__ typename KeyType<KIND>::type key_of(float x, int e)
+{
+    if constexpr (KIND == 0) {
+        const uint32_t b = __float_as_uint(x + 0.0f);   // (-0 is 0)
+        return x > -INFINITY ? ((b & 0x80000000u ? ~b : b | 0x80000000u) & 0xFFFFE000u) | (0x1FFFu - e) : 0;
+    } else {
+        const double d = (double)(x + 0.0f);
+        const uint32_t high = x > -INFINITY ? min(high_of(d), x < 0.0f ? 0xFFFFFFFFu : 0x7FE00000u) : kNotThereHigh;
+        return packed(high, low_of(d) | (high >> 31 ? e : 0x1FFF - e));
+    }
+}
+
+// Logits VPL l .. + VPL - 1 of a token, minus infinity behind the last one.  (Whole loads, none under a condition, or each waits for the one before.)
+template <int VPL, bool HALF>
+__device__ __forceinline__ void load_logits(const MoeRouteArgs& g, int64_t token, int l, float* x)
+{
+    const int64_t row = token * g.ld;
+    uint32_t raw[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const int64_t at = row + min(VPL * l + i, g.experts - 1);
+        if constexpr (HALF) raw[i] = ((const unsigned short*)g.logits)[at];
+        else raw[i] = ((const uint32_t*)g.logits)[at];
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const float v = HALF ? __half2float(__ushort_as_half((unsigned short)raw[i])) : __uint_as_float(raw[i]);
+        x[i] = VPL * l + i < g.experts ? v : -INFINITY;
+    }
+}
 
 // The choice of one token by LPT lanes, lane l holding experts VPL l .. + VPL - 1.  Lane j gets choice j: its expert, or -1, and weight.
-template <int LPT, int VPL, int KIND>
+template <int LPT, int VPL, int KIND, bool HALF>
 __device__ __forceinline__ void route_token(const MoeRouteArgs& g, int64_t token, int l, int* id_out, float* weight_out)
 {
     typedef typename KeyType<KIND>::type Key;
@@ -86,11 +115,13 @@ __device__ __forceinline__ void route_token(const MoeRouteArgs& g, int64_t token
     const auto larger = [](auto a, auto b) { return a > b ? a : b; };
     const auto sum = [](auto a, auto b) { return a + b; };
     float x[VPL];
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = VPL * l + i < g.experts ? logit(g, token, VPL * l + i) : -INFINITY;
+    load_logits<VPL, HALF>(g, token, l, x);
     if constexpr (KIND == 2) {
         float top = -INFINITY;
         double total = 0;
+        float bias[VPL];
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) bias[i] = g.bias[min(VPL * l + i, g.experts - 1)];
         if (!g.sigmoid) {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) top = fmaxf(top, x[i]);
@@ -101,43 +132,58 @@ __device__ __forceinline__ void route_token(const MoeRouteArgs& g, int64_t token
         }
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            key[i] = 0;
-            if (x[i] > -INFINITY) {
-                const double s = g.sigmoid ? 1.0 / (1.0 + exp(-(double)x[i])) : exp((double)x[i] - (double)top) / total;
-                key[i] = key_of(s + (double)g.bias[VPL * l + i]);
-            }
+            const double s = g.sigmoid ? 1.0 / (1.0 + exp(-(double)x[i])) : exp((double)x[i] - (double)top) / total;
+            const double k = s + (double)bias[i];
+            key[i] = x[i] > -INFINITY && k > -(double)INFINITY ? k : -(double)INFINITY;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            const uint32_t k = key_of(x[i]), e = VPL * l + i;
-            // (a binary16 value's binary32 form has thirteen zeros at its end, ones where the key is its complement)
-            if constexpr (KIND == 0) key[i] = k ? (k & 0xFFFFE000u) | (0x1FFFu - e) : 0;
-            else key[i] = k ? (uint64_t)k << 32 | (0xFFFFFFFFu - e) : 0;
-        }
+        for (int i = 0; i < VPL; ++i) key[i] = key_of<KIND>(x[i], VPL * l + i);
     }
     int id = -1;
+    float v = -INFINITY;   // the choice's logit
+    Key mine = 0;
     for (int j = 0; j < g.top; ++j) {
-        Key best = 0;
+        Key best = key[0];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) best = larger(best, key[i]);
-        best = reduce<LPT>(best, larger);
-        int e;
-        if constexpr (KIND == 0) e = 0x1FFF - (int)(best & 0x1FFFu);
-        else if constexpr (KIND == 1) e = (int)(0xFFFFFFFFu - (uint32_t)best);
-        else {
+        for (int i = 1; i < VPL; ++i) best = key_max(best, key[i]);
+        best = reduce<LPT>(best, [](Key a, Key b) { return key_max(a, b); });
+        if constexpr (KIND == 2) {
             uint32_t low = 0xFFFFFFFFu;
 #pragma unroll
             for (int i = VPL - 1; i >= 0; --i) low = key[i] == best ? (uint32_t)(VPL * l + i) : low;
-            e = (int)reduce<LPT>(low, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
-        }
-        if (best == 0) e = -1;
+            const int e = best > -(double)INFINITY ? (int)reduce<LPT>(low, [](uint32_t a, uint32_t b) { return a < b ? a : b; }) : -1;
+            float at = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) key[i] = VPL * l + i == e ? 0 : key[i];
-        if (l == j) id = e;
+            for (int i = 0; i < VPL; ++i) {
+                if (VPL * l + i == e) { key[i] = -(double)INFINITY; at = x[i]; }
+            }
+            at = reduce<LPT>(at, larger);
+            if (l == j) { id = e; v = at; }
+        } else if constexpr (KIND == 1) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) key[i] = packed(low_of(key[i]) == low_of(best) ? kNotThereHigh : high_of(key[i]), low_of(key[i]));
+            if (l == j) mine = best;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) key[i] = key[i] == best ? 0 : key[i];
+            if (l == j) mine = best;
+        }
+    }
+    // (the key's way back)
+    if constexpr (KIND == 0) {
+        if (l < g.top && mine != 0) {
+            id = 0x1FFF - (int)(mine & 0x1FFFu);
+            v = __uint_as_float((mine >> 31 ? mine & 0x7FFFFFFFu : ~mine) & 0xFFFFE000u);
+        }
+    } else if constexpr (KIND == 1) {
+        if (l < g.top && high_of(mine) != kNotThereHigh) {
+            id = (int)(low_of(mine) & 0x1FFFu);
+            id = high_of(mine) >> 31 ? id : 0x1FFF - id;
+            v = (float)packed(high_of(mine), low_of(mine) & 0xFFFFE000u);
+        }
     }
     // weights: the chosen experts' scores, over their sum where that is asked for (the largest logit taken out of all of them first)
-    const float v = id >= 0 ? logit(g, token, id) : -INFINITY;
     float w;
     if (g.sigmoid) {
         const float c = g.renormalize ? fminf(reduce<LPT>(v, larger), 0.0f) : 0.0f;
@@ -176,32 +222,37 @@ __device__ __forceinline__ uint64_t same_number(int id, int bits)
     return id >= 0 ? m : 0;
 }
 
-// Places of a chunk's rows.  counts: LDS [waves][experts], all zero; base: LDS [experts], the place of the chunk's first row of each expert.  Every
-// wave takes a run of the rows in order, so that the rows of one expert stay in theirs.
-__device__ __forceinline__ void place_rows(const RouteParams& prm, int64_t slot0, int slots, int32_t* counts, const int32_t* base)
+// Places of a run of rows.  ids: their experts; counts: LDS [waves][experts], all zero; base: LDS [experts], the place of the run's first row of each
+// expert.  Every wave takes a part of the rows in order, so that the rows of one expert stay in theirs.
+__device__ __forceinline__ void place_rows(const RouteParams& prm, const int32_t* ids, int64_t slot0, int slots, int32_t* counts, const int32_t* base)
 {
     const MoeRouteArgs& g = prm.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
     const int run = (slots + 64 * waves - 1) / (64 * waves) * 64, from = wave * run, to = min(from + run, slots);
     int32_t* mine = counts + wave * g.experts;
     for (int i = from; i < to; i += 64) {
-        const int id = i + lane < to ? g.ids[slot0 + i + lane] : -1;
+        const int id = i + lane < to ? ids[i + lane] : -1;
         const uint64_t same = same_number(id, prm.bits);
         if (same && lane == __ffsll((unsigned long long)same) - 1) mine[id] += __popcll(same);
     }
     __syncthreads();
     for (int e = tid; e < g.experts; e += blockDim.x) {
         int32_t at = base[e];
-        for (int w = 0; w < waves; ++w) {
-            const int32_t n = counts[w * g.experts + e];
-            counts[w * g.experts + e] = at;
-            at += n;
+        for (int w0 = 0; w0 * run < slots; w0 += 8) {   // (of the waves that have rows; a workgroup has a multiple of eight waves, or reads the rest for nothing)
+            int32_t n[8];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) n[w] = counts[min(w0 + w, waves - 1) * g.experts + e];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (w0 + w < waves) counts[(w0 + w) * g.experts + e] = at;
+                at += n[w];
+            }
         }
     }
     __syncthreads();
     for (int i = from; i < to; i += 64) {
         const bool there = i + lane < to;
-        const int id = there ? g.ids[slot0 + i + lane] : -1;
+        const int id = there ? ids[i + lane] : -1;
         const uint64_t same = same_number(id, prm.bits);
         int place = -1;
         if (id >= 0) {
@@ -237,38 +288,43 @@ __device__ __forceinline__ void expert_starts(const RouteParams& prm, const int3
     __syncthreads();
 }
 
+// Threads of a workgroup, at most: sixteen logits a lane with a bias take more than the 128 registers of 1024.
+__host__ __device__ constexpr int route_threads(int VPL, bool biased) { return VPL >= 16 && biased ? 512 : 1024; }
+
 // What bounds it: one token is latency (a launch, the logits, `top` rounds of a maximum over 16 lanes); many tokens are the vector ALU: a
 // round is some 3 VPL + 10 operations for the four tokens of a wave.  Up to kRouteOne tokens are one launch of one workgroup, which also sorts
 // the rows; more are a launch that chooses and counts, a workgroup per chunk, and a second one whose workgroups add the counts of the chunks before
 // theirs and place their rows (no atomics on memory: the same rows in the same order every time).
-template <int LPT, int VPL, int KIND>
-__global__ __launch_bounds__(1024) void moe_route_kernel(RouteParams prm)
+template <int LPT, int VPL, int KIND, bool HALF>
+__global__ __launch_bounds__(route_threads(VPL, KIND == 2)) void moe_route_kernel(RouteParams prm)
 {
-    extern __shared__ __align__(16) int32_t lds[];   // [experts] totals, [experts] before, [waves][experts] counts (one chunk: the place of its rows)
+    extern __shared__ __align__(16) int32_t lds[];   // [experts] totals; one chunk alone: [experts] before, [waves][experts] counts, [rows] ids
     __shared__ int32_t all;
     const MoeRouteArgs& g = prm.g;
     const int tid = threadIdx.x, l = tid % LPT, E = g.experts;
     const bool alone = prm.chunks == 1;
     const int64_t t0 = (int64_t)blockIdx.x * prm.chunk, t1 = min(t0 + prm.chunk, (int64_t)g.tokens);
-    for (int i = tid; i < (alone ? 2 + (int)(blockDim.x >> 6) : 1) * E; i += blockDim.x) lds[i] = 0;
+    const int counted = (alone ? 2 + (int)(blockDim.x >> 6) : 1) * E;
+    for (int i = tid; i < counted; i += blockDim.x) lds[i] = 0;
     __syncthreads();
     for (int64_t t = t0 + tid / LPT; t < t1; t += blockDim.x / LPT) {
         int id;
         float w;
-        route_token<LPT, VPL, KIND>(g, t, l, &id, &w);
+        route_token<LPT, VPL, KIND, HALF>(g, t, l, &id, &w);
         if (l < g.top) {
             g.ids[t * g.top + l] = id;
             g.weights[t * g.top + l] = w;
+            if (alone) lds[counted + (int)t * g.top + l] = id;
             if (id >= 0) atomicAdd(&lds[id], 1);
         }
     }
     __syncthreads();
-    if (!alone) {
-        for (int e = tid; e < E; e += blockDim.x) prm.hist[(size_t)blockIdx.x * E + e] = lds[e];
+    if (!alone) {   // (a count is at most a chunk's tokens, which kRouteTokens keeps below 2^16)
+        for (int e = tid; e < prm.padded; e += blockDim.x) prm.hist[(size_t)blockIdx.x * prm.padded + e] = (uint16_t)(e < E ? lds[e] : 0);
         return;
     }
     expert_starts(prm, lds, lds + E, &all, true);
-    place_rows(prm, 0, g.tokens * g.top, lds + 2 * E, lds + E);
+    place_rows(prm, lds + counted, 0, g.tokens * g.top, lds + 2 * E, lds + E);
     for (int i = all + tid; i < g.tokens * g.top; i += blockDim.x) g.order[i] = -1;
 }
 
@@ -277,38 +333,57 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     extern __shared__ __align__(16) int32_t lds[];   // [experts] totals, [experts] before, [waves][experts] counts
     __shared__ int32_t all;
     const MoeRouteArgs& g = prm.g;
-    const int tid = threadIdx.x, E = g.experts, c = blockIdx.x, waves = blockDim.x >> 6;
+    const int tid = threadIdx.x, E = g.experts, c0 = blockIdx.x * prm.each, waves = blockDim.x >> 6;
     int32_t *totals = lds, *before = lds + E, *counts = lds + 2 * E;
     for (int i = tid; i < (2 + waves) * E; i += blockDim.x) lds[i] = 0;
     __syncthreads();
-    // the chunks' counts: threads side by side along the experts, groups of them along the chunks (sums of whole numbers: any order)
-    const int wide = min(E, (int)blockDim.x), groups = blockDim.x / wide, group = tid / wide;
+    // the chunks' counts: threads side by side along the experts (eight each), groups of them along the chunks, a thread's loads all in flight (sums of whole
+    // numbers: any order)
+    const int eights = prm.padded / 8, wide = min(eights, (int)blockDim.x), groups = blockDim.x / wide, group = tid / wide;
+    const uint4* hist = reinterpret_cast<const uint4*>(prm.hist);
     if (group < groups)
-        for (int e = tid % wide; e < E; e += wide) {
-            int32_t sum = 0, pre = 0;
-#pragma unroll 8
-            for (int k = group; k < prm.chunks; k += groups) {
-                const int32_t n = prm.hist[(size_t)k * E + e];
-                sum += n;
-                pre += k < c ? n : 0;
+        for (int f = tid % wide; f < eights; f += wide) {
+            int sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, pre[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            for (int k0 = group; k0 < prm.chunks; k0 += 8 * groups) {
+                uint4 n[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) n[u] = hist[(size_t)min(k0 + u * groups, prm.chunks - 1) * eights + f];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int k = k0 + u * groups;
+                    const int all_of = k < prm.chunks ? 0xFFFF : 0, before_of = k < c0 ? 0xFFFF : 0;
+                    const uint32_t w[4] = {n[u].x, n[u].y, n[u].z, n[u].w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int v = (int)(w[e >> 1] >> (16 * (e & 1)));
+                        sum[e] += v & all_of;
+                        pre[e] += v & before_of;
+                    }
+                }
             }
-            atomicAdd(&totals[e], sum);
-            atomicAdd(&counts[e], pre);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (8 * f + e < E) {
+                    atomicAdd(&totals[8 * f + e], sum[e]);
+                    atomicAdd(&counts[8 * f + e], pre[e]);
+                }
         }
     __syncthreads();
-    expert_starts(prm, totals, before, &all, c == 0);
+    expert_starts(prm, totals, before, &all, c0 == 0);
     for (int e = tid; e < E; e += blockDim.x) { before[e] += counts[e]; counts[e] = 0; }
     __syncthreads();
-    const int64_t t0 = (int64_t)c * prm.chunk, t1 = min(t0 + prm.chunk, (int64_t)g.tokens);
-    place_rows(prm, t0 * g.top, (int)(t1 - t0) * g.top, counts, before);
-    for (int64_t i = all + (int64_t)c * blockDim.x + tid; i < (int64_t)g.tokens * g.top; i += (int64_t)prm.chunks * blockDim.x) g.order[i] = -1;
+    const int64_t t0 = (int64_t)c0 * prm.chunk, t1 = min(t0 + (int64_t)prm.each * prm.chunk, (int64_t)g.tokens);
+    place_rows(prm, g.ids + t0 * g.top, t0 * g.top, (int)(t1 - t0) * g.top, counts, before);
+    for (int64_t i = all + (int64_t)blockIdx.x * blockDim.x + tid; i < (int64_t)g.tokens * g.top; i += (int64_t)gridDim.x * blockDim.x) g.order[i] = -1;
 }
 
-constexpr int kRouteOne = 256, kRouteChunks = 256;   // tokens of a single launch; chunks of two, at most
+// Tokens of a single launch; of more, chunks of kRouteTokens (as many as the chip's units can have two of, or longer ones), placed by fewer workgroups, each of
+// which reads all chunks' counts.
+constexpr int kRouteOne = 256, kRouteTokens = 16, kRouteChunks = 512, kPlacers = 128;
 
 static void route_chunks(int tokens, int* chunk, int* chunks)
 {
-    *chunk = tokens <= kRouteOne ? tokens : std::max(64, (tokens + kRouteChunks - 1) / kRouteChunks);
+    *chunk = tokens <= kRouteOne ? tokens : std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks);
     *chunks = (tokens + *chunk - 1) / *chunk;
 }
 
@@ -316,16 +391,18 @@ size_t moe_route_workspace_bytes(int tokens, int experts)
 {
     int chunk, chunks;
     route_chunks(tokens, &chunk, &chunks);
-    return chunks == 1 ? 0 : (size_t)chunks * experts * sizeof(int32_t);
+    return chunks == 1 ? 0 : (size_t)chunks * ((experts + 7) / 8 * 8) * sizeof(uint16_t);
 }
 
 template <int LPT, int VPL>
 static void route_go(const RouteParams& prm, unsigned threads, size_t lds_bytes, hipStream_t s)
 {
     const unsigned grid = (unsigned)prm.chunks;
-    if (prm.g.bias) moe_route_kernel<LPT, VPL, 2><<<grid, threads, lds_bytes, s>>>(prm);
-    else if (prm.g.logits_bits == 16) moe_route_kernel<LPT, VPL, 0><<<grid, threads, lds_bytes, s>>>(prm);
-    else moe_route_kernel<LPT, VPL, 1><<<grid, threads, lds_bytes, s>>>(prm);
+    const bool half = prm.g.logits_bits == 16;
+    if (prm.g.bias && half) moe_route_kernel<LPT, VPL, 2, true><<<grid, threads, lds_bytes, s>>>(prm);
+    else if (prm.g.bias) moe_route_kernel<LPT, VPL, 2, false><<<grid, threads, lds_bytes, s>>>(prm);
+    else if (half) moe_route_kernel<LPT, VPL, 0, true><<<grid, threads, lds_bytes, s>>>(prm);
+    else moe_route_kernel<LPT, VPL, 1, false><<<grid, threads, lds_bytes, s>>>(prm);
 }
 
 hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
@@ -333,14 +410,16 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
     RouteParams prm;
     prm.g = g;
     route_chunks(g.tokens, &prm.chunk, &prm.chunks);
-    prm.hist = (int32_t*)g.workspace;
-    prm.bits = 32 - __builtin_clz((unsigned)g.experts);
+    prm.each = std::max((prm.chunks + kPlacers - 1) / kPlacers, (64 + prm.chunk - 1) / prm.chunk);
+    prm.hist = (uint16_t*)g.workspace;
+    prm.padded = (g.experts + 7) / 8 * 8;
+    prm.bits = g.experts > 1 ? 32 - __builtin_clz((unsigned)g.experts - 1) : 0;
     const int E = g.experts, lpt = E <= 256 ? 16 : 64;
     const int64_t lanes = (int64_t)prm.chunk * lpt;
     const unsigned most = E <= 512 ? 1024u : 512u;                               // (counts of every wave in 64 KiB of LDS)
-    const unsigned threads = lanes >= most ? most : (unsigned)((lanes + 63) / 64 * 64);
-    const size_t place_lds = (size_t)(2 + threads / 64) * E * sizeof(int32_t);
-    const size_t route_lds = prm.chunks == 1 ? place_lds : (size_t)E * sizeof(int32_t);
+    const unsigned routing = std::min(most, (unsigned)route_threads((E > 128 && E <= 256) || E > 512 ? 16 : 8, g.bias != nullptr));
+    const unsigned threads = lanes >= routing ? routing : (unsigned)((lanes + 63) / 64 * 64);
+    const size_t route_lds = (prm.chunks == 1 ? (size_t)(2 + threads / 64) * E + (size_t)g.tokens * g.top : (size_t)E) * sizeof(int32_t);
     if (E <= 16) route_go<16, 1>(prm, threads, route_lds, s);
     else if (E <= 32) route_go<16, 2>(prm, threads, route_lds, s);
     else if (E <= 64) route_go<16, 4>(prm, threads, route_lds, s);
@@ -349,7 +428,7 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
     else if (E <= 512) route_go<64, 8>(prm, threads, route_lds, s);
     else route_go<64, 16>(prm, threads, route_lds, s);
     if (hipError_t e = hipGetLastError()) return e;
-    if (prm.chunks > 1) moe_place_kernel<<<(unsigned)prm.chunks, most, (size_t)(2 + most / 64) * E * sizeof(int32_t), s>>>(prm);
+    if (prm.chunks > 1) moe_place_kernel<<<(unsigned)((prm.chunks + prm.each - 1) / prm.each), most, (size_t)(2 + most / 64) * E * sizeof(int32_t), s>>>(prm);
     return hipGetLastError();
 }
 
@@ -366,19 +445,18 @@ static int most_groups(int rows, int experts, int per)
 
 struct MoePlan {
     bool few;                    // the few-rows kernel, else the block kernel
-    int R, MT, kparts, tgroups;  // few
+    int R, kparts, tgroups;      // few
     int shape;                   // block
 };
 
-static bool rows_plan(int p, int K, int MT, MoePlan* pl)
+static bool rows_plan(int p, int K, MoePlan* pl)
 {
     const int nsuper = (K + kSuperK - 1) / kSuperK;
     for (int R = 1; R <= 4; ++R) {
-        const int most = moe_max_waves(p, R, MT);
+        const int most = moe_max_waves(p, R);
         if (most == 0 || nsuper > R * most) continue;
         pl->few = true;
         pl->R = R;
-        pl->MT = MT;
         pl->kparts = (nsuper + R - 1) / R;
         pl->tgroups = std::max(1, 8 / pl->kparts);
         return true;
@@ -386,12 +464,17 @@ static bool rows_plan(int p, int K, int MT, MoePlan* pl)
     return false;
 }
 
+// Rows of an expert, as far as the host knows: their mean.  The few-rows kernel passes over an expert's weights once for every 16 rows that one has, the
+// block kernel's 64 x 128 tiles once for 64, which costs it a launch that packs A; they meet at 8 rows, at 14 where a weight has one or two bits
+// (us, few / block: W4A8 eight of 4096->4096, 8 rows 15.4 / 15.7, 12 rows 20.9 / 15.8, 32 rows 33 / 16.3; W2A8 thirty-two 8 rows 29 / 39, 12 rows 35 / 40, 16 rows
+// 40 / 41, 32 rows 65 / 43).  64 x 128, 128 x 128 and 256 x 256 meet at 128 and 192 (W4A8 eight of 4096->4096, 96 rows 26 / 29 / 36, 160 rows 37 / 35 / 44,
+// 256 rows 50 / 49 / 47; W8A8 sixty-four of 1408->2048, 96 rows 66 / 69 / 71, 192 rows 100 / 89 / 86).
 static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int experts)
 {
     MoePlan pl{};
     const double mean = (double)rows / std::min(experts, rows);   // rows of an expert
-    if (K >= 16 && mean <= 32 && rows_plan(p, K, mean <= 16 ? 1 : 2, &pl)) return pl;
-    pl.shape = mean >= 192 ? 0 : (mean >= 80 ? 3 : 4);
+    if (K >= 16 && mean <= (p <= 2 ? 14 : 8) && rows_plan(p, K, &pl)) return pl;
+    pl.shape = mean >= 192 ? 0 : (mean >= 128 ? 3 : 4);
     return pl;
 }
 
@@ -424,20 +507,20 @@ hipError_t launch_moe_gemm(const MoeGemmArgs& g, const WeightLayout& W, hipStrea
         prm.ow = g.p == 8 ? 128 : 0;
         prm.a_mask = (uint32_t)((1 << g.q) - 1) * 0x01010101u;
         prm.kparts = pl.kparts; prm.tgroups = pl.tgroups;
-        prm.batch = pl.kparts >= 4 ? moe_batch(pl.MT) : 2;
+        prm.batch = moe_batch(pl.kparts);
         prm.groups_n = (W.NT + pl.tgroups - 1) / pl.tgroups;
-        prm.most = most_groups(g.rows, g.experts, 16 * pl.MT);
-        const int waves = pl.kparts * pl.tgroups, room = moe_max_waves(g.p, pl.R, pl.MT);   // (waves a unit holds)
+        prm.most = most_groups(g.rows, g.experts, 16);
+        const int waves = pl.kparts * pl.tgroups, room = moe_max_waves(g.p, pl.R);   // (waves a unit holds)
         const unsigned grid = (unsigned)std::min<int64_t>((int64_t)num_cus() * std::max(1, room / waves), (int64_t)prm.most * prm.groups_n);
         switch (g.p) {
-            case 1: return moe_rows_launch_p1(prm, pl.R, pl.MT, grid, s);
-            case 2: return moe_rows_launch_p2(prm, pl.R, pl.MT, grid, s);
-            case 3: return moe_rows_launch_p3(prm, pl.R, pl.MT, grid, s);
-            case 4: return moe_rows_launch_p4(prm, pl.R, pl.MT, grid, s);
-            case 5: return moe_rows_launch_p5(prm, pl.R, pl.MT, grid, s);
-            case 6: return moe_rows_launch_p6(prm, pl.R, pl.MT, grid, s);
-            case 7: return moe_rows_launch_p7(prm, pl.R, pl.MT, grid, s);
-            default: return moe_rows_launch_p8(prm, pl.R, pl.MT, grid, s);
+            case 1: return moe_rows_launch_p1(prm, pl.R, grid, s);
+            case 2: return moe_rows_launch_p2(prm, pl.R, grid, s);
+            case 3: return moe_rows_launch_p3(prm, pl.R, grid, s);
+            case 4: return moe_rows_launch_p4(prm, pl.R, grid, s);
+            case 5: return moe_rows_launch_p5(prm, pl.R, grid, s);
+            case 6: return moe_rows_launch_p6(prm, pl.R, grid, s);
+            case 7: return moe_rows_launch_p7(prm, pl.R, grid, s);
+            default: return moe_rows_launch_p8(prm, pl.R, grid, s);
         }
     }
     ActLayout A;

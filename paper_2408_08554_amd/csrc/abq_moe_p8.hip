@@ -3,6 +3,6 @@
 #include "abq_moe_rows_kernels.h"
 
 namespace abq {
-ABQ_MOE_ROWS_LAUNCH(8) { return moe_rows_launch<8>(prm, R, MT, grid, s); }
+ABQ_MOE_ROWS_LAUNCH(8) { return moe_rows_launch<8>(prm, R, grid, s); }
 ABQ_BLOCK_EXPERTS_LAUNCH(8) { return block_experts_launch<8>(prm, shape, s); }
 }  // namespace abq

@@ -1,12 +1,13 @@
 // Device code of the few-rows kernel of experts, and the templates that launch its variants.
 //
-// Each expert's weights are multiplied by the few rows that chose it, 16 MT of them at a time.  What bounds it is the stream of the
-// weights.  The work is a list of units (expert, its 16 MT rows, a group of output tiles), dealt out in even runs to a grid that fills the chip,
+// Each expert's weights are multiplied by the few rows that chose it, 16 of them at a time.  What bounds it is the stream of the
+// weights.  The work is a list of units (expert, its 16 rows, a group of output tiles), dealt out in even runs to a grid that fills the chip,
 // whatever the groups are: one token's two experts take as many compute units as sixty-four experts do.  Inside a workgroup the waves are a
 // grid of (part of K) x (tile of the group).  A wave keeps its part of A in registers, as operands, for as long as a run stays with the same rows
 // (unpacked codes are masked and made signed once, the sums of the codes are taken on the way), and streams weights past it: as a super-chunk
-// has been multiplied, the next tile's is asked for.  The parts of K of a tile meet in LDS, and one wave after the other adds a tile up and stores it
-// while the rest go on.
+// has been multiplied, the next tile's is asked for.  The parts of K of up to four tiles meet in LDS, and all waves add them up and store them: one barrier
+// to four tiles.  (With a barrier to every tile and its sum left to one wave, W2A8 64 rows of eight 11008->4096 took 30 us; now 20.9, 4.3 TB/s of weights; W4A8
+// one token's two experts 4096->11008 14.4 and now 11.4.)
 #pragma once
 #include "abq_moe.h"
 #include "abq_rows.h"
@@ -35,16 +36,15 @@ __device__ __forceinline__ uint32_t moe_dword(const mv4i* w, int j)
     return v;
 }
 
-template <int P, int MT, int SL = 0>
-__device__ __forceinline__ void moe_super_chunk(const mv4i* w, const mv4i (*a)[8], mv4i* acc)
+template <int P, int SL = 0>
+__device__ __forceinline__ void moe_super_chunk(const mv4i* w, const mv4i* a, mv4i& acc)
 {
     if constexpr (SL < 8) {
         mv4i b;
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[j] = (int)moe_dword<P, SL>(w, j);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[mt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[mt][SL], b, acc[mt], 0, 0, 0);
-        moe_super_chunk<P, MT, SL + 1>(w, a, acc);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[SL], b, acc, 0, 0, 0);
+        moe_super_chunk<P, SL + 1>(w, a, acc);
     }
 }
 
@@ -76,19 +76,15 @@ __device__ __forceinline__ void moe_operand_at_end(mv4i& v, uint32_t mask, uint3
     v = mv4i{v[0] & (int)(uint32_t)in_lo, v[1] & (int)(uint32_t)(in_lo >> 32), v[2] & (int)(uint32_t)in_hi, v[3] & (int)(uint32_t)(in_hi >> 32)};
 }
 
-// Waves a workgroup can have with R super-chunks a wave, 0 where the variant is not built: what the registers leave (A takes 32 MT R of
+// Waves a workgroup can have with R super-chunks a wave, 0 where the variant is not built: what the registers leave (A takes 32 R of
 // them, the weights in flight 4 P R, the rest 35 to 55; variants that spill are not built).
-__host__ __device__ constexpr int moe_max_waves(int P, int R, int MT)
+__host__ __device__ constexpr int moe_max_waves(int P, int R)
 {
-    if (MT == 2) return R == 1 ? 12 : (R == 2 ? 8 : 0);
     return R == 1 ? 16 : (R == 2 ? (P <= 6 ? 12 : 0) : (R == 3 ? (P >= 7 ? 8 : 0) : (R == 4 && P <= 4 ? 8 : 0)));
 }
 
 // Tiles in flight.
-__host__ __device__ constexpr int moe_depth(int P, int R, int MT)
-{
-    return P * R <= (MT == 1 ? 4 : 4) ? 2 : 1;
-}
+__host__ __device__ constexpr int moe_depth(int P, int R) { return P * R <= 4 ? 2 : 1; }
 
 // Every wave's LDS accesses are done; loads stay in flight (a workgroup fence would wait for them).
 __device__ __forceinline__ void moe_barrier()
@@ -100,49 +96,46 @@ __device__ __forceinline__ void moe_barrier()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Tiles between two barriers, at most: their parts of K meet in LDS together, and the waves share the work of adding them up.
-__host__ __device__ constexpr int moe_batch(int MT) { return MT == 1 ? 4 : 2; }
-// LDS: [2][batch][waves][MT][64] parts of tiles, [3][tgroups][64] channels' parameters.
-static size_t moe_rows_lds_bytes(const MoeRowsParams& prm, int MT) { return (size_t)(2 * prm.batch * prm.kparts * MT + 3) * prm.tgroups * 1024; }
+// Tiles between two barriers: their parts of K meet in LDS together, and the waves share the work of adding them up (where few parts share it, two).
+static int moe_batch(int kparts) { return kparts >= 4 ? 4 : 2; }
+// LDS: [2][batch][waves][64] parts of tiles, [3][tgroups][64] channels' parameters.
+static size_t moe_rows_lds_bytes(const MoeRowsParams& prm) { return (size_t)(2 * prm.batch * prm.kparts + 3) * prm.tgroups * 1024; }
 
-template <int P, int R, int MT>
-__global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(MoeRowsParams prm)
+template <int P, int R>
+__global__ __launch_bounds__(64 * moe_max_waves(P, R)) void moe_rows_kernel(MoeRowsParams prm)
 {
-    constexpr int D = moe_depth(P, R, MT);
+    constexpr int D = moe_depth(P, R);
     extern __shared__ __align__(16) mv4i lds[];
-    __shared__ int32_t row_sum[2][16 * MT];
-    __shared__ __align__(16) RowParams par_a[16 * MT];
+    __shared__ int32_t row_sum[2][16];
+    __shared__ __align__(16) RowParams par_a[16];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, G = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tg = wave / prm.kparts, kpart = wave - tg * prm.kparts;   // (blockDim = 64 kparts tgroups)
     const int k0 = kpart * R * kSuperK, waves = prm.kparts * prm.tgroups;
-    mv4i* const red = lds;                                               // part of tile b, buffer f: at ((f batch + b) waves + wave) MT 64
-    mv4i* const par_w = lds + 2 * prm.batch * waves * MT * 64;
+    mv4i* const red = lds;                                               // part of tile b, buffer f: at ((f batch + b) waves + wave) 64
+    mv4i* const par_w = lds + 2 * prm.batch * waves * 64;
 
-    const ExpertUnits<BlocksOf> units(prm.g, BlocksOf{16 * MT}, prm.most);
+    const ExpertUnits<BlocksOf> units(prm.g, BlocksOf{16}, prm.most);
     // this workgroup's run: all units are dealt out evenly
     const unsigned all = (unsigned)units.total * (unsigned)prm.groups_n, per = all / gridDim.x, rest = all - per * gridDim.x;   // (below 2^30)
     unsigned u = blockIdx.x * per + min(blockIdx.x, rest);
     const unsigned end = u + per + (blockIdx.x < rest ? 1u : 0u);
     const uint32_t flip = prm.oa ? 0x80808080u : 0u;
-    if (tid < 16 * MT) row_sum[0][tid] = 0;
+    if (tid < 16) row_sum[0][tid] = 0;
     int sums_at = 0, buf = 0, par_at = 0;   // buffers in turn: the runs' row sums, the batches' parts, their parameters
 
     while (u < end) {
         const int block = (int)(u / (unsigned)prm.groups_n), g0 = (int)u - block * prm.groups_n;
         const int count = min((int)(end - u), prm.groups_n - g0);
         const ExpertAt at = units.find(prm.g, block);
-        const int local = (block - at.before) * 16 * MT;
-        const int row0 = at.first + local, nrow = min(max(at.rows - local, 0), 16 * MT);
+        const int local = (block - at.before) * 16;
+        const int row0 = at.first + local, nrow = min(max(at.rows - local, 0), 16);
         const uint8_t* blob = prm.w + (size_t)at.expert * prm.w_stride;
         const RowParams* wparams = reinterpret_cast<const RowParams*>(blob + prm.off_params);
         u += count;
 
         // ---- loads.  The rows' numbers first, then the weights of the run's first tiles, which need the expert alone, then what waits for the numbers.
-        int entry[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) entry[mt] = moe_order(prm.g, min(row0 + min(16 * mt + r, max(nrow - 1, 0)), prm.g.rows - 1));
-        const int par_entry = moe_order(prm.g, min(row0 + min(tid & (16 * MT - 1), max(nrow - 1, 0)), prm.g.rows - 1));
+        const int entry = moe_order(prm.g, min(row0 + min(r, max(nrow - 1, 0)), prm.g.rows - 1));
         __builtin_amdgcn_sched_barrier(0);
         mv4i w[D][R][P];
         // (past the run's end a load goes to the blob's first KiB, for nobody: a load under a condition would make every wait one for all)
@@ -174,61 +167,43 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
         };
         load_params(0, par_at);
         load_tile(0);
-        // A: lane (r, G) holds bytes 16 G .. of slice s of rows r, r + 16; rows past the group's are its last one again.  Vectors past a row's
+        // A: lane (r, G) holds bytes 16 G .. of slice s of row r; rows past the group's are its last one again.  Vectors past a row's
         // end hold what follows in memory; those past the last row's end are moved back.  Both are put right below.
-        mv4i a[R][MT][8];
-        uint32_t off[MT];
-        const uint32_t a_end = (uint32_t)prm.g.tokens * (uint32_t)prm.K - 16u;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) off[mt] = (uint32_t)moe_row(prm.g, entry[mt]) * (uint32_t)prm.K + G * 16u;
+        mv4i a[R][8];
+        const int row = moe_row(prm.g, entry);
+        const uint32_t a_end = (uint32_t)prm.g.tokens * (uint32_t)prm.K - 16u, off = (uint32_t)row * (uint32_t)prm.K + G * 16u;
         const int last_slice = (prm.K - 1) / 64 * 64;
 #pragma unroll
         for (int rr = 0; rr < R; ++rr)
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const uint32_t ks = (uint32_t)min(k0 + rr * kSuperK + s * 64, last_slice);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const u32x4_byte v = *reinterpret_cast<const u32x4_byte*>(prm.a + ks + min(off[mt], a_end - ks));
-                    a[rr][mt][s] = mv4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
-                }
+                const u32x4_byte v = *reinterpret_cast<const u32x4_byte*>(prm.a + ks + min(off, a_end - ks));
+                a[rr][s] = mv4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
             }
-        const int par_row = moe_row(prm.g, par_entry);
-        const float par_scale = prm.a_scale[par_row];
-        const int32_t par_zero = prm.a_zero[par_row];
+        const float par_scale = prm.a_scale[row];
+        const int32_t par_zero = prm.a_zero[row];
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (D == 2) load_tile(1);
         moe_barrier();   // (every wave is done with the run before: its rows' parameters and sums)
         int K = prm.K, k_lane = G * 16;
         asm volatile("" : "+s"(K), "+v"(k_lane));   // (or every slice's masks are made ahead of the loop over the runs, and spilled)
-        uint32_t sums[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sums[mt] = 0;
+        uint32_t sum_a = 0;
 #pragma unroll
         for (int rr = 0; rr < R; ++rr)
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const int ks = k0 + rr * kSuperK + s * 64;
-                if (ks >= K) {                             // (the same for every lane; past the last super-chunk the weights are its own again)
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) a[rr][mt][s] = mv4i{0, 0, 0, 0};
-                    continue;
-                }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    if (ks + 64 > K) moe_operand_at_end(a[rr][mt][s], prm.a_mask, flip, sums[mt], ks + k_lane, K, off[mt], a_end - ks);
-                    else moe_operand(a[rr][mt][s], prm.a_mask, flip, sums[mt]);
-                }
+                if (ks >= K) a[rr][s] = mv4i{0, 0, 0, 0};   // (the same for every lane; past the last super-chunk the weights are its own again)
+                else if (ks + 64 > K) moe_operand_at_end(a[rr][s], prm.a_mask, flip, sum_a, ks + k_lane, K, off, a_end - ks);
+                else moe_operand(a[rr][s], prm.a_mask, flip, sum_a);
             }
         if (tg == 0) {   // (the waves of the other tile groups hold the same parts of A)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                sums[mt] += __shfl_xor(sums[mt], 16);
-                sums[mt] += __shfl_xor(sums[mt], 32);
-                if (lane < 16) atomicAdd(&row_sum[sums_at][16 * mt + lane], (int32_t)sums[mt]);   // (whole numbers: any order)
-            }
+            sum_a += __shfl_xor(sum_a, 16);
+            sum_a += __shfl_xor(sum_a, 32);
+            if (lane < 16) atomicAdd(&row_sum[sums_at][lane], (int32_t)sum_a);   // (whole numbers: any order)
         }
-        if (tid < 16 * MT) {
+        if (tid < 16) {
             row_sum[sums_at ^ 1][tid] = 0;
             par_a[tid] = RowParams{0, par_scale, par_zero, 0};
         }
@@ -236,16 +211,13 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
         // ---- the tiles, D of them in flight, a batch of them to a barrier
         auto tile_step = [&](auto DC, int i, int b) {
             constexpr int d = decltype(DC)::value;
-            mv4i acc[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) acc[mt] = mv4i{0, 0, 0, 0};
+            mv4i acc = mv4i{0, 0, 0, 0};
 #pragma unroll
             for (int rr = 0; rr < R; ++rr) {
-                moe_super_chunk<P, MT>(w[d][rr], a[rr], acc);
+                moe_super_chunk<P>(w[d][rr], a[rr], acc);
                 load_super(d, rr, i + D);
             }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) red[(((buf * prm.batch + b) * waves + wave) * MT + mt) * 64 + lane] = acc[mt];
+            red[((buf * prm.batch + b) * waves + wave) * 64 + lane] = acc;
         };
         for (int i0 = 0; i0 < count; i0 += prm.batch) {
             const int nb = min(prm.batch, count - i0), par_next = par_at == 2 ? 0 : par_at + 1;
@@ -257,25 +229,23 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
             }
             if constexpr (D == 2) { if (b < nb) tile_step(std::integral_constant<int, 0>{}, i0 + b, b); }
             moe_barrier();
-            // tile b of rows mt of this tile group: its waves in turn
-            for (int t = kpart; t < nb * MT; t += prm.kparts) {
+            for (int t = kpart; t < nb; t += prm.kparts) {   // tiles of this tile group: its waves in turn
                 int own = lane;
                 asm volatile("" : "+v"(own));   // (or every address below is made ahead of the loop, in registers that the operands need)
-                const int b = t / MT, mt = t - b * MT;
-                const mv4i* part = red + (((buf * prm.batch + b) * waves + tg * prm.kparts) * MT + mt) * 64 + own;
+                const mv4i* part = red + ((buf * prm.batch + t) * waves + tg * prm.kparts) * 64 + own;
                 mv4i sum = mv4i{0, 0, 0, 0};
                 for (int k = 0; k < prm.kparts; k += 4) {
                     mv4i v[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = part[min(k + j, prm.kparts - 1) * (MT * 64)];
+                    for (int j = 0; j < 4; ++j) v[j] = part[min(k + j, prm.kparts - 1) * 64];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) sum += v[j] & (k + j < prm.kparts ? -1 : 0);
                 }
-                const RowParams pw = reinterpret_cast<const RowParams*>(par_w)[(par_at * prm.tgroups + tg) * 64 + b * 16 + (own & 15)];
-                const int n = ((g0 + i0 + b) * prm.tgroups + tg) * kTileN + (own & 15);
+                const RowParams pw = reinterpret_cast<const RowParams*>(par_w)[(par_at * prm.tgroups + tg) * 64 + t * 16 + (own & 15)];
+                const int n = ((g0 + i0 + t) * prm.tgroups + tg) * kTileN + (own & 15);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int m = 16 * mt + 4 * (own >> 4) + e;
+                    const int m = 4 * (own >> 4) + e;
                     RowParams pa = par_a[m];
                     pa.sum = row_sum[sums_at][m];
                     int32_t raw;
@@ -290,30 +260,29 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R, MT)) void moe_rows_kernel(
     }
 }
 
-template <int P, int R, int MT>
+template <int P, int R>
 static hipError_t moe_rows_go(const MoeRowsParams& prm, unsigned grid, hipStream_t s)
 {
     static std::atomic<bool> attr_set{false};   // (an idempotent call: a lost race only repeats it)
     if (!attr_set.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute((const void*)moe_rows_kernel<P, R, MT>, hipFuncAttributeMaxDynamicSharedMemorySize, 159 * 1024);
+        const hipError_t e = hipFuncSetAttribute((const void*)moe_rows_kernel<P, R>, hipFuncAttributeMaxDynamicSharedMemorySize, 159 * 1024);
         if (e != hipSuccess) return e;
         attr_set.store(true, std::memory_order_release);
     }
-    moe_rows_kernel<P, R, MT><<<grid, 64 * prm.kparts * prm.tgroups, moe_rows_lds_bytes(prm, MT), s>>>(prm);
+    moe_rows_kernel<P, R><<<grid, 64 * prm.kparts * prm.tgroups, moe_rows_lds_bytes(prm), s>>>(prm);
     return hipGetLastError();
 }
 
-template <int P, int R = 1, int MT = 1>
-static hipError_t moe_rows_launch(const MoeRowsParams& prm, int Rwant, int MTwant, unsigned grid, hipStream_t s)
+template <int P, int R = 1>
+static hipError_t moe_rows_launch(const MoeRowsParams& prm, int Rwant, unsigned grid, hipStream_t s)
 {
-    if constexpr (moe_max_waves(P, R, MT) > 0)
-        if (Rwant == R && MTwant == MT) return moe_rows_go<P, R, MT>(prm, grid, s);
-    if constexpr (R < 4) return moe_rows_launch<P, R + 1, MT>(prm, Rwant, MTwant, grid, s);
-    else if constexpr (MT < 2) return moe_rows_launch<P, 1, MT + 1>(prm, Rwant, MTwant, grid, s);
+    if constexpr (moe_max_waves(P, R) > 0)
+        if (Rwant == R) return moe_rows_go<P, R>(prm, grid, s);
+    if constexpr (R < 4) return moe_rows_launch<P, R + 1>(prm, Rwant, grid, s);
     else return hipErrorInvalidValue;
 }
 
-#define ABQ_MOE_ROWS_LAUNCH(P) hipError_t moe_rows_launch_p##P(const MoeRowsParams& prm, int R, int MT, unsigned grid, hipStream_t s)
+#define ABQ_MOE_ROWS_LAUNCH(P) hipError_t moe_rows_launch_p##P(const MoeRowsParams& prm, int R, unsigned grid, hipStream_t s)
 ABQ_MOE_ROWS_LAUNCH(1);
 ABQ_MOE_ROWS_LAUNCH(2);
 ABQ_MOE_ROWS_LAUNCH(3);
