@@ -129,6 +129,7 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
     const uint8_t* const fields[3] = {at.fields[0], at.fields[1], at.fields[2]};
     const RowParams* const wparams = at.wparams;
     const int nsteps = prm.nsuper * 4;
+    const int last = kExperts ? (prm.K + kBkStep - 1) / kBkStep : nsteps;   // steps that there are k for
 
     // ---- loads.  1 KiB a wave and instruction: 16 bytes per lane from base + off (all but off wave-uniform) to LDS address dst + 16 lane.
     // Written as the instruction: the compiler takes the builtin for an LDS access of unknown order and waits for every outstanding
@@ -224,7 +225,7 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
             for (int i = 0; i < kLoads; ++i) load_piece(i, min(s, nsteps - 1), ring + s * kBuf);
         }
     };
-    static_assert(S <= 6, "below");
+    static_assert(S <= 6 && kAhead <= 4, "the places of narrow groups go by the step modulo 4; the loads below");
     load_first(std::integral_constant<int, 0>{});
     load_first(std::integral_constant<int, 1>{});
     load_first(std::integral_constant<int, 2>{});
@@ -317,25 +318,31 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
             }
         }
     };
-    if constexpr (S == 2) {
-        for (int sc = 0; sc < prm.nsuper; ++sc) {
-            step_body(std::integral_constant<int, 0>{}, 4 * sc, ring, ring + kBuf);
-            step_body(std::integral_constant<int, 1>{}, 4 * sc + 1, ring + kBuf, ring);
-            step_body(std::integral_constant<int, 2>{}, 4 * sc + 2, ring, ring + kBuf);
-            step_body(std::integral_constant<int, 3>{}, 4 * sc + 3, ring + kBuf, ring);
-        }
-    } else {
-        unsigned place = 0;
-        auto go = [&](auto TC, int step) {
+    unsigned place = 0;
+    auto go = [&](auto TC, int step) {
+        constexpr int T = decltype(TC)::value;
+        if constexpr (S == 2) step_body(TC, step, ring + T % 2 * kBuf, ring + (T + 1) % 2 * kBuf);
+        else {
             const unsigned nxt = place + kBuf == S * kBuf ? 0u : place + kBuf;
             step_body(TC, step, ring + place, ring + nxt);
             place = nxt;
-        };
-        for (int sc = 0; sc < prm.nsuper; ++sc) {
-            go(std::integral_constant<int, 0>{}, 4 * sc);
-            go(std::integral_constant<int, 1>{}, 4 * sc + 1);
-            go(std::integral_constant<int, 2>{}, 4 * sc + 2);
-            go(std::integral_constant<int, 3>{}, 4 * sc + 3);
+        }
+    };
+    const int whole = kExperts ? last >> 2 : prm.nsuper;
+    for (int sc = 0; sc < whole; ++sc) {
+        go(std::integral_constant<int, 0>{}, 4 * sc);
+        go(std::integral_constant<int, 1>{}, 4 * sc + 1);
+        go(std::integral_constant<int, 2>{}, 4 * sc + 2);
+        go(std::integral_constant<int, 3>{}, 4 * sc + 3);
+    }
+    if constexpr (kExperts) {   // (K seldom is a whole number of super-chunks, and an expert's is often short)
+        const int rest = last & 3;
+        if (rest > 0) {
+            go(std::integral_constant<int, 0>{}, 4 * whole);
+            if (rest > 1) {
+                go(std::integral_constant<int, 1>{}, 4 * whole + 1);
+                if (rest > 2) go(std::integral_constant<int, 2>{}, 4 * whole + 2);
+            }
         }
     }
 

@@ -330,12 +330,12 @@ __global__ __launch_bounds__(route_threads(VPL, KIND == 2)) void moe_route_kerne
 
 __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
 {
-    extern __shared__ __align__(16) int32_t lds[];   // [experts] totals, [experts] before, [waves][experts] counts
+    extern __shared__ __align__(16) int32_t lds[];   // [padded] totals, [padded] before, [waves][experts] counts (at least [padded])
     __shared__ int32_t all;
     const MoeRouteArgs& g = prm.g;
     const int tid = threadIdx.x, E = g.experts, c0 = blockIdx.x * prm.each, waves = blockDim.x >> 6;
-    int32_t *totals = lds, *before = lds + E, *counts = lds + 2 * E;
-    for (int i = tid; i < (2 + waves) * E; i += blockDim.x) lds[i] = 0;
+    int32_t *totals = lds, *before = lds + prm.padded, *counts = lds + 2 * prm.padded;
+    for (int i = tid; i < 2 * prm.padded + max(waves * E, prm.padded); i += blockDim.x) lds[i] = 0;
     __syncthreads();
     // the chunks' counts: threads side by side along the experts (eight each), groups of them along the chunks, a thread's loads all in flight (sums of whole
     // numbers: any order)
@@ -362,15 +362,18 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (8 * f + e < E) {
-                    atomicAdd(&totals[8 * f + e], sum[e]);
-                    atomicAdd(&counts[8 * f + e], pre[e]);
-                }
+            for (int e = 0; e < 8; ++e) {   // (expert 8 f + e at e eights + f: neighbours on neighbouring banks)
+                atomicAdd(&before[e * eights + f], sum[e]);
+                atomicAdd(&counts[e * eights + f], pre[e]);
+            }
         }
     __syncthreads();
+    for (int e = tid; e < E; e += blockDim.x) totals[e] = before[(e & 7) * eights + (e >> 3)];
+    __syncthreads();
     expert_starts(prm, totals, before, &all, c0 == 0);
-    for (int e = tid; e < E; e += blockDim.x) { before[e] += counts[e]; counts[e] = 0; }
+    for (int e = tid; e < E; e += blockDim.x) before[e] += counts[(e & 7) * eights + (e >> 3)];
+    __syncthreads();
+    for (int i = tid; i < prm.padded; i += blockDim.x) counts[i] = 0;
     __syncthreads();
     const int64_t t0 = (int64_t)c0 * prm.chunk, t1 = min(t0 + (int64_t)prm.each * prm.chunk, (int64_t)g.tokens);
     place_rows(prm, g.ids + t0 * g.top, t0 * g.top, (int)(t1 - t0) * g.top, counts, before);
@@ -428,7 +431,7 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
     else if (E <= 512) route_go<64, 8>(prm, threads, route_lds, s);
     else route_go<64, 16>(prm, threads, route_lds, s);
     if (hipError_t e = hipGetLastError()) return e;
-    if (prm.chunks > 1) moe_place_kernel<<<(unsigned)((prm.chunks + prm.each - 1) / prm.each), most, (size_t)(2 + most / 64) * E * sizeof(int32_t), s>>>(prm);
+    if (prm.chunks > 1) moe_place_kernel<<<(unsigned)((prm.chunks + prm.each - 1) / prm.each), most, (size_t)(2 * prm.padded + std::max((int)(most / 64) * E, prm.padded)) * sizeof(int32_t), s>>>(prm);
     return hipGetLastError();
 }
 
@@ -467,14 +470,20 @@ static bool rows_plan(int p, int K, MoePlan* pl)
 // Rows of an expert, as far as the host knows: their mean.  The few-rows kernel passes over an expert's weights once for every 16 rows that one has, the
 // block kernel's 64 x 128 tiles once for 64, which costs it a launch that packs A; they meet at 8 rows, at 14 where a weight has one or two bits
 // (us, few / block: W4A8 eight of 4096->4096, 8 rows 15.4 / 15.7, 12 rows 20.9 / 15.8, 32 rows 33 / 16.3; W2A8 thirty-two 8 rows 29 / 39, 12 rows 35 / 40, 16 rows
-// 40 / 41, 32 rows 65 / 43).  64 x 128, 128 x 128 and 256 x 256 meet at 128 and 192 (W4A8 eight of 4096->4096, 96 rows 26 / 29 / 36, 160 rows 37 / 35 / 44,
-// 256 rows 50 / 49 / 47; W8A8 sixty-four of 1408->2048, 96 rows 66 / 69 / 71, 192 rows 100 / 89 / 86).
+// 40 / 41, 32 rows 65 / 43).  From 128 rows an expert on the tall tiles are ahead where there are enough of them: about 0.7 to a compute unit of 256 rows, 1
+// of 128 (us, 64 / 128 / 256 rows a tile: W4A8 eight of 4096->4096, 100 rows 26 / 29 / 35, 200 rows 41 / 40 / 46, 320 rows 59 / 53 / 51; of 4096->11008, 144 rows
+// 84 / 82 / 79; W3A8 eight of 8192->2048, 200 rows 41 / 48 / 70; W8A8 sixty-four of 1408->2048, 200 rows 99 / 89 / 83).  Over 48 such sizes the choice takes
+// 1.006 times the best shape's time, 1.09 at most.
 static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int experts)
 {
     MoePlan pl{};
     const double mean = (double)rows / std::min(experts, rows);   // rows of an expert
     if (K >= 16 && mean <= (p <= 2 ? 14 : 8) && rows_plan(p, K, &pl)) return pl;
-    pl.shape = mean >= 192 ? 0 : (mean >= 128 ? 3 : 4);
+    const auto tiles = [&](int shape) {   // about: the last block of an expert is part of one
+        const int bm = expert_bm(shape), bn = expert_bn(p, shape);
+        return std::min(experts, rows) * std::max(1.0, mean / bm + 0.3) * ((N + bn - 1) / bn);
+    };
+    pl.shape = mean >= 128 && tiles(0) >= 0.7 * num_cus() ? 0 : (mean >= 128 && tiles(3) >= num_cus() ? 3 : 4);
     return pl;
 }
 

@@ -177,6 +177,24 @@ def test_ragged_groups(abq, counts):
     check_gemm(abq, 2, 8, counts, 272 if len(counts) < 200 else 16, 64, seed=len(counts))
 
 
+@pytest.mark.parametrize("p", range(1, 9))
+def test_heights_of_the_last_block(abq, p):
+    """Enough tiles for 256 rows each: last blocks of an expert with every height of tile, at its borders and inside."""
+    counts = [129, 1, 256, 192, 0, 193, 128, 64, 257, 384, 385, 255, 448, 449, 0, 512, 17, 320, 130, 200, 100, 191, 250, 127]
+    check_gemm(abq, p, 8, counts, 2048 + 8 * p, 130, top=2, seed=p, behind=7)
+    check_gemm(abq, p, 5, counts[::-1], 1031 + 1024, 700, seed=p)
+
+
+@pytest.mark.parametrize("p", [2, 3, 4, 7, 8])
+@pytest.mark.parametrize("K", [64, 128, 192, 256, 400, 512, 640, 768])
+def test_k_that_ends_inside_a_super_chunk(abq, p, K):
+    """Every number of steps modulo the super-chunk's four, on every height of tile."""
+    check_gemm(abq, p, 8, [1, 33, 64, 40], 144, K, top=2, seed=K)
+    if K % 256 == 0 or p in (2, 7):
+        check_gemm(abq, p, 8, [140, 128, 150], 11008, K, seed=K)
+        check_gemm(abq, p, 8, [300, 128, 180, 200], 11008, K, top=2, seed=K)
+
+
 def test_no_rows_at_all(abq):
     check_gemm(abq, 4, 8, [0] * 8, 64, 256, top=2, behind=16)
     check_gemm(abq, 4, 8, [0] * 8, 64, 256, top=2, behind=700)
