@@ -129,7 +129,6 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
     const uint8_t* const fields[3] = {at.fields[0], at.fields[1], at.fields[2]};
     const RowParams* const wparams = at.wparams;
     const int nsteps = prm.nsuper * 4;
-    const int last = kExperts ? (prm.K + kBkStep - 1) / kBkStep : nsteps;   // steps that there are k for
 
     // ---- loads.  1 KiB a wave and instruction: 16 bytes per lane from base + off (all but off wave-uniform) to LDS address dst + 16 lane.
     // Written as the instruction: the compiler takes the builtin for an LDS access of unknown order and waits for every outstanding
@@ -328,8 +327,17 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
             place = nxt;
         }
     };
-    const int whole = kExperts ? last >> 2 : prm.nsuper;
-    for (int sc = 0; sc < whole; ++sc) {
+    int whole = prm.nsuper;
+    const int last = (prm.K + kBkStep - 1) / kBkStep;   // steps that there are k for
+    if constexpr (kExperts) whole = last >> 2;
+    if constexpr (S == 2) {
+        for (int sc = 0; sc < whole; ++sc) {
+            step_body(std::integral_constant<int, 0>{}, 4 * sc, ring, ring + kBuf);
+            step_body(std::integral_constant<int, 1>{}, 4 * sc + 1, ring + kBuf, ring);
+            step_body(std::integral_constant<int, 2>{}, 4 * sc + 2, ring, ring + kBuf);
+            step_body(std::integral_constant<int, 3>{}, 4 * sc + 3, ring + kBuf, ring);
+        }
+    } else for (int sc = 0; sc < whole; ++sc) {
         go(std::integral_constant<int, 0>{}, 4 * sc);
         go(std::integral_constant<int, 1>{}, 4 * sc + 1);
         go(std::integral_constant<int, 2>{}, 4 * sc + 2);
