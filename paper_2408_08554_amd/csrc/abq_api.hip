@@ -976,7 +976,7 @@ static int check_route_shape(int tokens, int experts, int top)
 
 size_t abq_moe_route_workspace_bytes(int tokens, int experts, int top)
 {
-    return check_route_shape(tokens, experts, top) ? 0 : moe_route_workspace_bytes(tokens, experts);
+    return check_route_shape(tokens, experts, top) ? 0 : moe_route_workspace_bytes(tokens, experts, top);
 }
 
 int abq_moe_route(int tokens, int experts, int top, const void* logits, int logits_bits, int ld, const float* bias, int sigmoid, int renormalize,
@@ -989,7 +989,7 @@ int abq_moe_route(int tokens, int experts, int top, const void* logits, int logi
     if (ld < experts) return ABQ_ERR_SHAPE;
     if (misaligned(logits) || misaligned(bias) || misaligned(ids) || misaligned(weights) || misaligned(starts) || misaligned(order) || misaligned(places) || misaligned(workspace))
         return ABQ_ERR_ALIGN;
-    const size_t need = moe_route_workspace_bytes(tokens, experts);
+    const size_t need = moe_route_workspace_bytes(tokens, experts, top);
     if (need && !workspace) return ABQ_ERR_NULL;
     if (workspace_bytes < need) return ABQ_ERR_SIZE;
     const MoeRouteArgs g{tokens, experts, top, logits_bits, ld, logits, bias, sigmoid != 0, renormalize != 0, scale, ids, weights, starts, order, places, workspace};

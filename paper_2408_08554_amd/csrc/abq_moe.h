@@ -29,7 +29,7 @@ struct MoeRouteArgs {
     int32_t *starts, *order, *places;
     void* workspace;
 };
-size_t moe_route_workspace_bytes(int tokens, int experts);
+size_t moe_route_workspace_bytes(int tokens, int experts, int top);
 hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s);
 hipError_t launch_moe_combine(int tokens, int N, int rows, int top, const uint16_t* y, int ldy, const int32_t* places, const float* weights,
                               const uint16_t* add, int ldadd, uint16_t* out, int ldout, hipStream_t s);

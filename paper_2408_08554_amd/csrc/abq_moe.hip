@@ -87,11 +87,27 @@ __device__ __forceinline__ typename KeyType<KIND>::type key_of(float x, int e)
     }
 }
 
-// Logits VPL l .. + VPL - 1 of a token, minus infinity behind the last one.  (Whole loads, none under a condition, or each waits for the one before.)
-template <int VPL, bool HALF>
+// Logits VPL l .. + VPL - 1 of a token, minus infinity behind the last one: as vectors where the lanes have as many experts as there are (unaligned: any stride of
+// rows), else one by one.  (Whole loads, none under a condition of a lane's, or each waits for the one before.)
+template <int LPT, int VPL, bool HALF>
 __device__ __forceinline__ void load_logits(const MoeRouteArgs& g, int64_t token, int l, float* x)
 {
     const int64_t row = token * g.ld;
+    constexpr int kWords = HALF ? (VPL + 1) / 2 : VPL, kVec = kWords >= 4 ? 4 : kWords;
+    typedef uint32_t Vec __attribute__((ext_vector_type(kVec), aligned(2)));
+    if (VPL > 1 && g.experts == LPT * VPL) {
+        const Vec* at = reinterpret_cast<const Vec*>((const uint8_t*)g.logits + (row + VPL * l) * (HALF ? 2 : 4));
+        uint32_t raw[kWords];
+#pragma unroll
+        for (int v = 0; v < kWords / kVec; ++v) {
+            const Vec w = at[v];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) raw[kVec * v + e] = w[e];
+        }
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) x[i] = HALF ? __half2float(__ushort_as_half((unsigned short)(raw[i / 2] >> (16 * (i & 1))))) : __uint_as_float(raw[HALF ? 0 : i]);
+        return;
+    }
     uint32_t raw[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
@@ -115,7 +131,7 @@ __device__ __forceinline__ void route_token(const MoeRouteArgs& g, int64_t token
     const auto larger = [](auto a, auto b) { return a > b ? a : b; };
     const auto sum = [](auto a, auto b) { return a + b; };
     float x[VPL];
-    load_logits<VPL, HALF>(g, token, l, x);
+    load_logits<LPT, VPL, HALF>(g, token, l, x);
     if constexpr (KIND == 2) {
         float top = -INFINITY;
         double total = 0;
@@ -222,49 +238,77 @@ __device__ __forceinline__ uint64_t same_number(int id, int bits)
     return id >= 0 ? m : 0;
 }
 
-// Places of a run of rows.  ids: their experts; counts: LDS [waves][experts], all zero; base: LDS [experts], the place of the run's first row of each
-// expert.  Every wave takes a part of the rows in order, so that the rows of one expert stay in theirs.
-__device__ __forceinline__ void place_rows(const RouteParams& prm, const int32_t* ids, int64_t slot0, int slots, int32_t* counts, const int32_t* base)
-{
-    const MoeRouteArgs& g = prm.g;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
-    const int run = (slots + 64 * waves - 1) / (64 * waves) * 64, from = wave * run, to = min(from + run, slots);
-    int32_t* mine = counts + wave * g.experts;
-    for (int i = from; i < to; i += 64) {
-        const int id = i + lane < to ? ids[i + lane] : -1;
-        const uint64_t same = same_number(id, prm.bits);
-        if (same && lane == __ffsll((unsigned long long)same) - 1) mine[id] += __popcll(same);
+// Places of a run of rows, kept in registers: every wave takes a part of the rows in order, 64 at a time, kPlaceRounds times at most, so that the rows of one
+// expert stay in theirs.
+constexpr int kPlaceRounds = 8;
+struct PlacedRows {
+    int id[kPlaceRounds], at[kPlaceRounds];   // a row's expert, its place among the wave's rows of that expert
+    int from, rounds;                         // the wave's first row, its 64s of rows
+
+    __device__ __forceinline__ PlacedRows(const int32_t* ids, int slots)   // ids: the rows' experts
+    {
+        const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+        rounds = (slots + 64 * waves - 1) / (64 * waves);
+        from = (int)(threadIdx.x >> 6) * rounds * 64;
+#pragma unroll
+        for (int i = 0; i < kPlaceRounds; ++i) {
+            const int row = from + 64 * i + lane;
+            const int v = ids[min(row, slots - 1)];
+            id[i] = i < rounds && row < slots ? v : -1;
+        }
     }
-    __syncthreads();
-    for (int e = tid; e < g.experts; e += blockDim.x) {
-        int32_t at = base[e];
-        for (int w0 = 0; w0 * run < slots; w0 += 8) {   // (of the waves that have rows; a workgroup has a multiple of eight waves, or reads the rest for nothing)
-            int32_t n[8];
+    // counts: LDS [waves][experts], all zero; becomes the waves' own
+    __device__ __forceinline__ void count(const RouteParams& prm, int32_t* counts)
+    {
+        const int lane = threadIdx.x & 63;
+        int32_t* mine = counts + (threadIdx.x >> 6) * prm.g.experts;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) n[w] = counts[min(w0 + w, waves - 1) * g.experts + e];
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                if (w0 + w < waves) counts[(w0 + w) * g.experts + e] = at;
-                at += n[w];
+        for (int i = 0; i < kPlaceRounds; ++i) {
+            if (i < rounds) {
+                const uint64_t same = same_number(id[i], prm.bits);
+                const int before = mine[max(id[i], 0)], below = __popcll(same & ((1ull << lane) - 1));
+                at[i] = before + below;
+                __builtin_amdgcn_wave_barrier();
+                if (id[i] >= 0 && below == 0) mine[id[i]] = before + __popcll(same);
+                __builtin_amdgcn_wave_barrier();
             }
         }
     }
-    __syncthreads();
-    for (int i = from; i < to; i += 64) {
-        const bool there = i + lane < to;
-        const int id = there ? ids[i + lane] : -1;
-        const uint64_t same = same_number(id, prm.bits);
-        int place = -1;
-        if (id >= 0) {
-            place = mine[id] + __popcll(same & ((1ull << lane) - 1));
-            g.order[place] = (int32_t)(slot0 + i + lane);
+    // ... and base: LDS [experts], the place of the run's first row of each expert: order and places of the rows from slot0 on
+    __device__ __forceinline__ void store(const RouteParams& prm, int64_t slot0, int slots, int32_t* counts, const int32_t* base)
+    {
+        const MoeRouteArgs& g = prm.g;
+        const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+        __syncthreads();
+        for (int e = threadIdx.x; e < g.experts; e += blockDim.x) {
+            int32_t next = base[e];
+            for (int w0 = 0; w0 < waves; w0 += 8) {   // (loads first: the compiler takes every store for one to what is loaded next)
+                int32_t n[8];
+#pragma unroll
+                for (int w = 0; w < 8; ++w) n[w] = counts[min(w0 + w, waves - 1) * g.experts + e];
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    if (w0 + w < waves) counts[(w0 + w) * g.experts + e] = next;
+                    next += n[w];
+                }
+            }
         }
-        if (there) g.places[slot0 + i + lane] = place;
-        __builtin_amdgcn_wave_barrier();
-        if (same && lane == __ffsll((unsigned long long)same) - 1) mine[id] += __popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        __syncthreads();
+        const int32_t* mine = counts + (threadIdx.x >> 6) * g.experts;
+#pragma unroll
+        for (int i = 0; i < kPlaceRounds; ++i) {
+            const int row = from + 64 * i + lane;
+            if (i < rounds && row < slots) {
+                int place = -1;
+                if (id[i] >= 0) {
+                    place = mine[id[i]] + at[i];
+                    g.order[place] = (int32_t)(slot0 + row);
+                }
+                g.places[slot0 + row] = place;
+            }
+        }
     }
-}
+};
 
 // Sums of totals[0..experts-1] (LDS) before each expert, by the first wave; returns (to that wave) the sum of all.  Ends with a barrier.
 __device__ __forceinline__ void expert_starts(const RouteParams& prm, const int32_t* totals, int32_t* before, int32_t* all, bool store)
@@ -319,12 +363,14 @@ __global__ __launch_bounds__(route_threads(VPL, KIND == 2)) void moe_route_kerne
         }
     }
     __syncthreads();
-    if (!alone) {   // (a count is at most a chunk's tokens, which kRouteTokens keeps below 2^16)
+    if (!alone) {   // (a count is at most a chunk's tokens)
         for (int e = tid; e < prm.padded; e += blockDim.x) prm.hist[(size_t)blockIdx.x * prm.padded + e] = (uint16_t)(e < E ? lds[e] : 0);
         return;
     }
+    PlacedRows rows(lds + counted, g.tokens * g.top);
+    rows.count(prm, lds + 2 * E);
     expert_starts(prm, lds, lds + E, &all, true);
-    place_rows(prm, lds + counted, 0, g.tokens * g.top, lds + 2 * E, lds + E);
+    rows.store(prm, 0, g.tokens * g.top, lds + 2 * E, lds + E);
     for (int i = all + tid; i < g.tokens * g.top; i += blockDim.x) g.order[i] = -1;
 }
 
@@ -335,6 +381,9 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     const MoeRouteArgs& g = prm.g;
     const int tid = threadIdx.x, E = g.experts, c0 = blockIdx.x * prm.each, waves = blockDim.x >> 6;
     int32_t *totals = lds, *before = lds + prm.padded, *counts = lds + 2 * prm.padded;
+    const int64_t t0 = (int64_t)c0 * prm.chunk, t1 = min(t0 + (int64_t)prm.each * prm.chunk, (int64_t)g.tokens);
+    const int slots = (int)(t1 - t0) * g.top;
+    PlacedRows rows(g.ids + t0 * g.top, slots);
     for (int i = tid; i < 2 * prm.padded + max(waves * E, prm.padded); i += blockDim.x) lds[i] = 0;
     __syncthreads();
     // the chunks' counts: threads side by side along the experts (eight each), groups of them along the chunks, a thread's loads all in flight (sums of whole
@@ -345,20 +394,22 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
         for (int f = tid % wide; f < eights; f += wide) {
             int sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, pre[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             for (int k0 = group; k0 < prm.chunks; k0 += 8 * groups) {
-                uint4 n[8];
+                uint4 n[8], some = {0, 0, 0, 0}, rest = {0, 0, 0, 0};   // (two counts a word: eight of at most kRouteLongest tokens stay below 2^16)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) n[u] = hist[(size_t)min(k0 + u * groups, prm.chunks - 1) * eights + f];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const int k = k0 + u * groups;
-                    const int all_of = k < prm.chunks ? 0xFFFF : 0, before_of = k < c0 ? 0xFFFF : 0;
-                    const uint32_t w[4] = {n[u].x, n[u].y, n[u].z, n[u].w};
+                    const uint32_t before_of = k < c0 ? ~0u : 0u, rest_of = k >= c0 && k < prm.chunks ? ~0u : 0u;
+                    some.x += n[u].x & before_of; some.y += n[u].y & before_of; some.z += n[u].z & before_of; some.w += n[u].w & before_of;
+                    rest.x += n[u].x & rest_of; rest.y += n[u].y & rest_of; rest.z += n[u].z & rest_of; rest.w += n[u].w & rest_of;
+                }
+                const uint32_t a[4] = {some.x, some.y, some.z, some.w}, b[4] = {rest.x, rest.y, rest.z, rest.w};
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int v = (int)(w[e >> 1] >> (16 * (e & 1)));
-                        sum[e] += v & all_of;
-                        pre[e] += v & before_of;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const int v = (int)(a[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
+                    pre[e] += v;
+                    sum[e] += v + (int)(b[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
                 }
             }
 #pragma unroll
@@ -375,25 +426,28 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     __syncthreads();
     for (int i = tid; i < prm.padded; i += blockDim.x) counts[i] = 0;
     __syncthreads();
-    const int64_t t0 = (int64_t)c0 * prm.chunk, t1 = min(t0 + (int64_t)prm.each * prm.chunk, (int64_t)g.tokens);
-    place_rows(prm, g.ids + t0 * g.top, t0 * g.top, (int)(t1 - t0) * g.top, counts, before);
+    rows.count(prm, counts);
+    rows.store(prm, t0 * g.top, slots, counts, before);
     for (int64_t i = all + (int64_t)blockIdx.x * blockDim.x + tid; i < (int64_t)g.tokens * g.top; i += (int64_t)gridDim.x * blockDim.x) g.order[i] = -1;
 }
 
-// Tokens of a single launch; of more, chunks of kRouteTokens (as many as the chip's units can have two of, or longer ones), placed by fewer workgroups, each of
-// which reads all chunks' counts.
-constexpr int kRouteOne = 256, kRouteTokens = 16, kRouteChunks = 512, kPlacers = 128;
+// Tokens of a single launch; of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which
+// reads all chunks' counts and has room for the rows of place_room().
+constexpr int kRouteOne = 256, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
 
-static void route_chunks(int tokens, int* chunk, int* chunks)
+static int place_threads(int experts) { return experts <= 512 ? 1024 : 512; }   // (the counts of every wave in 64 KiB of LDS)
+static int place_room(int experts) { return place_threads(experts) * kPlaceRounds; }
+
+static void route_chunks(int tokens, int experts, int top, int* chunk, int* chunks)
 {
-    *chunk = tokens <= kRouteOne ? tokens : std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks);
+    *chunk = tokens <= kRouteOne ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
     *chunks = (tokens + *chunk - 1) / *chunk;
 }
 
-size_t moe_route_workspace_bytes(int tokens, int experts)
+size_t moe_route_workspace_bytes(int tokens, int experts, int top)
 {
     int chunk, chunks;
-    route_chunks(tokens, &chunk, &chunks);
+    route_chunks(tokens, experts, top, &chunk, &chunks);
     return chunks == 1 ? 0 : (size_t)chunks * ((experts + 7) / 8 * 8) * sizeof(uint16_t);
 }
 
@@ -412,14 +466,14 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
 {
     RouteParams prm;
     prm.g = g;
-    route_chunks(g.tokens, &prm.chunk, &prm.chunks);
-    prm.each = std::max((prm.chunks + kPlacers - 1) / kPlacers, (64 + prm.chunk - 1) / prm.chunk);
+    route_chunks(g.tokens, g.experts, g.top, &prm.chunk, &prm.chunks);
+    prm.each = std::min(std::max((prm.chunks + kPlacers - 1) / kPlacers, (64 + prm.chunk - 1) / prm.chunk), place_room(g.experts) / (prm.chunk * g.top));
     prm.hist = (uint16_t*)g.workspace;
     prm.padded = (g.experts + 7) / 8 * 8;
     prm.bits = g.experts > 1 ? 32 - __builtin_clz((unsigned)g.experts - 1) : 0;
     const int E = g.experts, lpt = E <= 256 ? 16 : 64;
     const int64_t lanes = (int64_t)prm.chunk * lpt;
-    const unsigned most = E <= 512 ? 1024u : 512u;                               // (counts of every wave in 64 KiB of LDS)
+    const unsigned most = (unsigned)place_threads(E);
     const unsigned routing = std::min(most, (unsigned)route_threads((E > 128 && E <= 256) || E > 512 ? 16 : 8, g.bias != nullptr));
     const unsigned threads = lanes >= routing ? routing : (unsigned)((lanes + 63) / 64 * 64);
     const size_t route_lds = (prm.chunks == 1 ? (size_t)(2 + threads / 64) * E + (size_t)g.tokens * g.top : (size_t)E) * sizeof(int32_t);
