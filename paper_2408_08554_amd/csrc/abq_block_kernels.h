@@ -463,15 +463,32 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
     }
 }
 
+// 256 rows of experts: tiles of a wave along N (widths of more than one group of planes: 192 channels, or one of the bodies spills).
+__host__ __device__ constexpr int bk_expert_nt(int p) { return p == 3 || p == 6 || p == 7 ? 3 : 4; }
+__host__ __device__ constexpr int bk_slow_bytes(int p, int tw, int ahead) { return tw * bk_slow_first(p, group_count(p), ahead) * 1024; }
+// Places in the ring of a body of 32 mt rows of experts: as many as fit, at most four.
+__host__ __device__ constexpr int bk_expert_s(int p, int mt)
+{
+    int s = 2;
+    const int tw = 4 * bk_expert_nt(p);
+    while (s < 4 && (s + 1) * bk_buf_bytes(p, 32 * mt, tw) + bk_slow_bytes(p, tw, s + 1) + 8192 + 1024 <= 160 * 1024) ++s;
+    return s;
+}
+__host__ __device__ constexpr int bk_most(int a, int b, int c) { return a > b ? (a > c ? a : c) : (b > c ? b : c); }
+
 // OCC: waves per SIMD that the registers are held to.  PRM: BlockParams or BlockExpertParams.
 template <int P, int RW, int CW, int MT, int NT, int S, int OCC, class PRM = BlockParams>
 __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
 {
     constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
-    constexpr int kSlow = kTW * bk_slow_first(P, group_count(P), bk_slow_ahead(kExperts, S)) * 1024;
-    __shared__ __align__(1024) uint8_t ring[S * bk_buf_bytes(P, kBM, kTW)];
-    __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
+    constexpr int S6 = bk_expert_s(P, 6), S4 = bk_expert_s(P, 4);   // (of experts: the shorter bodies' rings)
+    constexpr bool kHeights = kExperts && MT == 8;
+    constexpr int kRing = S * bk_buf_bytes(P, kBM, kTW), kSlow = bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, S));
+    constexpr int kRings = kHeights ? bk_most(kRing, S6 * bk_buf_bytes(P, 192, kTW), S4 * bk_buf_bytes(P, 128, kTW)) : kRing;
+    constexpr int kSlows = kHeights ? bk_most(kSlow, bk_slow_bytes(P, kTW, S6), bk_slow_bytes(P, kTW, S4)) : kSlow;
+    __shared__ __align__(1024) uint8_t ring[kRings];
+    __shared__ __align__(1024) uint8_t lds_slow[kSlows > 0 ? kSlows : 16];
     __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
     const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
     BlockTile at;
@@ -503,8 +520,8 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
         if constexpr (MT == 8) {
             static_assert(kBM == 256, "the heights");
             if (some(BlocksBetween<256, 192, 256>{})) block_body<P, RW, CW, 8, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, S6>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, S4>(prm, at, ring, lds_slow, par_a, par_w);
         } else if (some(BlocksOf{kBM})) {   // (the grid is what there can be at most)
             block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
         }
@@ -546,15 +563,13 @@ static hipError_t block_launch(const BlockParams& prm, int shape, hipStream_t s)
     }
 }
 
-// 256 rows of experts: tiles of a wave along N (widths of more than one group of planes: 192 channels, or one of the bodies spills).
-__host__ __device__ constexpr int bk_expert_nt(int p) { return p == 3 || p == 6 || p == 7 ? 3 : 4; }
 // Experts: 256 x 256 (or 192), 128 x 128 by four waves and 64 x 128 (shapes 0, 3, 4 above).
 template <int P>
 static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, hipStream_t s)
 {
     const unsigned grid = (unsigned)(prm.tiles_m * prm.tiles_n);
     switch (shape) {
-        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), 2, 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
+        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), bk_expert_s(P, 8), 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
         case 3: block_kernel<P, 2, 2, 4, 4, P >= 4 ? 2 : 3, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         case 4: block_kernel<P, 1, 4, 4, 2, P >= 6 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         default: return hipErrorInvalidValue;
