@@ -466,12 +466,11 @@ __device__ __forceinline__ void block_body(const PRM& prm, const BlockTile& at, 
 // 256 rows of experts: tiles of a wave along N (widths of more than one group of planes: 192 channels, or one of the bodies spills).
 __host__ __device__ constexpr int bk_expert_nt(int p) { return p == 3 || p == 6 || p == 7 ? 3 : 4; }
 __host__ __device__ constexpr int bk_slow_bytes(int p, int tw, int ahead) { return tw * bk_slow_first(p, group_count(p), ahead) * 1024; }
-// Places in the ring of a body of 32 mt rows of experts: as many as fit, at most four.
-__host__ __device__ constexpr int bk_expert_s(int p, int mt)
+// Places in the ring of a body of bm rows and tw tiles of channels of experts: as many as `room` KiB hold beside its records, two to four.
+__host__ __device__ constexpr int bk_expert_s(int p, int bm, int tw, int room)
 {
     int s = 2;
-    const int tw = 4 * bk_expert_nt(p);
-    while (s < 4 && (s + 1) * bk_buf_bytes(p, 32 * mt, tw) + bk_slow_bytes(p, tw, s + 1) + 8192 + 1024 <= 160 * 1024) ++s;
+    while (s < 4 && (s + 1) * bk_buf_bytes(p, bm, tw) + bk_slow_bytes(p, tw, s + 1) + 16 * ((bm + 63) / 64 * 64 + (16 * tw + 63) / 64 * 64) <= room * 1024) ++s;
     return s;
 }
 __host__ __device__ constexpr int bk_most(int a, int b, int c) { return a > b ? (a > c ? a : c) : (b > c ? b : c); }
@@ -482,11 +481,12 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
 {
     constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
     constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
-    constexpr int S6 = bk_expert_s(P, 6), S4 = bk_expert_s(P, 4);   // (of experts: the shorter bodies' rings)
-    constexpr bool kHeights = kExperts && MT == 8;
-    constexpr int kRing = S * bk_buf_bytes(P, kBM, kTW), kSlow = bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, S));
-    constexpr int kRings = kHeights ? bk_most(kRing, S6 * bk_buf_bytes(P, 192, kTW), S4 * bk_buf_bytes(P, 128, kTW)) : kRing;
-    constexpr int kSlows = kHeights ? bk_most(kSlow, bk_slow_bytes(P, kTW, S6), bk_slow_bytes(P, kTW, S4)) : kSlow;
+    // (of experts: the heights of the shorter bodies, in sixteens, and their rings)
+    constexpr bool kTall = kExperts && MT == 8, kMiddle = kExperts && MT == 4 && RW == 2;
+    constexpr int MB = kTall ? 6 : (kMiddle ? 3 : MT), MC = kTall ? 4 : MB, kRoom = kTall ? 160 : 80;
+    constexpr int SB = kTall || kMiddle ? bk_expert_s(P, 16 * MB * RW, kTW, kRoom) : S, SC = kTall ? bk_expert_s(P, 16 * MC * RW, kTW, kRoom) : SB;
+    constexpr int kRings = bk_most(S * bk_buf_bytes(P, kBM, kTW), SB * bk_buf_bytes(P, 16 * MB * RW, kTW), SC * bk_buf_bytes(P, 16 * MC * RW, kTW));
+    constexpr int kSlows = bk_most(bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, S)), bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, SB)), bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, SC)));
     __shared__ __align__(1024) uint8_t ring[kRings];
     __shared__ __align__(1024) uint8_t lds_slow[kSlows > 0 ? kSlows : 16];
     __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
@@ -509,19 +509,20 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
             const int in_expert = vid - e.before * prm.tiles_n, tiles_m = of(e.rows), last = (e.rows + kBM - 1) / kBM;
             const int band = in_expert / (prm.band_m * prm.tiles_n), in_band = in_expert - band * prm.band_m * prm.tiles_n;
             const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
-            // (an expert has one block at most that is not of the tallest, its last)
-            const int m_blk = std::is_same<decltype(of), BlocksBetween<256, 0, 128>>::value || std::is_same<decltype(of), BlocksBetween<256, 128, 192>>::value ? last - 1 : band * prm.band_m + in_band % band_rows;
+            const int m_blk = decltype(of)::kLast ? last - 1 : band * prm.band_m + in_band % band_rows;
             const int n_blk = in_band / band_rows;
             at = BlockTile{{prm.fields[0] + (size_t)e.expert * prm.w_stride, prm.fields[1] + (size_t)e.expert * prm.w_stride, prm.fields[2] + (size_t)e.expert * prm.w_stride},
                            reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(prm.wparams) + (size_t)e.expert * prm.w_stride),
                            e.rows, e.first, m_blk * kBM, n_blk * kBN, n_blk * kTW};
             return true;
         };
-        if constexpr (MT == 8) {
-            static_assert(kBM == 256, "the heights");
+        if constexpr (kTall) {
             if (some(BlocksBetween<256, 192, 256>{})) block_body<P, RW, CW, 8, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, S6>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, S4>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, SC>(prm, at, ring, lds_slow, par_a, par_w);
+        } else if constexpr (kMiddle) {
+            if (some(BlocksBetween<128, 96, 128>{})) block_body<P, RW, CW, 4, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+            else if (some(BlocksBetween<128, 0, 96>{})) block_body<P, RW, CW, 3, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
         } else if (some(BlocksOf{kBM})) {   // (the grid is what there can be at most)
             block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
         }
@@ -563,15 +564,15 @@ static hipError_t block_launch(const BlockParams& prm, int shape, hipStream_t s)
     }
 }
 
-// Experts: 256 x 256 (or 192), 128 x 128 by four waves and 64 x 128 (shapes 0, 3, 4 above).
+// Experts: 256 x 256 (or 192) with shorter tiles of 192 and 128 rows, 128 x 128 by four waves with shorter ones of 96 rows, and 64 x 128 (shapes 0, 3, 4 above).
 template <int P>
 static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, hipStream_t s)
 {
     const unsigned grid = (unsigned)(prm.tiles_m * prm.tiles_n);
     switch (shape) {
-        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), bk_expert_s(P, 8), 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
-        case 3: block_kernel<P, 2, 2, 4, 4, P >= 4 ? 2 : 3, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
-        case 4: block_kernel<P, 1, 4, 4, 2, P >= 6 ? 3 : 4, 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), bk_expert_s(P, 256, 4 * bk_expert_nt(P), 160), 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
+        case 3: block_kernel<P, 2, 2, 4, 4, bk_expert_s(P, 128, 8, 80), 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        case 4: block_kernel<P, 1, 4, 4, 2, bk_expert_s(P, 64, 8, 80), 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

@@ -122,12 +122,14 @@ struct ExpertUnits {
 };
 // Blocks of `per` rows, the last one with what is left.
 struct BlocksOf {
+    static constexpr bool kLast = false;
     int per;
     __device__ __forceinline__ int operator()(int rows) const { return (rows + per - 1) / per; }
 };
 // Of those with LO + 1 .. HI rows.
 template <int PER, int LO, int HI>
 struct BlocksBetween {
+    static constexpr bool kLast = HI != PER;   // an expert has one at most, its last
     __device__ __forceinline__ int operator()(int rows) const { return (HI == PER ? rows / PER : 0) + (rows % PER > LO && rows % PER <= HI ? 1 : 0); }
 };
 

@@ -490,7 +490,7 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
 }
 
 // ---- the products: choice of kernel --------------------------------------------------------------
-// Workgroup shapes of the block kernel: 0 (256 x 256), 3 (128 x 128), 4 (64 x 128).
+// Workgroup shapes of the block kernel: 0 (256 x 256, or 192 channels), 3 (128 x 128), 4 (64 x 128).
 static int expert_bm(int shape) { return shape == 0 ? 256 : (shape == 3 ? 128 : 64); }
 static int expert_bn(int p, int shape) { return shape == 0 ? 64 * bk_expert_nt(p) : 128; }
 
@@ -524,10 +524,10 @@ static bool rows_plan(int p, int K, MoePlan* pl)
 // Rows of an expert, as far as the host knows: their mean.  The few-rows kernel passes over an expert's weights once for every 16 rows that one has, the
 // block kernel's 64 x 128 tiles once for 64, which costs it a launch that packs A; they meet at 8 rows, at 14 where a weight has one or two bits
 // (us, few / block: W4A8 eight of 4096->4096, 8 rows 15.4 / 15.7, 12 rows 20.9 / 15.8, 32 rows 33 / 16.3; W2A8 thirty-two 8 rows 29 / 39, 12 rows 35 / 40, 16 rows
-// 40 / 41, 32 rows 65 / 43).  From 128 rows an expert on the tall tiles are ahead where there are enough of them: about 0.7 to a compute unit of 256 rows, 1
-// of 128 (us, 64 / 128 / 256 rows a tile: W4A8 eight of 4096->4096, 100 rows 26 / 29 / 35, 200 rows 41 / 40 / 46, 320 rows 59 / 53 / 51; of 4096->11008, 144 rows
-// 84 / 82 / 79; W3A8 eight of 8192->2048, 200 rows 41 / 48 / 70; W8A8 sixty-four of 1408->2048, 200 rows 99 / 89 / 83).  Over 48 such sizes the choice takes
-// 1.006 times the best shape's time, 1.09 at most.
+// 40 / 41, 32 rows 65 / 43).  Tiles of up to 256 rows are ahead from 80 rows an expert on where there are 1.2 of them to a compute unit, from 192 on with 0.7; of up to 128
+// rows from 100 on with one to a unit (us, 64 / 128 / 256 rows a tile: W4A8 eight of 4096->4096, 90 rows 26 / 28 / 35, 144 rows 32 / 30 / 45; of 4096->11008, 110
+// rows 70 / 70 / 66, 180 rows 98 / 94 / 83; W3A8 eight of 8192->2048, 180 rows 41 / 46 / 71; W8A8 sixty-four of 1408->2048, 180 rows 91 / 86 / 78).  Over 58 such
+// sizes the choice takes 1.007 times the best shape's time, 1.09 at most.
 static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int experts)
 {
     MoePlan pl{};
@@ -537,7 +537,7 @@ static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int ex
         const int bm = expert_bm(shape), bn = expert_bn(p, shape);
         return std::min(experts, rows) * std::max(1.0, mean / bm + 0.3) * ((N + bn - 1) / bn);
     };
-    pl.shape = mean >= 128 && tiles(0) >= 0.7 * num_cus() ? 0 : (mean >= 128 && tiles(3) >= num_cus() ? 3 : 4);
+    pl.shape = (mean >= 80 && tiles(0) >= 1.2 * num_cus()) || (mean >= 192 && tiles(0) >= 0.7 * num_cus()) ? 0 : (mean >= 100 && tiles(3) >= num_cus() ? 3 : 4);
     return pl;
 }
 

@@ -183,6 +183,7 @@ def test_heights_of_the_last_block(abq, p):
     counts = [129, 1, 256, 192, 0, 193, 128, 64, 257, 384, 385, 255, 448, 449, 0, 512, 17, 320, 130, 200, 100, 191, 250, 127]
     check_gemm(abq, p, 8, counts, 2048 + 8 * p, 130, top=2, seed=p, behind=7)
     check_gemm(abq, p, 5, counts[::-1], 1031 + 1024, 700, seed=p)
+    check_gemm(abq, p, 8, [97, 96, 128, 129, 0, 225, 1, 95, 224, 90], 4099, 640, top=2, seed=p, behind=3)   # (128 rows a tile, and 96)
 
 
 @pytest.mark.parametrize("p", [2, 3, 4, 7, 8])
