@@ -492,7 +492,7 @@ int abq_moe_route(int tokens, int experts, int top, const void* logits, int logi
  *   y_fp16   [rows][N] binary16: rows from starts[experts] on are left as they were
  * starts and order are never checked on the host.  Whatever they hold, nothing outside the tensors is read or written; starts that do
  * not ascend, and entries of order that name no row of A, leave the rows concerned with unspecified contents.
- *   1 <= rows, tokens <= 2^22;  tokens * K (K rounded up to 512) < 2^32;  (rows / 64 + experts) * ceil(N / 128) < 2^24;
+ *   1 <= rows, tokens <= 2^22;  N <= 2^27;  tokens * K (K rounded up to 512) < 2^32;  (rows / 64 + experts) * ceil(N / 128) < 2^24;
  *   the rest as for abq_gemm.  Workspace: at least abq_moe_gemm_workspace_bytes(...) bytes (0 where an expert has few rows: the codes
  *   are packed on the way there); contents on entry are irrelevant, calls that may overlap need one each. */
 size_t abq_moe_gemm_workspace_bytes(int p, int q, int rows, int N, int K, int tokens, int experts);

@@ -996,11 +996,11 @@ int abq_moe_route(int tokens, int experts, int top, const void* logits, int logi
     return hip_status(launch_moe_route(g, (hipStream_t)stream));
 }
 
-// Rows, and workgroups of 64 x 128 outputs, that a launch can have; packed rows of A below 4 GiB (their offsets have 32 bits).
+// Rows, and workgroups of 64 x 128 outputs, that a launch can have; packed rows of A and the channels' parameters below 4 GiB (their offsets have 32 bits).
 static int check_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int w_layout)
 {
     if (int e = check_gemm_shape(p, q, rows, N, K)) return e;
-    if (rows > (1 << 22) || tokens < 1 || tokens > (1 << 22) || experts < 1 || experts > ABQ_MOE_MAX_EXPERTS) return ABQ_ERR_SHAPE;
+    if (rows > (1 << 22) || N > (1 << 27) || tokens < 1 || tokens > (1 << 22) || experts < 1 || experts > ABQ_MOE_MAX_EXPERTS) return ABQ_ERR_SHAPE;
     if (((int64_t)rows / 64 + (experts < rows ? experts : rows)) * (((int64_t)N + 127) / 128) >= (1 << 24)) return ABQ_ERR_SHAPE;
     if ((int64_t)tokens * ((K + kSuperK - 1) / kSuperK * kSuperK) >= (1LL << 32)) return ABQ_ERR_SHAPE;
     return w_layout == ABQ_LAYOUT_AUTO || w_layout == ABQ_LAYOUT_FIELDS || w_layout == ABQ_LAYOUT_BOTH ? ABQ_OK : ABQ_ERR_LAYOUT;

@@ -59,7 +59,7 @@ __device__ __forceinline__ void moe_operand(mv4i& v, uint32_t mask, uint32_t fli
     }
 }
 // The same from k on where the row of K ends among them or before: zeros behind its end (the weights there are those of code 0, which
-// eight-bit blobs hold as -128).  They were loaded from `at`, or from the tensor's last sixteen bytes if those come first.
+// eight-bit blobs hold as -128).  They were loaded from `at`, or from `last`, the tensor's last sixteen bytes, if those come first.
 __device__ __forceinline__ void moe_operand_at_end(mv4i& v, uint32_t mask, uint32_t flip, uint32_t& sum, int k, int K, uint32_t at, uint32_t last)
 {
     uint64_t lo = (uint32_t)v[0] | (uint64_t)(uint32_t)v[1] << 32, hi = (uint32_t)v[2] | (uint64_t)(uint32_t)v[3] << 32;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R)) void moe_rows_kernel(MoeR
         for (int rr = 0; rr < R; ++rr)
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
-                const uint32_t ks = (uint32_t)min(k0 + rr * kSuperK + s * 64, last_slice);
+                const uint32_t ks = min((uint32_t)min(k0 + rr * kSuperK + s * 64, last_slice), a_end);   // (a single row's last slice may begin behind a_end)
                 const u32x4_byte v = *reinterpret_cast<const u32x4_byte*>(prm.a + ks + min(off, a_end - ks));
                 a[rr][s] = mv4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
             }
@@ -195,7 +195,10 @@ __global__ __launch_bounds__(64 * moe_max_waves(P, R)) void moe_rows_kernel(MoeR
             for (int s = 0; s < 8; ++s) {
                 const int ks = k0 + rr * kSuperK + s * 64;
                 if (ks >= K) a[rr][s] = mv4i{0, 0, 0, 0};   // (the same for every lane; past the last super-chunk the weights are its own again)
-                else if (ks + 64 > K) moe_operand_at_end(a[rr][s], prm.a_mask, flip, sum_a, ks + k_lane, K, off, a_end - ks);
+                else if (ks + 64 > K) {
+                    const uint32_t from = min((uint32_t)ks, a_end);
+                    moe_operand_at_end(a[rr][s], prm.a_mask, flip, sum_a, ks + k_lane, K, ks - from + off, a_end - from);
+                }
                 else moe_operand(a[rr][s], prm.a_mask, flip, sum_a);
             }
         if (tg == 0) {   // (the waves of the other tile groups hold the same parts of A)

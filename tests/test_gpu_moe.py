@@ -82,6 +82,22 @@ def test_experts_that_are_not_there(abq, T, half, kw):
     check_route(abq, torch.full((T, 24), -INF, dtype=x.dtype), 3, **kw)
 
 
+@pytest.mark.parametrize("half", [False, True])
+def test_logits_at_the_ends_of_their_type(abq, half):
+    """The smallest values beside zeros of both signs, the largest of both signs: all different, or ties."""
+    t = torch.float16 if half else torch.float32
+    f = torch.finfo(t)
+    values = [0.0, -0.0, f.smallest_normal, -f.smallest_normal, f.max, f.min, 1.0, -1.0, 1 + f.eps, -1 - f.eps] + [k * f.smallest_normal * f.eps for k in (1, 2, 3, -1, -2, -3)]
+    g = torch.Generator().manual_seed(2)
+    x = torch.tensor(values, dtype=torch.float64)[torch.randint(0, len(values), (200, 40), generator=g)].to(t)
+    assert ((x != 0) & (x.abs() < f.smallest_normal)).any()
+    got = check_route(abq, x, 8)
+    assert (got[0] >= 0).all()
+    x[:, 7] = INF   # the choice; what becomes of the weights is not said
+    ids = abq.abq_moe_route(x.cuda(), 3)[0].cpu()
+    assert (ids[:, 0] == 7).all() and torch.equal(ids[:, 1:].long(), routed(torch.cat([x[:, :7], x[:, 8:]], 1), 2)[0] + (routed(torch.cat([x[:, :7], x[:, 8:]], 1), 2)[0] >= 7).long())
+
+
 def test_a_bias_takes_experts_out(abq):
     bias = torch.zeros(12)
     bias[::2] = -INF
@@ -161,6 +177,21 @@ def test_lengths_that_divide_nothing(abq, K, top):
         check_gemm(abq, p, q, [2, 0, 1, 9], 40, K, top=top, seed=K)
         check_gemm(abq, p, q, [40, 60], 40, K, top=top, seed=K)
     check_gemm(abq, 4, 8, [1], 16, K, top=top)
+
+
+@pytest.mark.parametrize("T,K", [(1, 16), (1, 79), (1, 65), (1, 127), (1, 143), (1, 527), (1, 4111), (2, 79), (3, 1039)])
+def test_codes_that_end_with_their_allocation(abq, T, K):
+    """The last slice of the last row, also where it is the only row's and less than sixteen codes are left for it: the vectors that hold it are moved back
+    into the tensor, which ends with a 32 MiB allocation but for its alignment."""
+    s = layer(4, 8, 2, 40, K, T, K)
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    whole = torch.zeros(32 << 20, dtype=torch.uint8, device="cuda")
+    at = (len(whole) - T * K) // 16 * 16
+    codes = whole[at:at + T * K].view(T, K)
+    codes.copy_(s["a"][0])
+    starts = groups([T - 1, 1])
+    y = abq.abq_moe_gemm(4, 8, 40, codes, s["a"][1].cuda(), s["a"][2].cuda(), w, starts.cuda())
+    assert torch.equal(y.cpu().view(torch.int16), gemm(*s["a"], *s["w"], 4, 8, starts, None, 1, T).view(torch.int16))
 
 
 @pytest.mark.parametrize("N", [1, 2, 7, 15, 16, 17, 33, 127, 129, 255, 257, 1003])

@@ -27,7 +27,7 @@ def gemm(p=4, q=8, rows=32, N=128, K=256, T=16, E=4, top=2, a=A16, s=A16, z=A16,
 BAD_GEMM = [({n: None}, NULL) for n in ("a", "s", "z", "w", "starts", "y")] + [({n: A16 + 8}, ALIGN) for n in ("a", "s", "z", "w", "starts", "order", "y", "ws")]
 BAD_GEMM += [(dict(p=0), BITS), (dict(p=9), BITS), (dict(q=0), BITS), (dict(q=9), BITS), (dict(rows=0), SHAPE), (dict(rows=(1 << 22) + 1), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE),
              (dict(K=B.ABQ_MAX_K + 1), SHAPE), (dict(T=0), SHAPE), (dict(T=(1 << 22) + 1), SHAPE), (dict(E=0), SHAPE), (dict(E=1025), SHAPE), (dict(top=0), SHAPE), (dict(order=None), SHAPE),
-             (dict(p=8, q=8, K=65536), SHAPE), (dict(T=1 << 22, K=1000), SHAPE), (dict(rows=1 << 22, N=1 << 16), SHAPE), (dict(N=2**31 - 1), SHAPE), (dict(stride=(1 << 20) + 8), ALIGN), (dict(stride=16384), SIZE), (dict(stride=0), SIZE)]
+             (dict(p=8, q=8, K=65536), SHAPE), (dict(T=1 << 22, K=1000), SHAPE), (dict(rows=1 << 22, N=1 << 16), SHAPE), (dict(N=2**31 - 1), SHAPE), (dict(rows=1, T=1, E=1, top=1, N=(1 << 27) + 1), SHAPE), (dict(stride=(1 << 20) + 8), ALIGN), (dict(stride=16384), SIZE), (dict(stride=0), SIZE)]
 BAD_GEMM += [(dict(layout=v), LAYOUT) for v in (B.ABQ_LAYOUT_PLANES, B.ABQ_LAYOUT_FIELDS_G128, B.ABQ_LAYOUT_FIELDS | B.ABQ_USE_FIELDS, 77, -1)]
 BAD_GEMM += [(dict(rows=4096, T=2048, ws=None), NULL), (dict(rows=4096, T=2048, wsb=1024), SIZE)]
 
