@@ -300,6 +300,44 @@ def test_graphs_serve_whatever_the_arrays_hold_later(abq):
         assert torch.equal(got, step())
 
 
+def test_offsets_beyond_32_bits(abq):
+    """Experts' weights, and rows that the sum reads, more than 4 GiB from the first."""
+    s = layer(4, 8, 3, 48, 512, 40)
+    packed = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    stride = 5 << 29   # 2.5 GiB
+    far = torch.empty(2 * stride + packed.shape[1], dtype=torch.uint8, device="cuda").as_strided((3, packed.shape[1]), (stride, 1))
+    far.copy_(packed)
+    for counts in ([2, 3, 1], [13, 14, 13]):
+        n = sum(counts)
+        a, starts = [t[:n].clone().cuda() for t in s["a"]], groups(counts).cuda()
+        assert torch.equal(abq.abq_moe_gemm(4, 8, 48, *a, far, starts), abq.abq_moe_gemm(4, 8, 48, *a, packed, starts))
+    del far
+    rows = (1 << 32) // 8192 + 9
+    y = torch.empty((rows, 8192), dtype=torch.float16, device="cuda")
+    y[-7:] = torch.arange(7, device="cuda")[:, None].half()
+    places = torch.tensor([[rows - 1, rows - 7, rows - 3]], dtype=torch.int32, device="cuda")
+    out = abq.abq_moe_combine(y, places, torch.tensor([[1.0, 5.0, 0.5]], device="cuda"))
+    assert (out == 8).all()
+
+
+def test_new_outputs_are_tensors_of_their_own(abq):
+    """They are made in one allocation; each has its shape and type, and nothing written to one shows in another."""
+    x = some_logits(37, 24, True).cuda()
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            got = abq.abq_moe_route(x, 3)
+            assert [(t.shape, t.dtype, t.is_contiguous()) for t in got] == [((37, 3), torch.int32, True), ((37, 3), torch.float32, True), ((25,), torch.int32, True),
+                                                                            ((111,), torch.int32, True), ((37, 3), torch.int32, True)]
+            kept = [t.clone() for t in got]
+            for i, t in enumerate(got):
+                t.fill_(-9)
+                assert all(torch.equal(g, k) for g, k in list(zip(got, kept))[i + 1:]) and (t == -9).all()
+    a = torch.nn.Parameter(torch.ones(3, device="cuda"))
+    weights = abq.abq_moe_route(x, 3)[1]
+    (weights * a).sum().backward()
+    assert torch.allclose(a.grad, weights.sum(0), rtol=1e-5)
+
+
 def test_two_streams_at_once(abq):
     one, two = torch.cuda.Stream(), torch.cuda.Stream()
     s = layer(4, 8, 8, 256, 1024, 300)
