@@ -482,11 +482,16 @@ int abq_moe_route(int tokens, int experts, int top, const void* logits, int logi
                   int renormalize, float scale, int32_t* ids, float* weights, int32_t* starts, int32_t* order, int32_t* places,
                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* The weights of one linear layer of all experts: for each expert a blob of abq_pack_weights (the same bytes), `stride` bytes apart (a multiple of 16, at
+ * least abq_packed_weight_bytes(p, N, K, layout)).  w_codes [experts][N][K], w_scale, w_zero [experts][N], device; per-channel layouts only. */
+int abq_pack_experts(int p, int experts, int N, int K, const uint8_t* w_codes, const float* w_scale, const int32_t* w_zero, int layout,
+                     void* packed_out, size_t stride, void* stream);
+
 /* One linear layer of all experts: place r, which starts[e] <= r < starts[e+1] gives to expert e, is row r of Y:
  *   Y[r,:] = dequant( A[s] . W_e^T ),   s = order[r] / top, or r where order is NULL
  * with accumulator and epilogue of abq_gemm, to the bit (the int32 accumulator is not returned).
  *   a_codes  [tokens][K] uint8 (bits above q are dropped), a_scale [tokens] float, a_zero [tokens] int32
- *   packed_w one blob of abq_pack_weights(p, N, K, ..., w_layout) for each expert, w_stride bytes apart (a multiple of 16, at least the
+ *   packed_w of abq_pack_experts, or one blob of abq_pack_weights(p, N, K, ..., w_layout) for each expert, w_stride bytes apart (a multiple of 16, at least the
  *            blob's size); field-packed per-channel blobs (AUTO, FIELDS, BOTH), else ABQ_ERR_LAYOUT
  *   starts   [experts + 1] int32, ascending from 0 (device);  order [rows] int32 (device) or NULL, then tokens = rows
  *   y_fp16   [rows][N] binary16: rows from starts[experts] on are left as they were

@@ -65,6 +65,7 @@ _SIGNATURES = {
                                   _c.c_size_t, _c.c_void_p]),
     "abq_lora_add_workspace_bytes": (_c.c_size_t, [_c.c_int] * 4),
     "abq_lora_add": (_c.c_int, [_c.c_int] * 5 + [_c.c_void_p, _c.c_int] + [_c.c_void_p] * 4 + [_c.c_void_p, _c.c_int] * 2 + [_c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "abq_pack_experts": (_c.c_int, [_c.c_int] * 4 + [_c.c_void_p] * 3 + [_c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "abq_moe_route_workspace_bytes": (_c.c_size_t, [_c.c_int] * 3),
     "abq_moe_route": (_c.c_int, [_c.c_int] * 3 + [_c.c_void_p, _c.c_int, _c.c_int, _c.c_void_p, _c.c_int, _c.c_int, _c.c_float] + [_c.c_void_p] * 6 + [_c.c_size_t, _c.c_void_p]),
     "abq_moe_gemm_workspace_bytes": (_c.c_size_t, [_c.c_int] * 7),
@@ -178,13 +179,8 @@ def abq_pack_experts(p, w_codes, w_scale, w_zero, layout=ABQ_LAYOUT_AUTO, out=No
     nbytes = max(abq_packed_weight_bytes(p, N, K, layout), 16)
     if out is None:
         out = torch.empty((E, nbytes), dtype=torch.uint8, device=w_codes.device)
-    lib = load()
     with torch.cuda.device(w_codes.device):
-        _dev(out, torch.uint8, (E, nbytes))
-        whole = lambda x: x if x.data_ptr() % 16 == 0 else x.clone()   # (a row of the stacked operands may start off a 16-byte boundary)
-        for e in range(E):
-            codes, scale, zero = whole(w_codes[e]), whole(w_scale[e]), whole(w_zero[e])
-            _check(lib.abq_pack_weights(p, N, K, _ptr(codes), _ptr(scale), _ptr(zero), layout, _ptr(out[e]), nbytes, _stream()), "abq_pack_experts")
+        _check(load().abq_pack_experts(p, E, N, K, _ptr(w_codes), _ptr(w_scale), _ptr(w_zero), layout, _ptr(_dev(out, torch.uint8, (E, nbytes))), nbytes, _stream()), "abq_pack_experts")
     return out
 
 

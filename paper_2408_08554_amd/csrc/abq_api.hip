@@ -996,6 +996,19 @@ int abq_moe_route(int tokens, int experts, int top, const void* logits, int logi
     return hip_status(launch_moe_route(g, (hipStream_t)stream));
 }
 
+int abq_pack_experts(int p, int experts, int N, int K, const uint8_t* w_codes, const float* w_scale, const int32_t* w_zero, int layout,
+                     void* packed_out, size_t stride, void* stream)
+{
+    if (!w_codes || !w_scale || !w_zero || !packed_out) return ABQ_ERR_NULL;
+    if (int e = check_bits_shape(p, N, K)) return e;
+    if (experts < 1 || experts > ABQ_MOE_MAX_EXPERTS) return ABQ_ERR_SHAPE;
+    WeightLayout L;
+    if (!make_weight_layout(p, N, K, layout, &L) || L.g128) return ABQ_ERR_LAYOUT;
+    if (misaligned(w_codes) || misaligned(w_scale) || misaligned(w_zero) || misaligned(packed_out) || stride % 16 != 0) return ABQ_ERR_ALIGN;
+    if (stride < L.total) return ABQ_ERR_SIZE;
+    return hip_status(launch_pack_weights(L, w_codes, w_scale, w_zero, (uint8_t*)packed_out, (hipStream_t)stream, experts, stride));
+}
+
 // Rows, and workgroups of 64 x 128 outputs, that a launch can have; packed rows of A and the channels' parameters below 4 GiB (their offsets have 32 bits).
 static int check_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int w_layout)
 {

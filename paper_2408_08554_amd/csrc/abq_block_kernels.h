@@ -475,66 +475,73 @@ __host__ __device__ constexpr int bk_expert_s(int p, int bm, int tw, int room)
 }
 __host__ __device__ constexpr int bk_most(int a, int b, int c) { return a > b ? (a > c ? a : c) : (b > c ? b : c); }
 
-// OCC: waves per SIMD that the registers are held to.  PRM: BlockParams or BlockExpertParams.
-template <int P, int RW, int CW, int MT, int NT, int S, int OCC, class PRM = BlockParams>
-__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(PRM prm)
+// OCC: waves per SIMD that the registers are held to.
+template <int P, int RW, int CW, int MT, int NT, int S, int OCC>
+__global__ __launch_bounds__(64 * RW * CW, OCC) void block_kernel(BlockParams prm)
 {
-    constexpr bool kExperts = std::is_same<PRM, BlockExpertParams>::value;
+    constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW, kSlow = bk_slow_bytes(P, kTW, bk_slow_ahead(false, S));
+    __shared__ __align__(1024) uint8_t ring[S * bk_buf_bytes(P, kBM, kTW)];
+    __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
+    __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
+    // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD)
+    const int nwg = prm.tiles_m * prm.tiles_n;
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    const int per = nwg >> 3, rem = nwg & 7;
+    const int vid = xcd * per + min(xcd, rem) + slot;
+    const int band = vid / (prm.band_m * prm.tiles_n), in_band = vid - band * prm.band_m * prm.tiles_n;
+    const int band_rows = min(prm.band_m, prm.tiles_m - band * prm.band_m);
+    const int m_blk = band * prm.band_m + in_band % band_rows, n_blk = in_band / band_rows;
+    const BlockTile at{{prm.fields[0], prm.fields[1], prm.fields[2]}, prm.wparams, prm.M, 0, m_blk * kBM, n_blk * kBN, n_blk * kTW};
+    block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+}
+
+// Of experts: workgroup tiles of one expert's rows each.  A last block of few rows takes a shorter body, with a ring of its own; a tile's place in the order
+// goes by its height, tallest first (a body's time is about its height's: the short ones fill the gaps at the end); of one height the experts come one
+// after the other, each in bands.  (All of them 256 rows high and in the experts' order, W4A4 2048 tokens over eight 4096->11008 took 189 us, now 165.)
+template <int P, int RW, int CW, int MT, int NT, int S, int OCC>
+__global__ __launch_bounds__(64 * RW * CW, OCC) void expert_block_kernel(BlockExpertParams prm)
+{
     constexpr int kBM = 16 * MT * RW, kTW = NT * CW, kBN = 16 * kTW;
-    // (of experts: the heights of the shorter bodies, in sixteens, and their rings)
-    constexpr bool kTall = kExperts && MT == 8, kMiddle = kExperts && MT == 4 && RW == 2;
+    // heights of the shorter bodies, in sixteens of RW, and their rings
+    constexpr bool kTall = MT == 8, kMiddle = MT == 4 && RW == 2;
     constexpr int MB = kTall ? 6 : (kMiddle ? 3 : MT), MC = kTall ? 4 : MB, kRoom = kTall ? 160 : 80;
     constexpr int SB = kTall || kMiddle ? bk_expert_s(P, 16 * MB * RW, kTW, kRoom) : S, SC = kTall ? bk_expert_s(P, 16 * MC * RW, kTW, kRoom) : SB;
-    constexpr int kRings = bk_most(S * bk_buf_bytes(P, kBM, kTW), SB * bk_buf_bytes(P, 16 * MB * RW, kTW), SC * bk_buf_bytes(P, 16 * MC * RW, kTW));
-    constexpr int kSlows = bk_most(bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, S)), bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, SB)), bk_slow_bytes(P, kTW, bk_slow_ahead(kExperts, SC)));
-    __shared__ __align__(1024) uint8_t ring[kRings];
-    __shared__ __align__(1024) uint8_t lds_slow[kSlows > 0 ? kSlows : 16];
+    constexpr int kRing = bk_most(S * bk_buf_bytes(P, kBM, kTW), SB * bk_buf_bytes(P, 16 * MB * RW, kTW), SC * bk_buf_bytes(P, 16 * MC * RW, kTW));
+    constexpr int kSlow = bk_most(bk_slow_bytes(P, kTW, S), bk_slow_bytes(P, kTW, SB), bk_slow_bytes(P, kTW, SC));
+    __shared__ __align__(1024) uint8_t ring[kRing];
+    __shared__ __align__(1024) uint8_t lds_slow[kSlow > 0 ? kSlow : 16];
     __shared__ __align__(16) RowParams par_a[(kBM + 63) / 64 * 64], par_w[(kBN + 63) / 64 * 64];
     const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
     BlockTile at;
-    if constexpr (kExperts) {
-        // Of experts: a tile's place in the order by the height of the body that it takes, tallest first (the bodies' times are their heights': the short
-        // ones fill the gaps at the end), of one height the experts one after the other, each in bands.
-        int left = prm.tiles_m, taken = 0, before = 0;   // units that may come yet; workgroups of the XCD's, and extra ones, that taller tiles have
-        auto some = [&](auto of) -> bool {
-            const ExpertUnits<decltype(of)> units(prm.g, of, left);
-            left -= units.total;
-            const int nwg = units.total * prm.tiles_n, per = nwg >> 3, rem = nwg & 7;
-            const int turn = (xcd - before) & 7, here = slot - taken;
-            taken += per + (turn < rem ? 1 : 0);
-            before += rem;
-            if (slot >= taken) return false;
-            const int vid = turn * per + min(turn, rem) + here;
-            const ExpertAt e = units.find(prm.g, vid / prm.tiles_n);
-            const int in_expert = vid - e.before * prm.tiles_n, tiles_m = of(e.rows), last = (e.rows + kBM - 1) / kBM;
-            const int band = in_expert / (prm.band_m * prm.tiles_n), in_band = in_expert - band * prm.band_m * prm.tiles_n;
-            const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
-            const int m_blk = decltype(of)::kLast ? last - 1 : band * prm.band_m + in_band % band_rows;
-            const int n_blk = in_band / band_rows;
-            at = BlockTile{{prm.fields[0] + (size_t)e.expert * prm.w_stride, prm.fields[1] + (size_t)e.expert * prm.w_stride, prm.fields[2] + (size_t)e.expert * prm.w_stride},
-                           reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(prm.wparams) + (size_t)e.expert * prm.w_stride),
-                           e.rows, e.first, m_blk * kBM, n_blk * kBN, n_blk * kTW};
-            return true;
-        };
-        if constexpr (kTall) {
-            if (some(BlocksBetween<256, 192, 256>{})) block_body<P, RW, CW, 8, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, SC>(prm, at, ring, lds_slow, par_a, par_w);
-        } else if constexpr (kMiddle) {
-            if (some(BlocksBetween<128, 96, 128>{})) block_body<P, RW, CW, 4, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-            else if (some(BlocksBetween<128, 0, 96>{})) block_body<P, RW, CW, 3, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
-        } else if (some(BlocksOf{kBM})) {   // (the grid is what there can be at most)
-            block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
-        }
-    } else {
-        // tile order: as in tiled_kernel (a contiguous run of the banded order per XCD)
-        const int nwg = prm.tiles_m * prm.tiles_n;
-        const int per = nwg >> 3, rem = nwg & 7;
-        const int vid = xcd * per + min(xcd, rem) + slot;
-        const int band = vid / (prm.band_m * prm.tiles_n), in_band = vid - band * prm.band_m * prm.tiles_n;
-        const int band_rows = min(prm.band_m, prm.tiles_m - band * prm.band_m);
-        const int m_blk = band * prm.band_m + in_band % band_rows, n_blk = in_band / band_rows;
-        at = BlockTile{{prm.fields[0], prm.fields[1], prm.fields[2]}, prm.wparams, prm.M, 0, m_blk * kBM, n_blk * kBN, n_blk * kTW};
+    int left = prm.tiles_m, taken = 0, before = 0;   // units that may come yet; workgroups of the XCD's, and extra ones, that taller tiles have
+    auto some = [&](auto of) -> bool {
+        const ExpertUnits<decltype(of)> units(prm.g, of, left);
+        left -= units.total;
+        const int nwg = units.total * prm.tiles_n, per = nwg >> 3, rem = nwg & 7;
+        const int turn = (xcd - before) & 7, here = slot - taken;
+        taken += per + (turn < rem ? 1 : 0);
+        before += rem;
+        if (slot >= taken) return false;
+        const int vid = turn * per + min(turn, rem) + here;
+        const ExpertAt e = units.find(prm.g, vid / prm.tiles_n);
+        const int in_expert = vid - e.before * prm.tiles_n, tiles_m = of(e.rows), last = (e.rows + kBM - 1) / kBM;
+        const int band = in_expert / (prm.band_m * prm.tiles_n), in_band = in_expert - band * prm.band_m * prm.tiles_n;
+        const int band_rows = min(prm.band_m, tiles_m - band * prm.band_m);
+        const int m_blk = decltype(of)::kLast ? last - 1 : band * prm.band_m + in_band % band_rows;
+        const int n_blk = in_band / band_rows;
+        at = BlockTile{{prm.fields[0] + (size_t)e.expert * prm.w_stride, prm.fields[1] + (size_t)e.expert * prm.w_stride, prm.fields[2] + (size_t)e.expert * prm.w_stride},
+                       reinterpret_cast<const RowParams*>(reinterpret_cast<const uint8_t*>(prm.wparams) + (size_t)e.expert * prm.w_stride),
+                       e.rows, e.first, m_blk * kBM, n_blk * kBN, n_blk * kTW};
+        return true;
+    };
+    if constexpr (kTall) {
+        if (some(BlocksBetween<256, 192, 256>{})) block_body<P, RW, CW, 8, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+        else if (some(BlocksBetween<256, 128, 192>{})) block_body<P, RW, CW, 6, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
+        else if (some(BlocksBetween<256, 0, 128>{})) block_body<P, RW, CW, 4, NT, SC>(prm, at, ring, lds_slow, par_a, par_w);
+    } else if constexpr (kMiddle) {
+        if (some(BlocksBetween<128, 96, 128>{})) block_body<P, RW, CW, 4, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
+        else if (some(BlocksBetween<128, 0, 96>{})) block_body<P, RW, CW, 3, NT, SB>(prm, at, ring, lds_slow, par_a, par_w);
+    } else if (some(BlocksOf{kBM})) {   // (the grid is what there can be at most)
         block_body<P, RW, CW, MT, NT, S>(prm, at, ring, lds_slow, par_a, par_w);
     }
 }
@@ -570,9 +577,9 @@ static hipError_t block_experts_launch(const BlockExpertParams& prm, int shape, 
 {
     const unsigned grid = (unsigned)(prm.tiles_m * prm.tiles_n);
     switch (shape) {
-        case 0: block_kernel<P, 2, 4, 8, bk_expert_nt(P), bk_expert_s(P, 256, 4 * bk_expert_nt(P), 160), 2, BlockExpertParams><<<grid, 512, 0, s>>>(prm); break;
-        case 3: block_kernel<P, 2, 2, 4, 4, bk_expert_s(P, 128, 8, 80), 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
-        case 4: block_kernel<P, 1, 4, 4, 2, bk_expert_s(P, 64, 8, 80), 2, BlockExpertParams><<<grid, 256, 0, s>>>(prm); break;
+        case 0: expert_block_kernel<P, 2, 4, 8, bk_expert_nt(P), bk_expert_s(P, 256, 4 * bk_expert_nt(P), 160), 2><<<grid, 512, 0, s>>>(prm); break;
+        case 3: expert_block_kernel<P, 2, 2, 4, 4, bk_expert_s(P, 128, 8, 80), 2><<<grid, 256, 0, s>>>(prm); break;
+        case 4: expert_block_kernel<P, 1, 4, 4, 2, bk_expert_s(P, 64, 8, 80), 2><<<grid, 256, 0, s>>>(prm); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

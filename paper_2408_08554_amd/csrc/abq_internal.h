@@ -82,7 +82,8 @@ bool make_act_layout(int q, int M, int K, int layout, ActLayout* out);
 
 // ---- kernel launchers (each returns the hipError_t of the launch) --------------------------
 hipError_t launch_pack_weights(const WeightLayout& L, const uint8_t* w_codes, const float* w_scale,
-                               const int32_t* w_zero, uint8_t* blob, hipStream_t s);
+                               const int32_t* w_zero, uint8_t* blob, hipStream_t s,
+                               int experts = 1, size_t step = 0);   // (step: bytes from one expert's blob to the next)
 hipError_t launch_pack_weights_g128(const WeightLayout& L, const uint8_t* w_codes, const uint16_t* w_scale_half,
                                     const int32_t* w_zero, uint8_t* blob, hipStream_t s);
 hipError_t launch_unpack_weights(const WeightLayout& L, const uint8_t* blob, int which, uint8_t* out, hipStream_t s);

@@ -8,9 +8,11 @@
 namespace abq {
 
 // ---- blob header -----------------------------------------------------------------------------
-__global__ void write_header_kernel(uint32_t* hdr, uint32_t magic, int bits, int R, int K, int layout)
+// (One blob, or of experts one for every blockIdx.y, `step` bytes apart; the same below.)
+__global__ void write_header_kernel(uint32_t* hdr, uint32_t magic, int bits, int R, int K, int layout, size_t step = 0)
 {
     const int t = threadIdx.x;
+    hdr += blockIdx.y * (step / 4);
     uint32_t v = 0;
     if (t == 0) v = magic;
     else if (t == 1) v = 1;          // format version
@@ -24,8 +26,10 @@ __global__ void write_header_kernel(uint32_t* hdr, uint32_t magic, int bits, int
 // ---- 1-bit planes: [bits][R][Kw] words, bit (k mod 32) of word k/32 ---------------------------
 // One thread per output word; codes above K are zero bits.
 __global__ void pack_planes_kernel(const uint8_t* __restrict__ codes, int bits, int R, int K, int Kw,
-                                   uint32_t* __restrict__ planes)
+                                   uint32_t* __restrict__ planes, size_t step = 0)
 {
+    codes += blockIdx.y * ((size_t)R * K);
+    planes += blockIdx.y * (step / 4);
     const size_t total = (size_t)R * Kw;
     const size_t idx = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (idx >= total) return;
@@ -63,8 +67,10 @@ __global__ void unpack_planes_kernel(const uint32_t* __restrict__ planes, int bi
 // 128 is then filled with that group's zero-point instead of 0, so that (w - zero) vanishes there.
 __global__ void pack_fields_kernel(const uint8_t* __restrict__ w, int N, int K, int b, int shift, int chunks,
                                    size_t total_dwords, uint32_t* __restrict__ out, const int32_t* __restrict__ pad_zero = nullptr,
-                                   int ngroups128 = 0)
+                                   int ngroups128 = 0, size_t step = 0)
 {
+    w += blockIdx.y * ((size_t)N * K);
+    out += blockIdx.y * (step / 4);
     const size_t idx = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (idx >= total_dwords) return;
     const int j = (int)(idx & 3), l = (int)((idx >> 2) & 63);
@@ -114,8 +120,12 @@ __global__ void unpack_fields_kernel(const uint8_t* __restrict__ blob, WeightLay
 // One wave per row: sum of the (masked) codes, plus copies of scale and zero.
 __global__ void row_params_kernel(const uint8_t* __restrict__ codes, int bits, int R, int K,
                                   const float* __restrict__ scale, const int32_t* __restrict__ zero,
-                                  RowParams* __restrict__ out)
+                                  RowParams* __restrict__ out, size_t step = 0)
 {
+    codes += blockIdx.y * ((size_t)R * K);
+    scale += blockIdx.y * (size_t)R;
+    zero += blockIdx.y * (size_t)R;
+    out += blockIdx.y * (step / sizeof(RowParams));
     const int row = blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (row >= R) return;
@@ -444,19 +454,20 @@ __global__ void read_params_kernel(const RowParams* __restrict__ p, int R, float
 static inline unsigned blocks_for(size_t n, int block) { return (unsigned)((n + block - 1) / block); }
 
 hipError_t launch_pack_weights(const WeightLayout& L, const uint8_t* w, const float* w_scale, const int32_t* w_zero,
-                               uint8_t* blob, hipStream_t s)
+                               uint8_t* blob, hipStream_t s, int experts, size_t step)
 {
-    write_header_kernel<<<1, 64, 0, s>>>((uint32_t*)blob, kMagicW, L.p, L.N, L.K, L.layout);
-    row_params_kernel<<<blocks_for(L.N, 4), 256, 0, s>>>(w, L.p, L.N, L.K, w_scale, w_zero, (RowParams*)(blob + L.off_params));
+    const unsigned E = (unsigned)experts;
+    write_header_kernel<<<dim3(1, E), 64, 0, s>>>((uint32_t*)blob, kMagicW, L.p, L.N, L.K, L.layout, step);
+    row_params_kernel<<<dim3(blocks_for(L.N, 4), E), 256, 0, s>>>(w, L.p, L.N, L.K, w_scale, w_zero, (RowParams*)(blob + L.off_params), step);
     if (L.has_planes) {
         const size_t words = (size_t)L.N * L.Kw;
-        pack_planes_kernel<<<blocks_for(words, 256), 256, 0, s>>>(w, L.p, L.N, L.K, L.Kw, (uint32_t*)(blob + L.off_planes));
+        pack_planes_kernel<<<dim3(blocks_for(words, 256), E), 256, 0, s>>>(w, L.p, L.N, L.K, L.Kw, (uint32_t*)(blob + L.off_planes), step);
     }
     if (L.has_fields) {
         for (int g = 0; g < L.ngroups; ++g) {
             const size_t dwords = (size_t)L.NT * L.chunks[g] * 256;
-            pack_fields_kernel<<<blocks_for(dwords, 256), 256, 0, s>>>(w, L.N, L.K, L.gb[g], L.gs[g], L.chunks[g], dwords,
-                                                                      (uint32_t*)(blob + L.off_fields[g]));
+            pack_fields_kernel<<<dim3(blocks_for(dwords, 256), E), 256, 0, s>>>(w, L.N, L.K, L.gb[g], L.gs[g], L.chunks[g], dwords,
+                                                                                (uint32_t*)(blob + L.off_fields[g]), nullptr, 0, step);
         }
     }
     return hipGetLastError();

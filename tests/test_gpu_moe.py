@@ -232,6 +232,17 @@ def test_no_rows_at_all(abq):
     check_gemm(abq, 4, 8, [0] * 8, 64, 256, top=2, behind=700)
 
 
+@pytest.mark.parametrize("p,E,N,K", [(1, 3, 17, 65), (3, 1, 16, 512), (4, 5, 33, 1001), (6, 2, 1, 1), (7, 4, 100, 640), (8, 70, 40, 300)])
+def test_packed_together_as_one_by_one(abq, p, E, N, K):
+    w = [t.cuda() for t in layer(p, 8, E, N, K, 1, seed=p)["w"]]
+    for layout in (0, abq.ABQ_LAYOUT_PLANES, abq.ABQ_LAYOUT_BOTH):
+        got = abq.abq_pack_experts(p, *w, layout=layout, out=torch.zeros((E, abq.abq_packed_weight_bytes(p, N, K, layout)), dtype=torch.uint8, device="cuda"))
+        for e in range(E):
+            one = torch.zeros_like(got[e])
+            abq.abq_pack_weights(p, *(t[e].clone() for t in w), layout=layout, out=one)
+            assert torch.equal(got[e], one), f"expert {e}"
+
+
 def test_blobs_that_hold_planes_too(abq):
     check_gemm(abq, 4, 8, [3, 5], 64, 512, top=2, layout=abq.ABQ_LAYOUT_BOTH)
     check_gemm(abq, 5, 8, [90, 50], 64, 512, top=2, layout=abq.ABQ_LAYOUT_BOTH)

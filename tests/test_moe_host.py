@@ -48,6 +48,17 @@ def test_combine_refuses(kw, want):
     assert combine(**kw) == want
 
 
+def pack(p=4, E=4, N=128, K=256, w=A16, s=A16, z=A16, layout=0, out=A16, stride=1 << 20):
+    return B.load().abq_pack_experts(p, E, N, K, w, s, z, layout, out, stride, None)
+
+
+@pytest.mark.parametrize("kw,want", [({n: None}, NULL) for n in ("w", "s", "z", "out")] + [({n: A16 + 8}, ALIGN) for n in ("w", "s", "z", "out")] +
+                         [(dict(p=0), BITS), (dict(p=9), BITS), (dict(E=0), SHAPE), (dict(E=1025), SHAPE), (dict(E=-1), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=B.ABQ_MAX_K + 1), SHAPE),
+                          (dict(stride=(1 << 20) + 8), ALIGN), (dict(stride=16384), SIZE), (dict(stride=0), SIZE), (dict(layout=B.ABQ_LAYOUT_FIELDS_G128), LAYOUT), (dict(layout=77), LAYOUT)])
+def test_pack_refuses(kw, want):
+    assert pack(**kw) == want
+
+
 def test_workspace_queries():
     """Zero for what the call refuses, and where the calls need none."""
     assert B.abq_moe_route_workspace_bytes(1, 8, 2) == 0 and B.abq_moe_route_workspace_bytes(0, 8, 2) == 0 and B.abq_moe_route_workspace_bytes(300, 8, 9) == 0
