@@ -336,10 +336,10 @@ __device__ __forceinline__ void expert_starts(const RouteParams& prm, const int3
 __host__ __device__ constexpr int route_threads(int VPL, bool biased) { return VPL >= 16 && biased ? 512 : 1024; }
 
 // What bounds it: one token is latency (a launch, the logits, `top` rounds of a maximum over 16 lanes); many tokens are the vector ALU: a
-// round is some 3 VPL + 10 operations for the four tokens of a wave.  Up to kRouteOne tokens are one launch of one workgroup, which also sorts
+// round is some 3 VPL + 10 operations for the four tokens of a wave.  Few are one launch of one workgroup, which also sorts
 // the rows; more are a launch that chooses and counts, a workgroup per chunk, and a second one whose workgroups add the counts of the chunks before
 // theirs and place their rows (no atomics on memory: the same rows in the same order every time).  Measured: one token of eight experts 3.4 us, 64 of 128
-// (binary32) 7.2, 4099 of 64 with a bias 5.6 + 7.4, 32768 of 128 (binary16) 10.7 + 9.4.
+// (binary32) 7.2, 4099 of 64 with a bias 5.5 + 6.5, 32768 of 128 (binary16) 10.7 + 9.4.
 template <int LPT, int VPL, int KIND, bool HALF>
 __global__ __launch_bounds__(route_threads(VPL, KIND == 2)) void moe_route_kernel(RouteParams prm)
 {
@@ -388,8 +388,9 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     for (int i = tid; i < 2 * prm.padded + max(waves * E, prm.padded); i += blockDim.x) lds[i] = 0;
     __syncthreads();
     // the chunks' counts: threads side by side along the experts (eight each), groups of them along the chunks, a thread's loads all in flight (sums of whole
-    // numbers: any order)
-    const int eights = prm.padded / 8, wide = min(eights, (int)blockDim.x), groups = blockDim.x / wide, group = tid / wide;
+    // numbers: any order), no more groups than take eight chunks each: with few experts all of them add to the same words one after the other (300 tokens of eight
+    // experts took 20.6 us with every thread a group, 7.0 now)
+    const int eights = prm.padded / 8, wide = min(eights, (int)blockDim.x), groups = min((int)blockDim.x / wide, (prm.chunks + 7) / 8), group = tid / wide;
     const uint4* hist = reinterpret_cast<const uint4*>(prm.hist);
     if (group < groups)
         for (int f = tid % wide; f < eights; f += wide) {
@@ -432,16 +433,16 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     for (int64_t i = all + (int64_t)blockIdx.x * blockDim.x + tid; i < (int64_t)g.tokens * g.top; i += (int64_t)gridDim.x * blockDim.x) g.order[i] = -1;
 }
 
-// Tokens of a single launch; of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which
+// Tokens, and logits, of a single launch, whose one workgroup has one unit's vector ALU (256 tokens of 256 experts with a bias, all in one: 80 us, 15 now); of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which
 // reads all chunks' counts and has room for the rows of place_room().
-constexpr int kRouteOne = 256, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
+constexpr int kRouteOne = 512, kRouteOneLogits = 8192, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
 
 static int place_threads(int experts) { return experts <= 512 ? 1024 : 512; }   // (the counts of every wave in 64 KiB of LDS)
 static int place_room(int experts) { return place_threads(experts) * kPlaceRounds; }
 
 static void route_chunks(int tokens, int experts, int top, int* chunk, int* chunks)
 {
-    *chunk = tokens <= kRouteOne ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
+    *chunk = tokens <= kRouteOne && tokens * experts <= kRouteOneLogits ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
     *chunks = (tokens + *chunk - 1) / *chunk;
 }
 
@@ -635,12 +636,12 @@ struct CombineParams {
     int64_t ldout;
 };
 
-// One workgroup per token and run of 256 eights of its row; the terms are added in the order of the choices, in binary32.  Memory bounds it: 4099 tokens of
+// One workgroup per token and run of up to 256 eights of its row; the terms are added in the order of the choices, in binary32.  Memory bounds it: 4099 tokens of
 // eight rows of 5120 87 us, 4.8 TB/s.
 __global__ __launch_bounds__(256) void moe_combine_kernel(CombineParams prm)
 {
     const int64_t t = blockIdx.x;
-    const int v = blockIdx.y * 256 + threadIdx.x;
+    const int v = blockIdx.y * blockDim.x + threadIdx.x;
     if (8 * v >= prm.N) return;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     uint32_t h[4];
@@ -670,7 +671,8 @@ hipError_t launch_moe_combine(int tokens, int N, int rows, int top, const uint16
                               const uint16_t* add, int ldadd, uint16_t* out, int ldout, hipStream_t s)
 {
     const CombineParams prm{N, rows, top, y, ldy, places, weights, add, ldadd, out, ldout};
-    moe_combine_kernel<<<dim3((unsigned)tokens, (unsigned)((N + 2047) / 2048)), 256, 0, s>>>(prm);
+    const int eights = (N + 7) / 8, threads = std::min(256, (eights + 63) / 64 * 64);
+    moe_combine_kernel<<<dim3((unsigned)tokens, (unsigned)((eights + threads - 1) / threads)), threads, 0, s>>>(prm);
     return hipGetLastError();
 }
 
