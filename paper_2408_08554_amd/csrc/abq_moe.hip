@@ -433,16 +433,20 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
     for (int64_t i = all + (int64_t)blockIdx.x * blockDim.x + tid; i < (int64_t)g.tokens * g.top; i += (int64_t)gridDim.x * blockDim.x) g.order[i] = -1;
 }
 
-// Tokens, and logits, of a single launch, whose one workgroup has one unit's vector ALU (256 tokens of 256 experts with a bias, all in one: 80 us, 15 now); of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which
-// reads all chunks' counts and has room for the rows of place_room().
-constexpr int kRouteOne = 512, kRouteOneLogits = 8192, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
+// A single launch is for so many tokens and logits at most, and for so many rounds of its one workgroup, which has one unit's vector ALU (a round of 1024 lanes
+// takes 0.2 to 0.45 us, the two launches together about 9; 256 tokens of 256 experts with a bias, all in one: 80 us, 15 now; 436 of eight, top 6, with a bias
+// 26, 9.4 now).  Of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which reads all
+// chunks' counts and has room for the rows of place_room().
+constexpr int kRouteOne = 512, kRouteOneLogits = 8192, kRouteOneRounds = 16, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
 
+static int route_lanes(int experts) { return experts <= 256 ? 16 : 64; }   // lanes of a token
 static int place_threads(int experts) { return experts <= 512 ? 1024 : 512; }   // (the counts of every wave in 64 KiB of LDS)
 static int place_room(int experts) { return place_threads(experts) * kPlaceRounds; }
 
 static void route_chunks(int tokens, int experts, int top, int* chunk, int* chunks)
 {
-    *chunk = tokens <= kRouteOne && tokens * experts <= kRouteOneLogits ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
+    const int64_t rounds = ((int64_t)tokens * route_lanes(experts) + 1023) / 1024 * top;
+    *chunk = tokens <= kRouteOne && tokens * experts <= kRouteOneLogits && rounds <= kRouteOneRounds ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
     *chunks = (tokens + *chunk - 1) / *chunk;
 }
 
@@ -473,7 +477,7 @@ hipError_t launch_moe_route(const MoeRouteArgs& g, hipStream_t s)
     prm.hist = (uint16_t*)g.workspace;
     prm.padded = (g.experts + 7) / 8 * 8;
     prm.bits = g.experts > 1 ? 32 - __builtin_clz((unsigned)g.experts - 1) : 0;
-    const int E = g.experts, lpt = E <= 256 ? 16 : 64;
+    const int E = g.experts, lpt = route_lanes(E);
     const int64_t lanes = (int64_t)prm.chunk * lpt;
     const unsigned most = (unsigned)place_threads(E);
     const unsigned routing = std::min(most, (unsigned)route_threads((E > 128 && E <= 256) || E > 512 ? 16 : 8, g.bias != nullptr));

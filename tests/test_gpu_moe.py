@@ -45,7 +45,7 @@ def test_tokens(abq, T):
         check_route(abq, some_logits(T, 130, T % 2 == 1, T), 7, renormalize=False)
 
 
-@pytest.mark.parametrize("T,E,top", [(512, 16, 16), (513, 16, 16), (512, 1, 1), (513, 1, 1), (64, 128, 16), (65, 128, 16), (32, 256, 16), (33, 256, 16), (8, 1024, 16), (9, 1024, 16), (31, 257, 16), (700, 8, 2), (2000, 4, 4)])
+@pytest.mark.parametrize("T,E,top", [(512, 16, 16), (513, 16, 16), (512, 1, 1), (513, 1, 1), (64, 128, 16), (65, 128, 16), (32, 256, 16), (33, 256, 16), (8, 1024, 16), (9, 1024, 16), (31, 257, 16), (128, 16, 8), (129, 16, 8), (64, 60, 16), (436, 8, 6), (700, 8, 2), (2000, 4, 4)])
 def test_at_the_border_of_one_launch(abq, T, E, top):
     for half in (True, False):
         check_route(abq, some_logits(T, E, half, T), top)
