@@ -530,7 +530,9 @@ static bool rows_plan(int p, int K, MoePlan* pl)
 // Rows of an expert, as far as the host knows: their mean.  The few-rows kernel passes over an expert's weights once for every 16 rows that one has, the
 // block kernel's 64 x 128 tiles once for 64, which costs it a launch that packs A; they meet at 8 rows, at 14 where a weight has one or two bits
 // (us, few / block: W4A8 eight of 4096->4096, 8 rows 15.4 / 15.7, 12 rows 20.9 / 15.8, 32 rows 33 / 16.3; W2A8 thirty-two 8 rows 29 / 39, 12 rows 35 / 40, 16 rows
-// 40 / 41, 32 rows 65 / 43).  Tiles of up to 256 rows are ahead from 80 rows an expert on where there are 1.2 of them to a compute unit, from 192 on with 0.7; of up to 128
+// 40 / 41, 32 rows 65 / 43).  Where the block kernel's tiles leave half the units without one, its time is that of one tile, 5.5 us and 0.22 or 0.32 a step, and the
+// few-rows kernel's its passes' bytes at 5.7 TB/s and 3.5 us: the lesser of the two, up to 96 rows (us, few / block: W5A8 67 rows of eight 448->320 5.7 / 9.5,
+// W8A8 10 rows of eight 4096->512 8.1 / 14.5, W4A8 25 rows of eight 8192->1024 14.8 / 19.2, W8A8 32 rows of four 4096->2048 18.3 / 15.1).  Tiles of up to 256 rows are ahead from 80 rows an expert on where there are 1.2 of them to a compute unit, from 192 on with 0.7; of up to 128
 // rows from 100 on with one to a unit (us, 64 / 128 / 256 rows a tile: W4A8 eight of 4096->4096, 90 rows 26 / 28 / 35, 144 rows 32 / 30 / 45; of 4096->11008, 110
 // rows 70 / 70 / 66, 180 rows 98 / 94 / 83; W3A8 eight of 8192->2048, 180 rows 41 / 46 / 71; W8A8 sixty-four of 1408->2048, 180 rows 91 / 86 / 78).  Over 58 such
 // sizes the choice takes 1.007 times the best shape's time, 1.09 at most.
@@ -538,11 +540,16 @@ static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int ex
 {
     MoePlan pl{};
     const double mean = (double)rows / std::min(experts, rows);   // rows of an expert
-    if (K >= 16 && mean <= (p <= 2 ? 14 : 8) && rows_plan(p, K, &pl)) return pl;
     const auto tiles = [&](int shape) {   // about: the last block of an expert is part of one
         const int bm = expert_bm(shape), bn = expert_bn(p, shape);
         return std::min(experts, rows) * std::max(1.0, mean / bm + 0.3) * ((N + bn - 1) / bn);
     };
+    bool few = mean <= (p <= 2 ? 14 : 8);
+    if (!few && mean <= 96 && tiles(4) <= 0.5 * num_cus()) {
+        const double passes = mean / 16 + 0.5, weights = (double)std::min(experts, rows) * p * N * K / 8;
+        few = 3.5 + passes * weights / 5.7e6 < 5.5 + (K + 127) / 128 * (p <= 4 ? 0.22 : 0.32);
+    }
+    if (K >= 16 && few && rows_plan(p, K, &pl)) return pl;
     pl.shape = (mean >= 80 && tiles(0) >= 1.2 * num_cus()) || (mean >= 192 && tiles(0) >= 0.7 * num_cus()) ? 0 : (mean >= 100 && tiles(3) >= num_cus() ? 3 : 4);
     return pl;
 }

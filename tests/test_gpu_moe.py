@@ -177,6 +177,15 @@ def test_widths(abq, p, q):
     check_gemm(abq, p, q, [300, 256], 528, 1024, top=2, seed=p)
 
 
+@pytest.mark.parametrize("q", [3, 8])
+@pytest.mark.parametrize("p", range(1, 9))
+def test_widths_of_64_rows(abq, p, q):
+    """Enough channels for tiles of 64 rows: whole and ragged ones, with and without order."""
+    check_gemm(abq, p, q, [70, 33, 64, 0, 1], 4400 + 8 * p, 640, top=2, seed=p, behind=4)
+    check_gemm(abq, p, q, [20, 32, 17], 8193, 130, seed=p)
+    check_gemm(abq, p, q, [65] + [16] * 40, 523, 257, top=3, seed=p)
+
+
 @pytest.mark.parametrize("K", [1, 7, 15, 16, 17, 31, 63, 64, 65, 100, 127, 500, 511, 512, 513, 1000, 1408, 2047, 4095, 5121, 8193, 12289, 16383])
 @pytest.mark.parametrize("top", [0, 3])
 def test_lengths_that_divide_nothing(abq, K, top):
@@ -206,6 +215,8 @@ def test_columns_that_divide_nothing(abq, N):
     for counts in ([1], [3, 0, 12], [40, 25], [100, 150], [500, 230]):
         check_gemm(abq, 4, 8, counts, N, 320, top=2, seed=N)
         check_gemm(abq, 6, 6, counts, N, 200, seed=N, behind=3)
+    for counts in ([40, 25, 0, 60], [100] * 3):   # (wide enough for blocks)
+        check_gemm(abq, 4, 8, counts, 6144 + N, 320, top=2, seed=N)
 
 
 @pytest.mark.parametrize("counts", [[0, 0, 0, 5], [5, 0, 0, 0], [0] * 70 + [3] + [0] * 60 + [1, 2], [1] * 64, [1] * 65, [17] + [1] * 40, [100] + [1] * 12, [1000] + [0] * 40 + [1] * 3,
@@ -229,6 +240,7 @@ def test_heights_of_the_last_block(abq, p):
 def test_k_that_ends_inside_a_super_chunk(abq, p, K):
     """Every number of steps modulo the super-chunk's four, on every height of tile."""
     check_gemm(abq, p, 8, [1, 33, 64, 40], 144, K, top=2, seed=K)
+    check_gemm(abq, p, 8, [1, 33, 64, 40], 4400, K, top=2, seed=K)
     if K % 256 == 0 or p in (2, 7):
         check_gemm(abq, p, 8, [140, 128, 150], 11008, K, seed=K)
         check_gemm(abq, p, 8, [300, 128, 180, 200], 11008, K, top=2, seed=K)
