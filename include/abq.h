@@ -475,8 +475,8 @@ int abq_lora_add(int M, int N, int K, int rank, int adapters, const uint16_t* x,
  *   starts   [experts + 1] int32: expert e has the places starts[e] .. starts[e+1] - 1, in the order of their slots
  *   order    [tokens * top] int32: the slot at each place, -1 behind the last one
  *   1 <= experts <= ABQ_MOE_MAX_EXPERTS, 1 <= top <= min(experts, ABQ_MOE_MAX_TOP), tokens * top <= 2^22
- *   workspace at least abq_moe_route_workspace_bytes(...) bytes (0 for few tokens); contents on entry are irrelevant, calls that
- *            may overlap need one each. */
+ *   workspace at least abq_moe_route_workspace_bytes(...) bytes (0 for few tokens; never falls as tokens grow, so that one of the
+ *            largest batch serves all); contents on entry are irrelevant, calls that may overlap need one each. */
 size_t abq_moe_route_workspace_bytes(int tokens, int experts, int top);
 int abq_moe_route(int tokens, int experts, int top, const void* logits, int logits_bits, int ld, const float* bias, int sigmoid,
                   int renormalize, float scale, int32_t* ids, float* weights, int32_t* starts, int32_t* order, int32_t* places,
@@ -499,7 +499,7 @@ int abq_pack_experts(int p, int experts, int N, int K, const uint8_t* w_codes, c
  * not ascend, and entries of order that name no row of A, leave the rows concerned with unspecified contents.
  *   1 <= rows, tokens <= 2^22;  N <= 2^27;  tokens * K (K rounded up to 512) < 2^32;  (rows / 64 + experts) * ceil(N / 128) < 2^24;
  *   the rest as for abq_gemm.  Workspace: at least abq_moe_gemm_workspace_bytes(...) bytes (0 where an expert has few rows: the codes
- *   are packed on the way there); contents on entry are irrelevant, calls that may overlap need one each. */
+ *   are packed on the way there; never falls as rows and tokens grow together); contents on entry are irrelevant, calls that may overlap need one each. */
 size_t abq_moe_gemm_workspace_bytes(int p, int q, int rows, int N, int K, int tokens, int experts);
 int abq_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, int top,
                  const uint8_t* a_codes, const float* a_scale, const int32_t* a_zero, const void* packed_w, size_t w_stride, int w_layout,

@@ -443,18 +443,25 @@ static int route_lanes(int experts) { return experts <= 256 ? 16 : 64; }   // la
 static int place_threads(int experts) { return experts <= 512 ? 1024 : 512; }   // (the counts of every wave in 64 KiB of LDS)
 static int place_room(int experts) { return place_threads(experts) * kPlaceRounds; }
 
+static int route_longest(int experts, int top) { return std::min(kRouteLongest, place_room(experts) / top); }   // tokens of a chunk, at most
+
 static void route_chunks(int tokens, int experts, int top, int* chunk, int* chunks)
 {
     const int64_t rounds = ((int64_t)tokens * route_lanes(experts) + 1023) / 1024 * top;
-    *chunk = tokens <= kRouteOne && tokens * experts <= kRouteOneLogits && rounds <= kRouteOneRounds ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), std::min(kRouteLongest, place_room(experts) / top));
+    *chunk = tokens <= kRouteOne && tokens * experts <= kRouteOneLogits && rounds <= kRouteOneRounds ? tokens : std::min(std::max(kRouteTokens, (tokens + kRouteChunks - 1) / kRouteChunks), route_longest(experts, top));
     *chunks = (tokens + *chunk - 1) / *chunk;
 }
 
+// Counts of the most chunks that so many tokens or fewer are cut into, so that a workspace of the largest batch serves all: a chunk grows by whole tokens, and
+// their number falls where it does (8192 tokens are 512 chunks, 8193 are 482).
 size_t moe_route_workspace_bytes(int tokens, int experts, int top)
 {
     int chunk, chunks;
     route_chunks(tokens, experts, top, &chunk, &chunks);
-    return chunks == 1 ? 0 : (size_t)chunks * ((experts + 7) / 8 * 8) * sizeof(uint16_t);
+    if (chunks == 1) return 0;   // (and for fewer tokens)
+    const int longest = route_longest(experts, top);
+    const int most = std::max(std::min((tokens + kRouteTokens - 1) / kRouteTokens, kRouteChunks), (tokens + longest - 1) / longest);
+    return (size_t)most * ((experts + 7) / 8 * 8) * sizeof(uint16_t);
 }
 
 template <int LPT, int VPL>

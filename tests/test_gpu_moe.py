@@ -123,6 +123,19 @@ def test_strides_and_given_outputs(abq):
         assert all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+@pytest.mark.parametrize("experts,top,most", [(128, 8, 16385), (16, 2, 8704), (640, 4, 9000)])
+def test_one_workspace_of_the_largest_batch(abq, experts, top, most):
+    """It serves every smaller batch, and nothing behind its end is written."""
+    need = abq.abq_moe_route_workspace_bytes(most, experts, top)
+    around = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    x = torch.randn(most, experts, generator=torch.Generator().manual_seed(top)).half().cuda()
+    for T in (most, 8192, 8193, 700, 5, 4097):
+        want = abq.abq_moe_route(x[:T], top)
+        got = abq.abq_moe_route(x[:T], top, workspace=around[:need])
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), f"{T} tokens"
+        assert (around[need:] == 0x5A).all()
+
+
 def test_every_token_to_the_same_experts(abq):
     x = torch.zeros(3000, 32)
     x[:, 5], x[:, 30] = 2.0, 1.0

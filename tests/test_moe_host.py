@@ -67,6 +67,24 @@ def test_workspace_queries():
     assert B.abq_moe_gemm_workspace_bytes(4, 8, 4096, 128, 256, 2048, 4) >= 2048 * 512
 
 
+@pytest.mark.parametrize("experts,top", [(1, 1), (8, 2), (64, 6), (128, 8), (256, 16), (512, 16), (513, 16), (1024, 1)])
+def test_the_routers_workspace_never_falls_as_tokens_grow(experts, top):
+    """So that one of the largest batch serves every smaller one."""
+    most = (1 << 22) // top
+    tokens = sorted({t for t in [*range(1, 20000), *(c * 512 + d for c in range(1, most // 512, 97) for d in (-1, 0, 1)), *range(most - 600, most + 1)] if 1 <= t <= most})
+    sizes = [B.abq_moe_route_workspace_bytes(t, experts, top) for t in tokens]
+    falls = [(a, b) for a, b, x, y in zip(tokens, tokens[1:], sizes, sizes[1:]) if y < x]
+    assert not falls, f"{len(falls)} times, first from {falls[0][0]} to {falls[0][1]} tokens"
+    assert sizes[-1] > 0
+
+
+@pytest.mark.parametrize("p,experts,top,N,K", [(4, 8, 2, 512, 4096), (8, 64, 6, 320, 448), (2, 128, 8, 1408, 2048), (1, 1, 1, 64, 8), (5, 8, 2, 4096, 14336)])
+def test_the_products_workspace_never_falls_as_tokens_grow(p, experts, top, N, K):
+    for gather in (True, False):   # (down projections: as many rows of codes as rows)
+        sizes = [B.abq_moe_gemm_workspace_bytes(p, 8, t * top, N, K, t if gather else t * top, experts) for t in range(1, 3000)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[-1] > 0
+
+
 def test_operands_on_the_host_are_refused():
     """Every operand is a device tensor; the binding says so before anything is launched."""
     x = torch.zeros(4, 8)
