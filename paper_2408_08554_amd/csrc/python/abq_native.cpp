@@ -889,7 +889,7 @@ PyObject* moe_route(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject
     Workspace ws;
     if (!t.workspace(a[6], abq_moe_route_workspace_bytes(T, E, top), &ws)) return nullptr;
     if (!call_on("abq_moe_route", *t.on, [&] {
-            if (T > (1 << 22) || top > ABQ_MOE_MAX_TOP || top > E) return ABQ_ERR_SHAPE;   // (before anything of that size is allocated)
+            if ((int64_t)T * top > (1 << 22) || E > ABQ_MOE_MAX_EXPERTS || top > ABQ_MOE_MAX_TOP || top > E) return ABQ_ERR_SHAPE;   // (before anything of that size is allocated)
             if (!given) make_together(out, shapes, types, 5, *t.on);
             void* wsp = ws.make(*t.on);
             return abq_moe_route(T, E, top, x->data_ptr(), x->scalar_type() == at::kHalf ? 16 : 32, ld, (const float*)bp, sigmoid, renormalize, (float)scale, (int32_t*)out[0].ptr,
@@ -933,7 +933,7 @@ PyObject* moe_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject*
     Workspace ws;
     if (!t.output(a[11], "y", rows, N, &y) || !t.workspace(a[12], abq_moe_gemm_workspace_bytes(p, q, rows, N, K, T, E), &ws)) return nullptr;
     if (!call_on("abq_moe_gemm", *t.on, [&] {
-            if (rows < 1 || N < 1) return ABQ_ERR_SHAPE;   // (sizes that no tensor has)
+            if (rows < 1 || N < 1 || rows > (1 << 22) || T > (1 << 22) || N > (1 << 27) || E > ABQ_MOE_MAX_EXPERTS) return ABQ_ERR_SHAPE;   // (before anything of that size is allocated)
             uint16_t* yp = y.half(rows, N, *t.on);
             void* wsp = ws.make(*t.on);
             return abq_moe_gemm(p, q, rows, N, K, T, E, top, (const uint8_t*)cp, (const float*)sp, (const int32_t*)zp, w->data_ptr(), (size_t)stride, layout, (const int32_t*)tp,

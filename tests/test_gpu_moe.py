@@ -381,6 +381,23 @@ def test_new_outputs_are_tensors_of_their_own(abq):
     assert torch.allclose(a.grad, weights.sum(0), rtol=1e-5)
 
 
+def test_refused_sizes_take_no_memory(abq):
+    """Outputs of a size that the library refuses are not made first."""
+    routes = [(torch.zeros((1 << 18) + 1, 16, dtype=torch.float16, device="cuda"), 16), (torch.zeros(1000, 1025, device="cuda"), 16)]
+    rows = (1 << 22) + 1
+    a = torch.zeros((1, 16), dtype=torch.uint8, device="cuda"), torch.ones(1, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    w = torch.zeros((2, abq.abq_packed_weight_bytes(4, 256, 16)), dtype=torch.uint8, device="cuda")
+    starts, order = groups([3, 4]).cuda(), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for call in [lambda x=x, top=top: abq.abq_moe_route(x, top) for x, top in routes] + [lambda: abq.abq_moe_gemm(4, 8, 256, *a, w, starts, order=order)]:
+        with pytest.raises(abq.AbqError) as e:
+            call()
+        assert e.value.status == abq.ABQ_ERR_SHAPE
+    assert torch.cuda.max_memory_allocated() == before
+
+
 def test_two_streams_at_once(abq):
     one, two = torch.cuda.Stream(), torch.cuda.Stream()
     s = layer(4, 8, 8, 256, 1024, 300)
