@@ -907,14 +907,17 @@ PyObject* moe_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject*
     HANDLE_TH_ERRORS
     PyObject* a[13];
     Operands t;
-    int n3[3], T, K, E, rows, blob, top = 1, layout = ABQ_LAYOUT_AUTO;
+    int n3[3], T, K, E, rows, top = 1, layout = ABQ_LAYOUT_AUTO;
     void *cp, *sp, *zp, *tp, *op = nullptr;
     if (!sig_moe_gemm.parse(args, nargs, kw, a) || !to_ints(a, 3, n3) || (!is_none(a[9]) && !to_int(a[9], &top)) || (!is_none(a[10]) && !to_int(a[10], &layout))) return nullptr;
     const int p = n3[0], q = n3[1], N = n3[2];
     const at::Tensor* c = tensor(a[3]);
     if (!c || !rows_cols(c, &T, &K) || !t.whole(a[3], "a_codes", at::kByte, c->sizes(), &cp) || !t.whole(a[4], "a_scale", at::kFloat, {T}, &sp) || !t.whole(a[5], "a_zero", at::kInt, {T}, &zp)) return nullptr;
     const at::Tensor* w = tensor(a[6]);
-    if (!w || !rows_cols(w, &E, &blob)) return nullptr;
+    if (!w) return nullptr;
+    if (w->dim() != 2) return PyErr_SetString(PyExc_ValueError, "packed_w: a tensor of two dimensions"), nullptr;
+    const int64_t blob = w->size(1);   // (of one expert, 2 GiB and more it may be)
+    if (!fits_int(w->size(0), &E)) return nullptr;
     if (!w->is_cuda() || w->scalar_type() != at::kByte || w->stride(1) != 1) return t.refuse(*w, "packed_w", "Byte, contiguous rows"), nullptr;
     if (!t.same_device(*w, "packed_w")) return nullptr;
     if (!t.whole(a[7], "starts", at::kInt, {(int64_t)E + 1}, &tp)) return nullptr;

@@ -363,6 +363,25 @@ def test_offsets_beyond_32_bits(abq):
     assert (out == 8).all()
 
 
+@pytest.mark.parametrize("N,K,few", [((1 << 19) + 4099, 4096, True), ((1 << 17) + 67, 16512, False)])
+def test_experts_of_more_than_2_gib(abq, N, K, few):
+    """One expert's weights beyond 2 GiB of codes and of blob, on both kernels: columns at either end and around the 2 GiB."""
+    n = 3
+    g = torch.Generator(device="cuda").manual_seed(K)
+    codes = torch.randint(0, 256, (2, N, K), generator=g, device="cuda", dtype=torch.uint8)
+    s = layer(8, 8, 2, 1, K, 2 * n)
+    scale, zero = torch.rand(2, N, generator=g, device="cuda") / 2**14, torch.randint(0, 256, (2, N), generator=g, device="cuda", dtype=torch.int32)
+    assert (abq.abq_moe_gemm_workspace_bytes(8, 8, 2 * n, N, K, 2 * n, 2) == 0) == few
+    w = abq.abq_pack_experts(8, codes, scale, zero)
+    assert w.shape[1] > 1 << 31
+    starts = groups([n, n])
+    got = abq.abq_moe_gemm(8, 8, N, *(t.cuda() for t in s["a"]), w, starts.cuda())
+    for at in (0, (1 << 31) // K - 16, N - 32):
+        at = slice(at, at + 32)
+        want = gemm(*s["a"], codes[:, at].cpu(), scale[:, at].cpu(), zero[:, at].cpu(), 8, 8, starts, None, 1, 2 * n)
+        assert torch.equal(got[:, at].cpu().view(torch.int16), want.view(torch.int16)), f"columns from {at.start}"
+
+
 def test_new_outputs_are_tensors_of_their_own(abq):
     """They are made in one allocation; each has its shape and type, and nothing written to one shows in another."""
     x = some_logits(37, 24, True).cuda()
