@@ -314,6 +314,40 @@ def test_arrays_that_name_nothing_touch_nothing_else(abq):
             assert (y.view(torch.int16).cpu()[~mine] == POISON).all()
 
 
+def kernel_of(abq, p, q, counts, N, K, top=0, behind=0):
+    """Whether the product packs its codes for the block kernel, or takes them as they are in the few-rows kernel."""
+    rows = sum(counts) + behind
+    return "block" if abq.abq_moe_gemm_workspace_bytes(p, q, rows, N, K, -(-rows // top) if top else rows, len(counts)) else "few rows"
+
+
+# Means of 110, and of 220 rows an expert, with tiles for every unit: 128 and 256 rows a workgroup (192 channels there for p = 7).
+@pytest.mark.parametrize("p,E,rows,N", [(4, 10, 1100, 4100), (7, 10, 1100, 4100), (4, 24, 5300, 2050), (7, 24, 5300, 2050), (8, 70, 16100, 600), (2, 130, 14300, 300)])
+def test_arrays_that_name_nothing_on_tall_tiles(abq, p, E, rows, N):
+    """Starts that name more tiles than there can be, fewer, or rows outside: what no expert has stays, and what lies around Y. The same launch serves
+    starts that ascend right after."""
+    K, T = 130, 64
+    assert kernel_of(abq, p, 8, [rows // E] * (E - 1) + [rows - rows // E * (E - 1)], N, K) == "block"
+    s = layer(p, 8, E, N, K, T, seed=E)
+    w = abq.abq_pack_experts(p, *(t.cuda() for t in s["w"]))
+    a = [t.cuda() for t in s["a"]]
+    g = torch.Generator().manual_seed(rows)
+    for starts in (([0, 5, -3, 1 << 30, 7, 40, 9] * E)[:E] + [rows // 2], list(range(-E, 1)), [1 << 30] * (E + 1), [rows - rows * i // E for i in range(E + 1)],
+                   [0 if i % 2 == 0 else rows for i in range(E + 1)], [rows // 3 if i % 2 == 0 else rows - rows // 7 for i in range(E + 1)], [i * ((1 << 30) // E) for i in range(E + 1)]):
+        around = torch.full((rows + 32, N), POISON, dtype=torch.int16, device="cuda")
+        y = around[16:16 + rows].view(torch.float16)
+        order = torch.randint(-(1 << 31), (1 << 31) - 1, (rows,), generator=g).to(torch.int32).cuda()
+        abq.abq_moe_gemm(p, 8, N, *a, w, torch.tensor(starts, dtype=torch.int32).cuda(), order=order, top=2, y=y)
+        assert (around[:16] == POISON).all() and (around[16 + rows:] == POISON).all()
+        mine = torch.zeros(rows, dtype=torch.bool)
+        for lo, hi in zip(starts, starts[1:]):
+            mine[min(max(lo, 0), rows):min(max(hi, 0), rows)] = True
+        assert (y.view(torch.int16).cpu()[~mine] == POISON).all()
+    starts = torch.tensor([rows * i // E for i in range(E + 1)], dtype=torch.int32)
+    order = torch.randint(0, 2 * T, (rows,), generator=g).to(torch.int32)
+    y = abq.abq_moe_gemm(p, 8, N, *a, w, starts.cuda(), order=order.cuda(), top=2)
+    assert torch.equal(y.cpu().view(torch.int16), gemm(*s["a"], *s["w"], p, 8, starts, order, 2, rows).view(torch.int16))
+
+
 def test_graphs_serve_whatever_the_arrays_hold_later(abq):
     """Router, products and sum captured once; replayed for other logits, other codes."""
     T, E, top, N, K = 40, 16, 3, 96, 512
