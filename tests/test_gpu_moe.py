@@ -473,6 +473,31 @@ def test_two_streams_at_once(abq):
     assert all(torch.equal(g, want) for g in got)
 
 
+def test_two_streams_with_work_of_their_own(abq):
+    """Each stream its own logits, codes and results, through the calls that take workspaces (the router's counts, the packed codes): nothing is shared between them."""
+    T, E, top, N, K = 1700, 8, 2, 256, 512
+    assert abq.abq_moe_route_workspace_bytes(T, E, top) > 0 and abq.abq_moe_gemm_workspace_bytes(4, 8, T * top, N, K, T, E) > 0
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in layer(4, 8, E, N, K, 1)["w"]))
+
+    def step(x, a):
+        ids, weights, starts, order, places = abq.abq_moe_route(x, top)
+        y = abq.abq_moe_gemm(4, 8, N, *a, w, starts, order=order, top=top)
+        return ids, starts, order, y, abq.abq_moe_combine(y, places, weights)
+
+    work = [(torch.cuda.Stream(), some_logits(T, E, False, seed).cuda(), [t.cuda() for t in layer(4, 8, 1, 1, K, T, seed)["a"]]) for seed in (1, 2)]
+    want = [step(x, a) for _, x, a in work]
+    assert not any(torch.equal(one, two) for one, two in zip(*want))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(6):
+        for i, (stream, x, a) in enumerate(work):
+            with torch.cuda.stream(stream):
+                got.append((i, step(x, a)))
+    torch.cuda.synchronize()
+    for n, (i, outs) in enumerate(got):
+        assert all(torch.equal(g, w) for g, w in zip(outs, want[i])), f"call {n}"
+
+
 # ---- weighted sum ----------------------------------------------------------------------------------
 def check_combine(abq, T, top, N, rows, seed=0, add=True, missing=0.1):
     g = torch.Generator().manual_seed(seed)
