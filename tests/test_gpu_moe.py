@@ -377,6 +377,51 @@ def test_graphs_serve_whatever_the_arrays_hold_later(abq):
         assert torch.equal(got, step())
 
 
+def test_graphs_with_workspaces(abq):
+    """The same through the router's two launches and the block kernel, whose counts and packed codes lie in workspaces of the graph: every replay against the
+    64-bit form, with other eager work of the same calls in between."""
+    T, E, top, N, K = 900, 8, 2, 136, 320
+    assert abq.abq_moe_route_workspace_bytes(T, E, top) > 0 and abq.abq_moe_gemm_workspace_bytes(4, 8, T * top, N, K, T, E) > 0
+    s = layer(4, 8, E, N, K, T)
+    w = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    a = [t.cuda() for t in s["a"]]
+    x = some_logits(T, E, False).cuda()
+
+    def step(x, a):
+        routed_to = abq.abq_moe_route(x, top)
+        y = abq.abq_moe_gemm(4, 8, N, *a, w, routed_to[2], order=routed_to[3], top=top)
+        return (*routed_to, y, abq.abq_moe_combine(y, routed_to[4], routed_to[1]))
+
+    step(x, a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x, a)
+    for seed in range(5):
+        logits, codes = some_logits(T, E, False, seed + 20), layer(4, 8, 1, 1, K, T, seed + 1)["a"]
+        if seed == 1:
+            logits[:, 1:] = -INF          # every token to one expert, the other choices none
+        if seed == 3:
+            logits[::3] = -INF            # padding
+            logits[:, 2] = 50.0
+            logits[::3, 2] = -INF
+        x.copy_(logits)
+        for t, new in zip(a, codes):
+            t.copy_(new)
+        graph.replay()
+        ids, weights, starts, order, places, y, total = [t.cpu() for t in out]
+        want = routed(logits, top)
+        for name, g, r in zip(("ids", "starts", "order", "places"), (ids, starts, order, places), (want[0], want[2], want[3], want[4])):
+            assert torch.equal(g.long(), r), f"{name}, replay {seed}"
+        assert ((weights.double() - want[1]).abs() <= want[5]).all()
+        used = int(starts[-1])
+        assert torch.equal(y[:used].view(torch.int16), gemm(*codes, *s["w"], 4, 8, starts, order, top, T * top)[:used].view(torch.int16)), f"replay {seed}"
+        full, bound = combined(torch.where(torch.arange(T * top)[:, None] < used, y, 0), places, weights)
+        assert ((total.double() - full).abs() <= bound).all(), f"replay {seed}"
+        step(some_logits(T, E, False, seed + 40).cuda(), a)
+        torch.cuda.synchronize()
+
+
 def test_offsets_beyond_32_bits(abq):
     """Experts' weights, and rows that the sum reads, more than 4 GiB from the first."""
     s = layer(4, 8, 3, 48, 512, 40)
