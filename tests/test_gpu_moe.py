@@ -348,6 +348,88 @@ def test_arrays_that_name_nothing_on_tall_tiles(abq, p, E, rows, N):
     assert torch.equal(y.cpu().view(torch.int16), gemm(*s["a"], *s["w"], p, 8, starts, order, 2, rows).view(torch.int16))
 
 
+# Rows of each expert that the rule sends to the block kernel, with as many channels as each shape of its tiles wants: means of 117, 110 and 207 rows an
+# expert; too few tiles for anything but 64 rows a workgroup, enough for 128 and its shorter ones of 96, enough for 256, 192 and 128.
+TILES_OF_64 = [120, 101, 130]
+TILES_OF_128 = [97, 96, 128, 129, 0, 225, 1, 95, 224, 105]
+TILES_OF_256 = [129, 1, 256, 192, 0, 193, 128, 64, 257, 384, 385, 255, 448, 449, 0, 512, 17, 320, 130, 200, 100, 191, 250, 127]
+
+
+def check_block(abq, p, q, counts, N, K, top=0, behind=0, **kw):
+    assert kernel_of(abq, p, q, counts, N, K, top, behind) == "block"
+    check_gemm(abq, p, q, counts, N, K, top=top, behind=behind, **kw)
+
+
+@pytest.mark.parametrize("q", [1, 4, 7, 8])
+@pytest.mark.parametrize("p", range(1, 9))
+def test_widths_on_every_tile(abq, p, q):
+    """Every pair of widths on tiles of 64, 128 and 256 rows and their shorter ones, and on the few-rows kernel with one to four super-chunks a wave."""
+    check_block(abq, p, q, TILES_OF_64, 80 + p, 640, top=2, seed=p)
+    check_block(abq, p, q, TILES_OF_128, 4096 + 4 * p, 192, seed=p, behind=3)
+    check_block(abq, p, q, TILES_OF_256, 2048 + 8 * p, 200, top=3, seed=q)
+    for K in (1024, 8704, 12288) + ((14336, 16384) if p <= 4 else ()):
+        assert kernel_of(abq, p, q, [2, 0, 7], 40, K, 2) == "few rows"
+        check_gemm(abq, p, q, [2, 0, 7], 40, K, top=2, seed=p)
+
+
+@pytest.mark.parametrize("K", [1, 7, 15, 16, 17, 31, 63, 64, 65, 100, 127, 500, 511, 512, 513, 1000, 1408, 2047, 4095, 5121, 8193, 12289, 16385])
+@pytest.mark.parametrize("top", [0, 3])
+def test_lengths_that_divide_nothing_on_blocks(abq, K, top):
+    for p, q in ((4, 8), (3, 5), (8, 8)):
+        check_block(abq, p, q, [140, 0, 160, 1, 199], 40, K, top=top, seed=K)
+
+
+@pytest.mark.parametrize("N", [1, 2, 7, 15, 17, 33, 127, 129, 191, 193, 255])
+def test_columns_that_divide_nothing_on_blocks(abq, N):
+    check_block(abq, 4, 8, TILES_OF_64, N, 320, top=2, seed=N)
+    check_block(abq, 4, 8, TILES_OF_128, 4096 + N, 96, top=2, seed=N)
+    check_block(abq, 6, 6, TILES_OF_256, 2048 + N, 96, seed=N, behind=2)
+    check_block(abq, 8, 8, TILES_OF_256, 2048 + N, 96, seed=N)
+
+
+# Row sums of 2^23 and more, up to the longest K: the epilogue's 32-bit multiplies.
+@pytest.mark.parametrize("p,q,K", [(8, 8, 33000), (4, 8, 40000), (1, 8, 131072)])
+@pytest.mark.parametrize("counts,N", [([4, 5], 40), ([129, 91], 14200), ([260, 180], 19800)])
+def test_sums_of_more_than_24_bits(abq, p, q, K, counts, N):
+    """64, 128 and 256 rows a workgroup; columns at either end and in the middle."""
+    rows = sum(counts)
+    assert kernel_of(abq, p, q, counts, N, K) == "block" and K * (2**max(p, q) - 1) >= 1 << 23
+    g = torch.Generator(device="cuda").manual_seed(K)
+    codes = torch.randint(0, 2**p, (2, N, K), generator=g, device="cuda", dtype=torch.uint8)
+    scale, zero = (torch.rand(2, N, generator=g, device="cuda") + 0.5) / (K**0.5 * 2**p), torch.randint(0, 2**p, (2, N), generator=g, device="cuda", dtype=torch.int32)
+    a, starts = layer(p, q, 1, 1, K, rows)["a"], groups(counts)
+    got = abq.abq_moe_gemm(p, q, N, *(t.cuda() for t in a), abq.abq_pack_experts(p, codes, scale, zero), starts.cuda())
+    for at in (0, N // 2, N - 17):
+        at = slice(at, at + 17)
+        want = gemm(*a, codes[:, at].cpu(), scale[:, at].cpu(), zero[:, at].cpu(), p, q, starts, None, 1, rows)
+        assert torch.equal(got[:, at].cpu().view(torch.int16), want.view(torch.int16)), f"columns from {at.start}"
+
+
+def test_blobs_that_hold_planes_too_on_blocks(abq):
+    check_block(abq, 5, 8, TILES_OF_64, 64, 512, top=2, layout=abq.ABQ_LAYOUT_BOTH)
+    check_block(abq, 3, 8, TILES_OF_128, 4100, 130, layout=abq.ABQ_LAYOUT_BOTH)
+
+
+@pytest.mark.parametrize("p,q,counts,N,K", [(8, 8, [130, 122], 2048, 1408), (6, 6, [190, 175], 1003, 4096), (4, 8, [130, 99, 120], 12000, 1024), (4, 4, [500, 612], 16384, 512)])
+def test_same_bits_as_the_products_of_one_expert_on_blocks(abq, p, q, counts, N, K):
+    assert kernel_of(abq, p, q, counts, N, K) == "block"
+    test_same_bits_as_the_products_of_one_expert(abq, p, q, counts, N, K)
+
+
+@pytest.mark.parametrize("counts,N", [([130, 97, 200], 48), ([190, 0, 140], 16500), ([600, 500, 700], 6200)])
+def test_offsets_beyond_32_bits_on_blocks(abq, counts, N):
+    """The second and third expert's weights 2.5 and 5 GiB from the first, on tiles of 64, 128 and 256 rows."""
+    K, n = 512, sum(counts)
+    assert kernel_of(abq, 4, 8, counts, N, K) == "block"
+    s = layer(4, 8, 3, N, K, n)
+    packed = abq.abq_pack_experts(4, *(t.cuda() for t in s["w"]))
+    stride = 5 << 29
+    far = torch.empty(2 * stride + packed.shape[1], dtype=torch.uint8, device="cuda").as_strided((3, packed.shape[1]), (stride, 1))
+    far.copy_(packed)
+    a, starts = [t.cuda() for t in s["a"]], groups(counts).cuda()
+    assert torch.equal(abq.abq_moe_gemm(4, 8, N, *a, far, starts), abq.abq_moe_gemm(4, 8, N, *a, packed, starts))
+
+
 def test_graphs_serve_whatever_the_arrays_hold_later(abq):
     """Router, products and sum captured once; replayed for other logits, other codes."""
     T, E, top, N, K = 40, 16, 3, 96, 512
