@@ -543,6 +543,59 @@ def test_experts_of_more_than_2_gib(abq, N, K, few):
         assert torch.equal(got[:, at].cpu().view(torch.int16), want.view(torch.int16)), f"columns from {at.start}"
 
 
+@pytest.mark.parametrize("T,E,top,half", [(1 << 22, 8, 1, False), (1 << 18, 1024, 16, True), ((1 << 19) - 5, 513, 8, False), (700001, 64, 5, True), ((1 << 22) - 3, 520, 1, True)])
+def test_the_routers_largest_batches(abq, T, E, top, half):
+    """The most rows there can be, the longest chunks, logits past 4 GiB. (Choices compared on the device, in pieces.)"""
+    g = torch.Generator(device="cuda").manual_seed(E)
+    x = torch.empty((T, E), dtype=torch.float16 if half else torch.float32, device="cuda").normal_(generator=g)
+    x[::7] = -INF
+    ids, weights, starts, order, places = abq.abq_moe_route(x, top)
+    for at in range(0, T, 1 << 16):
+        piece = x[at:at + (1 << 16)].float()
+        for j in range(top):   # the largest that is left, the first of equals
+            best = torch.where(piece == piece.amax(1, keepdim=True), torch.arange(E, device="cuda"), E).amin(1)
+            best = torch.where(piece.amax(1) > -INF, best, -1)
+            assert torch.equal(ids[at:at + (1 << 16), j].long(), best), f"tokens from {at}, choice {j}"
+            piece.scatter_(1, best.clamp(min=0)[:, None], -INF)
+    there = ids >= 0
+    assert ((weights.sum(1) - there.any(1).float()).abs() < 1e-5).all()
+    flat = torch.where(there, ids, E).flatten()
+    by_expert, slots = torch.sort(flat, stable=True)
+    assert torch.equal(starts.long(), torch.searchsorted(by_expert, torch.arange(E + 1, device="cuda")))
+    assert torch.equal(order.long(), torch.where(by_expert < E, slots, -1))
+    want = torch.empty_like(slots)
+    want[slots] = torch.arange(len(slots), device="cuda")
+    assert torch.equal(places.flatten().long(), torch.where(flat < E, want, -1))
+
+
+def check_far_rows(abq, p, q, N, K, T, counts, order, look):
+    """Rows `look` of Y, of codes that are made on the device."""
+    g = torch.Generator(device="cuda").manual_seed(K)
+    codes = torch.empty((T, K), dtype=torch.uint8, device="cuda").random_(0, 256, generator=g)
+    scale, zero = torch.rand(T, generator=g, device="cuda") / 64, torch.randint(0, 2**q, (T,), generator=g, device="cuda", dtype=torch.int32)
+    w, starts = layer(p, q, len(counts), N, K, 1)["w"], groups(counts)
+    y = abq.abq_moe_gemm(p, q, N, codes, scale, zero, abq.abq_pack_experts(p, *(t.cuda() for t in w)), starts.cuda(), order=order)
+    src = look if order is None else order.cpu()[look].long()
+    expert = torch.searchsorted(starts.long(), look, right=True) - 1
+    for e in range(len(counts)):
+        mine = look[expert == e]
+        if len(mine):
+            at = src[expert == e].cuda()
+            want = gemm(codes[at].cpu(), scale[at].cpu(), zero[at].cpu(), *w, p, q, groups([0] * e + [len(mine)] + [0] * (len(counts) - e - 1)), None, 1, len(mine))
+            assert torch.equal(y[mine.cuda()].cpu().view(torch.int16), want.view(torch.int16)), f"expert {e}"
+
+
+def test_the_products_largest_batches(abq):
+    """The most rows there can be, codes and outputs of more than 4 GiB, on both kernels."""
+    T = (1 << 22) - 1
+    ends = lambda n: torch.cat([torch.arange(0, 300), torch.arange(n // 3 - 150, n // 3 + 150), torch.arange(n // 2 - 150, n // 2 + 150), torch.arange(n - 300, n)])
+    check_far_rows(abq, 4, 8, 24, 1000, T, [T // 3, T // 2 - T // 3, T - T // 2], None, ends(T))
+    check_far_rows(abq, 4, 8, 24, 1000, T, [3, 0, 5], torch.tensor([T - 1, 0, T - 2, T // 2, T - 1, 7, T - 600, T // 2 + 1], dtype=torch.int32, device="cuda"), torch.arange(8))
+    n = 1 << 18
+    check_far_rows(abq, 8, 8, 16400, 16, n, [n // 3, n // 2 - n // 3, n - n // 2], None, ends(n))
+    check_far_rows(abq, 2, 8, 1 << 20, 16, 2100, [700, 700, 700], None, torch.tensor([0, 699, 700, 2098, 2099]))
+
+
 def test_new_outputs_are_tensors_of_their_own(abq):
     """They are made in one allocation; each has its shape and type, and nothing written to one shows in another."""
     x = some_logits(37, 24, True).cuda()
