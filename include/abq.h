@@ -510,7 +510,7 @@ int abq_moe_gemm(int p, int q, int rows, int N, int K, int tokens, int experts, 
  * over the choices whose place is in 0..rows-1 (add NULL: without it; a shared expert's output, or the residual).
  *   y [rows][N] row stride ldy, add, out [tokens][N] row strides ldadd, ldout (binary16, strides in elements, any value >= N); out may be add
  *   itself (same stride), and overlaps nothing else;  weights [tokens][top] float, places [tokens][top] int32 (device)
- *   1 <= tokens, rows <= 2^22, 1 <= N <= 2^20, tokens * ceil(N / 2048) < 2^24 */
+ *   1 <= tokens, rows <= 2^22, 1 <= top <= ABQ_MOE_MAX_EXPERTS, 1 <= N <= 2^20, tokens * ceil(N / 2048) < 2^24 */
 int abq_moe_combine(int tokens, int N, int rows, int top, const uint16_t* y, int ldy, const int32_t* places, const float* weights,
                     const uint16_t* add, int ldadd, uint16_t* out, int ldout, void* stream);
 

@@ -435,7 +435,10 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(RouteParams prm)
 
 // A single launch is for so many tokens and logits at most, and for so many rounds of its one workgroup, which has one unit's vector ALU (a round of 1024 lanes
 // takes 0.2 to 0.45 us, the two launches together about 9; 256 tokens of 256 experts with a bias, all in one: 80 us, 15 now; 436 of eight, top 6, with a bias
-// 26, 9.4 now).  Of more, chunks of kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which reads all
+// 26, 9.4 now).  At the bounds (us, one / two launches, binary32, and with a bias): 64 of 128, top 8, 7.9 / 9.7, 14.1 / 12.1; 128 of 64, top 2, 7.0 / 8.7,
+// 11.2 / 9.5; 32 of 256, top 8, 8.0 / 11.2, 14.9 / 15.4; 512 of 16, top 2, 12.0 / 8.5, 20.2 / 9.1; past them 128 of 128, top 2, 8.1 / 9.2, 16.3 / 10.5; 256 of
+// 64, top 2, 9.5 / 8.8, 17.9 / 9.5.  (So two launches would be ahead earlier where few experts have many tokens, and where there is a bias.)  Of more, chunks of
+// kRouteTokens (about kRouteChunks longer ones of many), placed by about kPlacers workgroups, each of which reads all
 // chunks' counts and has room for the rows of place_room().
 constexpr int kRouteOne = 512, kRouteOneLogits = 8192, kRouteOneRounds = 16, kRouteTokens = 16, kRouteLongest = 4096, kRouteChunks = 512, kPlacers = 128;
 
@@ -539,11 +542,14 @@ static bool rows_plan(int p, int K, MoePlan* pl)
 // (us, few / block: W4A8 eight of 4096->4096, 8 rows 15.4 / 15.7, 12 rows 20.9 / 15.8, 32 rows 33 / 16.3; W2A8 thirty-two 8 rows 29 / 39, 12 rows 35 / 40, 16 rows
 // 40 / 41, 32 rows 65 / 43).  Where the block kernel's tiles leave half the units without one, its time is that of one tile, 5.5 us and 0.22 or 0.32 a step, and the
 // few-rows kernel's its passes' bytes at 5.7 TB/s and 3.5 us: the lesser of the two, up to 96 rows (us, few / block: W5A8 67 rows of eight 448->320 5.7 / 9.5,
-// W8A8 10 rows of eight 4096->512 8.1 / 14.5, W4A8 25 rows of eight 8192->1024 14.8 / 19.2, W8A8 32 rows of four 4096->2048 18.3 / 15.1).  Tiles of up to 256 rows are ahead from 80 rows an expert on where there are 1.2 of them to a compute unit, from 192 on with 0.7; of up to 128
-// rows from 100 on with one to a unit (us, 64 / 128 / 256 rows a tile: W4A8 eight of 4096->4096, 90 rows 26 / 28 / 35, 144 rows 32 / 30 / 45; of 4096->11008, 110
-// rows 70 / 70 / 66, 180 rows 98 / 94 / 83; W3A8 eight of 8192->2048, 180 rows 41 / 46 / 71; W8A8 sixty-four of 1408->2048, 180 rows 91 / 86 / 78).  Over 58 such
-// sizes the choice takes 1.007 times the best shape's time, 1.09 at most.
-static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int experts)
+// W8A8 10 rows of eight 4096->512 8.1 / 14.5, W4A8 25 rows of eight 8192->1024 14.8 / 19.2, W8A8 32 rows of four 4096->2048 18.3 / 15.1; over 40 sizes with so few
+// tiles the choice takes 1.02 times the lesser time, 1.31 at most: W8A8 37 rows of thirty-two 320->384 11.1 / 8.5).  Tiles of up to 256 rows are ahead from 80 rows
+// an expert on where there are 1.2 of them to a compute unit, from 192 on with 0.7; of up to 128 rows from 100 on with one to a unit (us, 64 / 128 / 256 rows a tile:
+// W4A8 eight of 4096->4096, 90 rows 26 / 28 / 35, 144 rows 32 / 30 / 45; of 4096->11008, 110 rows 70 / 70 / 66, 180 rows 98 / 94 / 83; W3A8 eight of 8192->2048, 180
+// rows 41 / 46 / 71; W8A8 sixty-four of 1408->2048, 180 rows 91 / 86 / 78).  Over 58 drawn sizes of all kinds the choice takes 1.02 times the best kernel's time, 1.20 at
+// most.  Rows that are spread less evenly than their mean cost 1.5 times at most of what was measured: 32 tokens that all choose the same two of eight
+// W4A8 4096->11008, 22.4 us in two passes, 16.1 with blocks (14.9 where one expert has all rows).
+static MoePlan moe_plan(int p, int rows, int N, int K, int experts)
 {
     MoePlan pl{};
     const double mean = (double)rows / std::min(experts, rows);   // rows of an expert
@@ -563,7 +569,7 @@ static MoePlan moe_plan(int p, int q, int rows, int N, int K, int tokens, int ex
 
 size_t moe_gemm_workspace_bytes(int p, int q, int rows, int N, int K, int tokens, int experts)
 {
-    if (moe_plan(p, q, rows, N, K, tokens, experts).few) return 0;
+    if (moe_plan(p, rows, N, K, experts).few) return 0;
     ActLayout A;
     make_act_layout(q, tokens, K, ABQ_LAYOUT_FIELDS, &A);
     return A.total;
@@ -573,7 +579,7 @@ static MoeGroups groups_of(const MoeGemmArgs& g) { return MoeGroups{g.starts, g.
 
 hipError_t launch_moe_gemm(const MoeGemmArgs& g, const WeightLayout& W, hipStream_t s)
 {
-    const MoePlan pl = moe_plan(g.p, g.q, g.rows, g.N, g.K, g.tokens, g.experts);
+    const MoePlan pl = moe_plan(g.p, g.rows, g.N, g.K, g.experts);
     if (pl.few) {
         MoeRowsParams prm{};
         prm.w = g.w_blobs;

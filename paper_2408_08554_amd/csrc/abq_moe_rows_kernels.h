@@ -6,8 +6,9 @@
 // grid of (part of K) x (tile of the group).  A wave keeps its part of A in registers, as operands, for as long as a run stays with the same rows
 // (unpacked codes are masked and made signed once, the sums of the codes are taken on the way), and streams weights past it: as a super-chunk
 // has been multiplied, the next tile's is asked for.  The parts of K of up to four tiles meet in LDS, and all waves add them up and store them: one barrier
-// to four tiles.  (With a barrier to every tile and its sum left to one wave, W2A8 64 rows of eight 11008->4096 took 30 us; now 20.9, 4.3 TB/s of weights; W4A8
-// one token's two experts 4096->11008 14.4 and now 11.4.)
+// to four tiles.  (With a barrier to every tile and its sum left to one wave, W2A8 64 rows of eight 11008->4096 took 30 us; now 20.8 to 25, differing from run to
+// run of the same binary, 3.7 to 4.4 TB/s of weights; W4A8 one token's two experts 4096->11008 14.4 and now 11.4.)
+// A whole row of A is in one workgroup's registers, which bounds K (moe_max_waves): 16384 up to four bits, 12288 from five on.
 #pragma once
 #include "abq_moe.h"
 #include "abq_rows.h"
